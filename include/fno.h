@@ -225,6 +225,91 @@ int fno_rel_l2_loss(int64_t n, const float* pred, const float* target, float* lo
 int fno_adam_step(int64_t n, float* param, const float* grad, float* m, float* v, double lr, double beta1,
                   double beta2, double eps, int32_t step, void* stream);
 
+/* Group norm with an activation over a field of C = channels and P = npoints points, for the C / groups channels and all
+ * points of every (batch entry, group) together:
+ *   mean, var = sum (x - mean)^2 / n, n = P C / groups;  rstd = 1 / sqrt(var + eps);  xh = (x - mean) rstd;
+ *   y = act(gamma xh + beta), gamma and beta [C], one value a channel.
+ * layout FNO_LAYOUT_CHANNELS_FIRST: [B][C][P], the layout of every other call here; FNO_LAYOUT_CHANNELS_LAST: [B][P][C].
+ * dtype is that of x, y, gy and gx: float, or bf16 (16 bits, each the upper half of a float).  Everything else is float.
+ * Sums and statistics are held in double or, over a few values, in float, whatever the dtype; bf16 results are rounded
+ * once, to nearest even.  activation: FNO_ACT_IDENTITY, FNO_ACT_GELU or FNO_ACT_SILU (z / (1 + exp(-z))). */
+enum { FNO_ACT_SILU = 2 };       /* fno_group_norm_fwd and fno_group_norm_bwd only */
+enum { FNO_LAYOUT_CHANNELS_FIRST = 0, FNO_LAYOUT_CHANNELS_LAST = 1 };
+enum { FNO_DTYPE_F32 = 0, FNO_DTYPE_BF16 = 1 };
+typedef struct {
+  int64_t npoints;     /* P >= 0                                                      */
+  double eps;          /* >= 0, finite                                                */
+  int32_t batch;       /* B >= 1                                                      */
+  int32_t channels;    /* C, 1 .. 1024                                                */
+  int32_t groups;      /* divides C                                                   */
+  int32_t layout;      /* FNO_LAYOUT_*                                                */
+  int32_t dtype;       /* FNO_DTYPE_*                                                 */
+  int32_t activation;  /* FNO_ACT_*                                                   */
+  int32_t flags;       /* FNO_FLAG_ACCUMULATE_GRADS (of the backward call) or 0       */
+} fno_norm_desc;
+
+/* Bytes of device scratch that both calls need for this descriptor (host-only). */
+int fno_group_norm_workspace_bytes(const fno_norm_desc* desc, size_t* bytes);
+
+/* Forward.  gamma, beta nullable (1 and 0); mean, rstd out float [B][groups], nullable: what the backward call needs.
+ * y may be x itself; no other overlap.  x and y 16-byte aligned, ws 256-byte aligned.  npoints = 0 gives mean 0 and
+ * rstd 1 / sqrt(eps).  An infinity or a NaN in a group makes the whole group NaN.  Fixed summation order: the same bits
+ * on every run. */
+int fno_group_norm_fwd(const fno_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
+                       float* mean, float* rstd, void* ws, size_t ws_bytes, void* stream);
+
+/* Adjoint, from the statistics that the forward call saved and the cotangent gy of y; with gz = gy act'(gamma xh + beta):
+ *   gbeta[c] = sum gz,  ggamma[c] = sum gz xh  (over batch entries and points, Sec. 2.1),
+ *   gx = rstd (gamma gz - S1 / n - xh S2 / n),  S1 = sum gamma gz, S2 = sum gamma gz xh over the group.
+ * gx, ggamma, gbeta nullable; gx is overwritten and may be gy or x itself (no other overlap); ggamma and gbeta are
+ * overwritten, or added to with FNO_FLAG_ACCUMULATE_GRADS.  gamma and beta as in the forward call. */
+int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* gamma, const float* beta,
+                       const float* mean, const float* rstd, const void* gy, void* gx, float* ggamma, float* gbeta,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* One AdamW step over many tensors (Loshchilov & Hutter, Algorithm 2: Adam, Sec. 4, with the decay apart from the
+ * gradient), in place, in as few launches as the tensors' addresses fit (64 tensors each).  For every value
+ *   g' = s g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
+ *   param = param (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),
+ * s = min(1, max_norm / *grad_norm), or 1 where grad_norm is null.  grad_norm is a device scalar (of fno_grad_norm): where
+ * it is not finite the step writes nothing at all.  Complex parameters are passed as 2n floats.  step counts from 1.
+ *
+ * state_bits 32: m and v are float [n], exps is not used.
+ * state_bits 8: m and v are bytes [n] and exps bytes [ceil(n / 256)][2], the exponents that the 256 consecutive values of
+ * a block share, m's and v's.  With E the exponent, a code's lower three bits f and the bits e above them stand for
+ * (1 + f / 8) 2^(e + E - 127 - K), code 0 for zero: v has no sign, five bits e and K = 31; m has its sign in bit 7, four bits
+ * e and K = 15.  All bytes zero are moments of zero.  E = 255 (its codes are 0): a value of the block was not finite, and every
+ * one of it is NaN from then on.  The update uses the new moments before they are rounded.  They are rounded up or down at random with the
+ * odds that keep the mean (a decay of 0.1 % a step would never move a code otherwise), by a hash of seed, step, the tensor's
+ * place in the list and the value's place in it: the same bits on every run.  A v that is not zero is at least the smallest
+ * code, so that no step is divided by a vanished v.
+ *
+ * tensors: host array, read during the call only; every pointer in it is a device pointer, param, grad, m and v 4-byte
+ * aligned, exps 2-byte.  Tensors must not overlap.  n = 0 and count = 0 are allowed. */
+typedef struct {
+  float* param;
+  const float* grad;
+  void* m;
+  void* v;
+  void* exps;            /* state_bits 8 only, else ignored */
+  int64_t n;
+  double weight_decay;
+} fno_adamw_tensor;
+int fno_adamw_step(int32_t count, const fno_adamw_tensor* tensors, int32_t state_bits, double lr, double beta1,
+                   double beta2, double eps, int32_t step, const float* grad_norm, double max_norm, uint32_t seed,
+                   void* stream);
+
+/* The Euclidean norm of all gradients of the list together, to the device scalar `norm`; sums in double in a fixed order,
+ * the same bits on every run.  param, m, v and exps of the tensors are not used.  ws: device scratch of
+ * fno_grad_norm_workspace_bytes() bytes (host-only call), 8-byte aligned. */
+int fno_grad_norm_workspace_bytes(int32_t count, const fno_adamw_tensor* tensors, size_t* bytes);
+int fno_grad_norm(int32_t count, const fno_adamw_tensor* tensors, float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* The values that moments in 8 bits stand for, as bf16, which every code is exactly: m_out[k], v_out[k] (host arrays of
+ * `count` device pointers) receive n bf16 values of tensor k.  param and grad are not used. */
+int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* const* m_out, void* const* v_out,
+                         void* stream);
+
 /* Projection to the output channels (end of Sec. 2.4) through one hidden layer, fused per point:
  *   y = W2 gelu(W1 x + b1) + b2,  W1 [hidden][c_in], W2 [c_out][hidden].  The hidden tensor is
  * never stored.  c_in <= 32, c_out <= 4. */

@@ -475,6 +475,131 @@ def adam_step(param, grad, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8
     return param - lr * mhat / (np.sqrt(vhat) + eps), m, v
 
 
+def silu(z):
+    """z / (1 + exp(-z)), through tanh so that no exponential overflows."""
+    z = np.asarray(z, np.float64)
+    return 0.5 * z * (1.0 + np.tanh(0.5 * z))
+
+
+def silu_prime(z):
+    z = np.asarray(z, np.float64)
+    s = 0.5 * (1.0 + np.tanh(0.5 * z))
+    return s + z * s * (1.0 - s)
+
+
+_ACTS = {"identity": (lambda z: z, np.ones_like), "gelu": (lambda z: gelu(z), lambda z: gelu_prime(z)),
+         "silu": (lambda z: silu(z), lambda z: silu_prime(z))}
+
+
+def group_norm_fwd(x, gamma, beta, groups, eps, act="gelu"):
+    """Group norm with an activation of x (B, C, ...), statistics over the C / groups channels and all points of
+    every (batch entry, group).  Returns (y, mean, rstd); gamma, beta None = 1, 0."""
+    x = np.asarray(x, np.float64)
+    b, c = x.shape[:2]
+    xg = x.reshape(b, groups, -1)
+    if xg.shape[2] == 0:
+        return x.copy(), np.zeros((b, groups)), np.full((b, groups), 1.0 / np.sqrt(eps))
+    mean = xg.mean(2)
+    var = ((xg - mean[:, :, None]) ** 2).mean(2)
+    with np.errstate(divide="ignore"):
+        rstd = 1.0 / np.sqrt(var + eps)
+    xh = ((xg - mean[:, :, None]) * rstd[:, :, None]).reshape(b, c, -1)
+    z = xh * (1.0 if gamma is None else np.asarray(gamma, np.float64)[None, :, None])
+    z = z + (0.0 if beta is None else np.asarray(beta, np.float64)[None, :, None])
+    return _ACTS[act][0](z).reshape(x.shape), mean, rstd
+
+
+def group_norm_bwd(x, gamma, beta, mean, rstd, groups, gy, act="gelu"):
+    """Adjoint of group_norm_fwd for a cotangent gy, from the statistics of the forward pass: the chain rule through
+    act, the affine map, and xh = (x - mean) rstd, whose mean and rstd depend on every x of the group."""
+    x, gy = np.asarray(x, np.float64), np.asarray(gy, np.float64)
+    b, c = x.shape[:2]
+    d = c // groups
+    ga = np.ones(c) if gamma is None else np.asarray(gamma, np.float64)
+    be = np.zeros(c) if beta is None else np.asarray(beta, np.float64)
+    mu, rs = (np.repeat(np.asarray(t, np.float64).reshape(b, groups), d, axis=1)[:, :, None] for t in (mean, rstd))
+    xh = (x.reshape(b, c, -1) - mu) * rs
+    gz = gy.reshape(b, c, -1) * _ACTS[act][1](xh * ga[None, :, None] + be[None, :, None])
+    gh = gz * ga[None, :, None]
+    n = max(d * xh.shape[2], 1)
+    s1 = np.repeat(gh.reshape(b, groups, -1).sum(2), d, axis=1)[:, :, None] / n
+    s2 = np.repeat((gh * xh).reshape(b, groups, -1).sum(2), d, axis=1)[:, :, None] / n
+    return {"gx": (rs * (gh - s1 - xh * s2)).reshape(x.shape), "ggamma": (gz * xh).sum((0, 2)), "gbeta": gz.sum((0, 2))}
+
+
+def adamw_step(param, grad, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, scale=1.0):
+    """One update of AdamW: Adam of the scaled gradient, and the parameter's own decay apart from it.  Returns
+    (param, m, v)."""
+    param = np.asarray(param, np.float64)
+    new, m, v = adam_step(param, scale * np.asarray(grad, np.float64), m, v, step, lr, beta1, beta2, eps)
+    return new - lr * weight_decay * param, m, v
+
+
+# Moments in 8 bits: blocks of 256 values share a power of two 2^(E - 127); a code's three lower bits f and the bits e
+# above them stand for (1 + f / 8) 2^(e + E - 127 - span), code 0 for zero.
+CODE_BLOCK = 256
+CODE_SPAN = {"m": 15, "v": 31}
+
+
+def code_values(codes, exps, which):
+    """What the codes (uint8) of a flat moment stand for, exps one shared exponent a block; E = 255 stands for NaN."""
+    codes = np.asarray(codes, np.int64)
+    e = np.repeat(np.asarray(exps, np.int64), CODE_BLOCK)[: codes.size]
+    mag = codes % 128 if which == "m" else codes
+    val = np.where(mag == 0, 0.0, np.ldexp(1.0 + (mag % 8) / 8.0, (mag // 8 + e - 127 - CODE_SPAN[which]).astype(np.int64)))
+    if which == "m":
+        val = np.where(codes >= 128, -val, val)
+    return np.where(e == 255, np.nan, val)
+
+
+def code_bits(n, seed, step, tensor):
+    """The 32 random bits of every value: a hash of seed, step, the tensor's place in the list and the value's in it."""
+    def mix(x):
+        x = np.asarray(x, np.uint64) & np.uint64(0xFFFFFFFF)
+        x = x ^ (x >> np.uint64(16))
+        x = (x * np.uint64(0xCB4F2D3B)) & np.uint64(0xFFFFFFFF)
+        x = x ^ (x >> np.uint64(13))
+        x = (x * np.uint64(0xFDB6A5C3)) & np.uint64(0xFFFFFFFF)
+        return x ^ (x >> np.uint64(16))
+
+    key = mix(mix(mix(seed) ^ np.uint64(step)) ^ np.uint64(tensor))
+    i = np.arange(n, dtype=np.uint64)
+    q = i // np.uint64(CODE_BLOCK)
+    block = mix(mix(q + key) + (q >> np.uint64(32)))
+    return mix(block + (i % np.uint64(CODE_BLOCK)) * np.uint64(0x9E3779B1)).astype(np.int64)
+
+
+def encode_moment(x, bits16, which):
+    """(codes, exps) of a flat moment x: E from the largest of a block rounded up to four significant bits; every value
+    rounded up where the part that is cut, in units of the last place, exceeds 1 - bits16 / 65536, below the smallest
+    code where it exceeds bits16 / 65536 of it.  A v that is not zero is at least the smallest code."""
+    x = np.asarray(x, np.float64)
+    span, last = CODE_SPAN[which], 127 if which == "m" else 255
+    n = x.size
+    pad = np.zeros(-(-n // CODE_BLOCK) * CODE_BLOCK)
+    pad[:n] = np.abs(x)
+    rows = pad.reshape(-1, CODE_BLOCK)
+    top = rows.max(1)                                    # NaN where a value is NaN
+    frac, power = np.frexp(np.where(np.isfinite(top) & (top > 0), top, 1.0))
+    e = power - 1 + 127 + (frac > 15.0 / 16.0)
+    e = np.where(top > 0, e, 0)
+    e = np.clip(e, span + 1, 254)
+    e = np.where(np.isfinite(top), e, 255)
+    per = np.repeat(e, CODE_BLOCK)[:n]
+    a = np.abs(x)
+    least = np.ldexp(1.125, (per - 127 - span).astype(np.int64))
+    _, power = np.frexp(np.where(np.isfinite(a) & (a > 0), a, 1.0))
+    q = np.floor(np.ldexp(np.where(np.isfinite(a), a, 0.0), (4 - power).astype(np.int64)) + np.asarray(bits16) / 65536.0)  # 8 .. 16
+    code = (power - 1 + 127 - (per - span)) * 8 + q - 8
+    code = np.clip(code, 0, last)
+    code = np.where(a < least, (least * (np.asarray(bits16) / 65536.0) < a).astype(np.float64), code)
+    if which == "v":
+        code = np.where(a > 0, np.maximum(code, 1), 0)
+    else:
+        code = np.where(x < 0, code + 128, code)
+    return np.where(per == 255, 0, code).astype(np.uint8), e.astype(np.uint8)
+
+
 def pointwise_mlp2(x, w1, b1, w2, b2):
     """Projection to the output channels through one hidden layer: W2 sigma(W1 x + b1) + b2."""
     return channel_affine(gelu(channel_affine(x, w1, b1)), w2, b2)

@@ -18,6 +18,9 @@ LIB_PATH = os.path.join(_HERE, "libfno.so")
 
 FNO_OK, FNO_EINVAL, FNO_EUNSUPPORTED, FNO_ENOSPC, FNO_EHIP = 0, -1, -2, -3, -4
 FNO_ACT_IDENTITY, FNO_ACT_GELU = 0, 1
+FNO_ACT_SILU = 2                 # group norm only
+FNO_LAYOUT_CHANNELS_FIRST, FNO_LAYOUT_CHANNELS_LAST = 0, 1
+FNO_DTYPE_F32, FNO_DTYPE_BF16 = 0, 1
 FNO_OP_SPECTRAL_CONV_FWD, FNO_OP_SPECTRAL_CONV_BWD, FNO_OP_BLOCK_FWD, FNO_OP_BLOCK_BWD = 0, 1, 2, 3
 FNO_FLAG_MSE_TARGET = 1
 FNO_FLAG_ACCUMULATE_GRADS = 2
@@ -31,6 +34,8 @@ EXPORTS = [
     "fno_pointwise_bwd_workspace_bytes", "fno_pointwise_linear_bwd", "fno_pointwise_mlp2_bwd",
     "fno_time_lift_bwd_workspace_bytes", "fno_time_lift_bwd",
     "fno_spectral_conv_fwd_static",
+    "fno_group_norm_workspace_bytes", "fno_group_norm_fwd", "fno_group_norm_bwd",
+    "fno_adamw_step", "fno_grad_norm_workspace_bytes", "fno_grad_norm", "fno_adamw_state_read",
     "fno_status_string", "fno_timing_enable", "fno_timing_read",
 ]
 
@@ -42,6 +47,17 @@ class FnoDesc(ctypes.Structure):
                 ("grid", ctypes.c_int32 * 4), ("modes", ctypes.c_int32 * 4),
                 ("mode_rule", ctypes.c_int32), ("activation", ctypes.c_int32),
                 ("flags", ctypes.c_int32)]
+
+
+class FnoNormDesc(ctypes.Structure):
+    _fields_ = [("npoints", ctypes.c_int64), ("eps", ctypes.c_double), ("batch", ctypes.c_int32),
+                ("channels", ctypes.c_int32), ("groups", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class FnoAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("exps", ctypes.c_void_p), ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
 
 
 class FnoError(RuntimeError):
@@ -292,6 +308,132 @@ def fno_adam_step(n, param, grad, m, v, lr, beta1, beta2, eps, step) -> None:
     _check(lib().fno_adam_step(ctypes.c_int64(n), _ptr(param, name="param"), _ptr(grad, name="grad"),
                                _ptr(m, name="m"), _ptr(v, name="v"), ctypes.c_double(lr), ctypes.c_double(beta1),
                                ctypes.c_double(beta2), ctypes.c_double(eps), ctypes.c_int32(step), _stream()))
+
+
+def make_norm_desc(batch: int, channels: int, groups: int, npoints: int, layout: int = FNO_LAYOUT_CHANNELS_FIRST,
+                   dtype: int = FNO_DTYPE_F32, activation: int = FNO_ACT_GELU, eps: float = 1e-5,
+                   flags: int = 0) -> FnoNormDesc:
+    return FnoNormDesc(npoints, eps, batch, channels, groups, layout, dtype, activation, flags)
+
+
+def fno_group_norm_workspace_bytes(desc: FnoNormDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fno_group_norm_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_norm_workspace(desc: FnoNormDesc, device="cuda") -> torch.Tensor:
+    return torch.empty(max(fno_group_norm_workspace_bytes(desc), 256), dtype=torch.uint8, device=device)
+
+
+def _norm_ptrs(desc, fields, channels, stats):
+    """Pointers of (name, tensor) lists: fields of the descriptor's type and size, channel vectors, statistics."""
+    dtype = torch.bfloat16 if desc.dtype == FNO_DTYPE_BF16 else torch.float32
+    out = []
+    for group, numel, kind in ((fields, desc.batch * desc.channels * desc.npoints, dtype), (channels, desc.channels, torch.float32),
+                               (stats, desc.batch * desc.groups, torch.float32)):
+        for name, t in group:
+            if t is not None and t.is_complex():
+                raise ValueError(f"{name} has dtype {t.dtype}")
+            _expect(t, name, numel)
+            out.append(_ptr(t, kind, name))
+    return out
+
+
+def fno_group_norm_fwd(desc, x, gamma, beta, y, mean, rstd, ws) -> None:
+    px, py, pg, pb, pm, pr = _norm_ptrs(desc, (("x", x), ("y", y)), (("gamma", gamma), ("beta", beta)),
+                                        (("mean", mean), ("rstd", rstd)))
+    p, n = _ws(ws)
+    _check(lib().fno_group_norm_fwd(ctypes.byref(desc), px, pg, pb, py, pm, pr, p, n, _stream()))
+
+
+def fno_group_norm_bwd(desc, x, gamma, beta, mean, rstd, gy, gx, ggamma, gbeta, ws) -> None:
+    px, pgy, pgx, pg, pb, pgg, pgb, pm, pr = _norm_ptrs(
+        desc, (("x", x), ("gy", gy), ("gx", gx)),
+        (("gamma", gamma), ("beta", beta), ("ggamma", ggamma), ("gbeta", gbeta)), (("mean", mean), ("rstd", rstd)))
+    p, n = _ws(ws)
+    _check(lib().fno_group_norm_bwd(ctypes.byref(desc), px, pg, pb, pm, pr, pgy, pgx, pgg, pgb, p, n, _stream()))
+
+
+class AdamwTensors:
+    """The host array of tensors that fno_adamw_step, fno_grad_norm and fno_adamw_state_read take, and the tensors
+    themselves, which have to live as long as the array is used.  Built by make_adamw_tensors()."""
+
+    def __init__(self, array, count, sizes, bits, device, keep):
+        self.array, self.count, self.sizes, self.bits, self.device, self.keep = array, count, sizes, bits, device, keep
+
+
+def adamw_exps_shape(n: int) -> tuple:
+    """Shape of the uint8 tensor with the shared exponents of a tensor of n values (a complex one has 2 n)."""
+    return (-(-n // 256), 2)
+
+
+def make_adamw_tensors(params, grads, m, v, exps=None, weight_decay=0.0) -> AdamwTensors:
+    """Lists of tensors on one GPU: parameters and gradients in float32 (or complex64, as pairs of floats), moments in
+    float32, or in uint8 with exps (uint8, adamw_exps_shape()).  weight_decay: one number, or one a tensor."""
+    count = len(params)
+    decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+    if not (len(grads) == len(m) == len(v) == len(decay) == count) or (exps is not None and len(exps) != count):
+        raise ValueError("params, grads, m, v, exps and weight_decay must have one entry a tensor")
+    state = torch.float32 if exps is None else torch.uint8
+    array, sizes = (FnoAdamwTensor * max(count, 1))(), []
+    devices = set()
+    for k in range(count):
+        n = params[k].numel() * (2 if params[k].is_complex() else 1)
+        _expect(grads[k], f"grads[{k}]", n)
+        _expect(m[k], f"m[{k}]", n)
+        _expect(v[k], f"v[{k}]", n)
+        e = None if exps is None else exps[k]
+        if e is not None and e.numel() != 2 * -(-n // 256):
+            raise ValueError(f"exps[{k}] holds {e.numel()} bytes, its tensor implies {2 * -(-n // 256)}")
+        array[k] = FnoAdamwTensor(_ptr(params[k], name=f"params[{k}]"), _ptr(grads[k], name=f"grads[{k}]"),
+                                  _ptr(m[k], state, f"m[{k}]"), _ptr(v[k], state, f"v[{k}]"),
+                                  _ptr(e, torch.uint8, f"exps[{k}]"), n, decay[k])
+        sizes.append(n)
+        devices |= {t.device for t in (params[k], grads[k], m[k], v[k]) + (() if e is None else (e,))}
+    if len(devices) > 1:
+        raise ValueError("all tensors of a list must live on one GPU")
+    return AdamwTensors(array, count, sizes, 32 if exps is None else 8, devices.pop() if devices else None,
+                        (list(params), list(grads), list(m), list(v), None if exps is None else list(exps)))
+
+
+def fno_adamw_step(tensors: AdamwTensors, lr, beta1, beta2, eps, step, grad_norm=None, max_norm=1.0, seed=0) -> None:
+    _expect(grad_norm, "grad_norm", 1)
+    _check(lib().fno_adamw_step(ctypes.c_int32(tensors.count), tensors.array, ctypes.c_int32(tensors.bits),
+                                ctypes.c_double(lr), ctypes.c_double(beta1), ctypes.c_double(beta2), ctypes.c_double(eps),
+                                ctypes.c_int32(step), _ptr(grad_norm, name="grad_norm"), ctypes.c_double(max_norm),
+                                ctypes.c_uint32(seed), _stream()))
+
+
+def fno_grad_norm_workspace_bytes(tensors: AdamwTensors) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fno_grad_norm_workspace_bytes(ctypes.c_int32(tensors.count), tensors.array, ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_grad_norm_workspace(tensors: AdamwTensors, device="cuda") -> torch.Tensor:
+    return torch.empty(max(fno_grad_norm_workspace_bytes(tensors), 256), dtype=torch.uint8, device=device)
+
+
+def fno_grad_norm(tensors: AdamwTensors, norm, ws) -> None:
+    _expect(norm, "norm", 1)
+    p, n = _ws(ws)
+    _check(lib().fno_grad_norm(ctypes.c_int32(tensors.count), tensors.array, _ptr(norm, name="norm"), p, n, _stream()))
+
+
+def fno_adamw_state_read(tensors: AdamwTensors, m_out, v_out) -> None:
+    """bf16 tensors m_out[k], v_out[k] receive what the 8-bit moments of tensor k stand for."""
+    if tensors.bits != 8:
+        raise ValueError("the moments of this list are in 32 bits")
+    if len(m_out) != tensors.count or len(v_out) != tensors.count:
+        raise ValueError("m_out and v_out must have one entry a tensor")
+    pm, pv = ((ctypes.c_void_p * max(tensors.count, 1))() for _ in range(2))
+    for k, n in enumerate(tensors.sizes):
+        _expect(m_out[k], f"m_out[{k}]", n)
+        _expect(v_out[k], f"v_out[{k}]", n)
+        pm[k] = _ptr(m_out[k], torch.bfloat16, f"m_out[{k}]").value
+        pv[k] = _ptr(v_out[k], torch.bfloat16, f"v_out[{k}]").value
+    _check(lib().fno_adamw_state_read(ctypes.c_int32(tensors.count), tensors.array, pm, pv, _stream()))
 
 
 def fno_pointwise_mlp2(batch, c_in, hidden, c_out, npoints, x, W1, b1, W2, b2, y) -> None:

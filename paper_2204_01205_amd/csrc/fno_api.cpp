@@ -3,9 +3,11 @@
 #include "../../include/fno.h"
 #include "fno_kernels.h"
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <new>
 #include <vector>
 
 namespace {
@@ -342,6 +344,58 @@ int conv_bwd_common(const Plan& p, const float* x, const float* xhat_saved, cons
   return FNO_OK;
 }
 
+// Validates a group norm's descriptor.
+int norm_shape(const fno_norm_desc* d, fno::NormShape* n) {
+  if (d == nullptr) { set_detail("descriptor is null"); return FNO_EINVAL; }
+  if (d->batch < 1 || d->channels < 1 || d->groups < 1 || d->npoints < 0) { set_detail("batch, channels and groups must be >= 1, npoints >= 0"); return FNO_EINVAL; }
+  if (d->channels % d->groups != 0) { set_detail("groups must divide channels"); return FNO_EINVAL; }
+  if (d->layout != FNO_LAYOUT_CHANNELS_FIRST && d->layout != FNO_LAYOUT_CHANNELS_LAST) { set_detail("unknown layout"); return FNO_EINVAL; }
+  if (d->dtype != FNO_DTYPE_F32 && d->dtype != FNO_DTYPE_BF16) { set_detail("unknown dtype"); return FNO_EINVAL; }
+  if (d->activation != FNO_ACT_IDENTITY && d->activation != FNO_ACT_GELU && d->activation != FNO_ACT_SILU) { set_detail("unknown activation"); return FNO_EINVAL; }
+  if (d->flags & ~FNO_FLAG_ACCUMULATE_GRADS) { set_detail("unknown flag bits"); return FNO_EINVAL; }
+  if (!(d->eps >= 0.0) || !std::isfinite(d->eps)) { set_detail("eps must be finite and at least 0"); return FNO_EINVAL; }
+  if (d->channels > fno::kMaxNormChannels || d->batch > 65535 || d->npoints > ((int64_t)1 << 40)) {
+    set_detail("group_norm covers channels <= %d, batch <= 65535, npoints <= 2^40", fno::kMaxNormChannels);
+    return FNO_EUNSUPPORTED;
+  }
+  *n = fno::NormShape{d->batch, d->channels, d->groups, d->npoints, d->layout == FNO_LAYOUT_CHANNELS_LAST,
+                      d->dtype == FNO_DTYPE_BF16, d->activation, d->eps};
+  return FNO_OK;
+}
+
+int check_norm_ws(const fno::NormShape& n, void* ws, size_t ws_bytes) {
+  if (ws == nullptr) { set_detail("workspace is null"); return FNO_EINVAL; }
+  if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) { set_detail("workspace must be 256-byte aligned"); return FNO_ENOSPC; }
+  const size_t need = fno::group_norm_workspace_bytes(n);
+  if (ws_bytes < need) { set_detail("workspace too small: need %lld bytes", (long long)need); return FNO_ENOSPC; }
+  return FNO_OK;
+}
+
+// Validates a list of tensors; `need`: which of their pointers the call uses.
+enum { kAdamwParam = 1, kAdamwGrad = 2, kAdamwState = 4, kAdamwCodes = 8 };
+int adamw_list(int32_t count, const fno_adamw_tensor* t, int need, std::vector<fno::AdamwTensor>* out) {
+  if (count < 0 || (count > 0 && t == nullptr)) { set_detail("count must be non-negative, tensors not null"); return FNO_EINVAL; }
+  out->resize((size_t)count);
+  for (int k = 0; k < count; ++k) {
+    if (t[k].n < 0 || t[k].n > ((int64_t)1 << 40)) { set_detail("n of tensor %d must lie in 0 .. 2^40", k); return FNO_EINVAL; }
+    if (!std::isfinite(t[k].weight_decay)) { set_detail("weight_decay of tensor %d must be finite", k); return FNO_EINVAL; }
+    if (t[k].n > 0) {
+      uintptr_t bits = 0;
+      bool null = false;
+      auto use = [&](const void* p) { bits |= reinterpret_cast<uintptr_t>(p); null = null || p == nullptr; };
+      if (need & kAdamwParam) use(t[k].param);
+      if (need & kAdamwGrad) use(t[k].grad);
+      if (need & kAdamwState) { use(t[k].m); use(t[k].v); }
+      if ((need & kAdamwCodes) && t[k].exps == nullptr) null = true;
+      if (null) { set_detail("a pointer of tensor %d is null", k); return FNO_EINVAL; }
+      if (bits & 3) { set_detail("pointers of tensor %d must be 4-byte aligned", k); return FNO_EINVAL; }
+      if ((need & kAdamwCodes) && (reinterpret_cast<uintptr_t>(t[k].exps) & 1)) { set_detail("exps of tensor %d must be 2-byte aligned", k); return FNO_EINVAL; }
+    }
+    (*out)[k] = fno::AdamwTensor{t[k].param, t[k].grad, t[k].m, t[k].v, t[k].exps, t[k].n, t[k].weight_decay};
+  }
+  return FNO_OK;
+}
+
 }  // namespace
 
 namespace fno {
@@ -576,6 +630,108 @@ int fno_adam_step(int64_t n, float* param, const float* grad, float* m, float* v
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) { set_detail("beta1 and beta2 must lie in [0, 1)"); return FNO_EINVAL; }
   FNO_HIP(fno::launch_adam(n, param, grad, m, v, lr, beta1, beta2, eps, step, static_cast<hipStream_t>(stream)));
   return FNO_OK;
+}
+
+int fno_group_norm_workspace_bytes(const fno_norm_desc* desc, size_t* bytes) {
+  fno::NormShape n;
+  const int rc = norm_shape(desc, &n);
+  if (rc != FNO_OK) return rc;
+  if (bytes == nullptr) { set_detail("bytes is required"); return FNO_EINVAL; }
+  *bytes = fno::group_norm_workspace_bytes(n);
+  return FNO_OK;
+}
+
+int fno_group_norm_fwd(const fno_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
+                       float* mean, float* rstd, void* ws, size_t ws_bytes, void* stream) {
+  fno::NormShape n;
+  int rc = norm_shape(desc, &n);
+  if (rc != FNO_OK) return rc;
+  if (x == nullptr || y == nullptr) { set_detail("x and y are required"); return FNO_EINVAL; }
+  if (misaligned16(x, y)) return FNO_EINVAL;
+  rc = check_norm_ws(n, ws, ws_bytes);
+  if (rc != FNO_OK) return rc;
+  FNO_HIP(fno::launch_group_norm_fwd(n, x, gamma, beta, y, mean, rstd, ws, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+}
+
+int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* gamma, const float* beta,
+                       const float* mean, const float* rstd, const void* gy, void* gx, float* ggamma, float* gbeta,
+                       void* ws, size_t ws_bytes, void* stream) {
+  fno::NormShape n;
+  int rc = norm_shape(desc, &n);
+  if (rc != FNO_OK) return rc;
+  if (x == nullptr || mean == nullptr || rstd == nullptr || gy == nullptr) { set_detail("x, mean, rstd and gy are required"); return FNO_EINVAL; }
+  if (misaligned16(x, gy, gx)) return FNO_EINVAL;
+  rc = check_norm_ws(n, ws, ws_bytes);
+  if (rc != FNO_OK) return rc;
+  if (gx == nullptr && ggamma == nullptr && gbeta == nullptr) return FNO_OK;
+  FNO_HIP(fno::launch_group_norm_bwd(n, x, gamma, beta, mean, rstd, gy, gx, ggamma, gbeta,
+                                     (desc->flags & FNO_FLAG_ACCUMULATE_GRADS) ? 1 : 0, ws,
+                                     static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+}
+
+int fno_adamw_step(int32_t count, const fno_adamw_tensor* tensors, int32_t state_bits, double lr, double beta1,
+                   double beta2, double eps, int32_t step, const float* grad_norm, double max_norm, uint32_t seed,
+                   void* stream) try {
+  if (state_bits != 8 && state_bits != 32) { set_detail("state_bits must be 8 or 32"); return FNO_EINVAL; }
+  if (step < 1) { set_detail("step counts from 1"); return FNO_EINVAL; }
+  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) { set_detail("beta1 and beta2 must lie in [0, 1)"); return FNO_EINVAL; }
+  if (!std::isfinite(lr) || !(eps >= 0.0)) { set_detail("lr must be finite and eps at least 0"); return FNO_EINVAL; }
+  if (grad_norm != nullptr && !(max_norm > 0.0)) { set_detail("max_norm must be positive"); return FNO_EINVAL; }
+  std::vector<fno::AdamwTensor> list;
+  const int rc = adamw_list(count, tensors, kAdamwParam | kAdamwGrad | kAdamwState | (state_bits == 8 ? kAdamwCodes : 0), &list);
+  if (rc != FNO_OK) return rc;
+  const fno::AdamwStep st{state_bits, lr, beta1, beta2, eps, step, grad_norm, max_norm, seed};
+  FNO_HIP(fno::launch_adamw(list.data(), (int)list.size(), st, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+} catch (const std::bad_alloc&) {
+  set_detail("out of host memory");
+  return FNO_EHIP;
+}
+
+int fno_grad_norm_workspace_bytes(int32_t count, const fno_adamw_tensor* tensors, size_t* bytes) try {
+  if (bytes == nullptr) { set_detail("bytes is required"); return FNO_EINVAL; }
+  std::vector<fno::AdamwTensor> list;
+  const int rc = adamw_list(count, tensors, 0, &list);
+  if (rc != FNO_OK) return rc;
+  *bytes = fno::grad_norm_workspace_bytes(list.data(), (int)list.size());
+  return FNO_OK;
+} catch (const std::bad_alloc&) {
+  set_detail("out of host memory");
+  return FNO_EHIP;
+}
+
+int fno_grad_norm(int32_t count, const fno_adamw_tensor* tensors, float* norm, void* ws, size_t ws_bytes, void* stream) try {
+  std::vector<fno::AdamwTensor> list;
+  const int rc = adamw_list(count, tensors, kAdamwGrad, &list);
+  if (rc != FNO_OK) return rc;
+  if (norm == nullptr || ws == nullptr) { set_detail("norm and ws are required"); return FNO_EINVAL; }
+  if (reinterpret_cast<uintptr_t>(ws) % 8 != 0 || reinterpret_cast<uintptr_t>(norm) % 4 != 0) { set_detail("ws must be 8-byte aligned, norm 4-byte"); return FNO_EINVAL; }
+  if (ws_bytes < fno::grad_norm_workspace_bytes(list.data(), (int)list.size())) { set_detail("workspace too small"); return FNO_ENOSPC; }
+  FNO_HIP(fno::launch_grad_norm(list.data(), (int)list.size(), norm, ws, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+} catch (const std::bad_alloc&) {
+  set_detail("out of host memory");
+  return FNO_EHIP;
+}
+
+int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* const* m_out, void* const* v_out,
+                         void* stream) try {
+  std::vector<fno::AdamwTensor> list;
+  const int rc = adamw_list(count, tensors, kAdamwState | kAdamwCodes, &list);
+  if (rc != FNO_OK) return rc;
+  if (count > 0 && (m_out == nullptr || v_out == nullptr)) { set_detail("m_out and v_out are required"); return FNO_EINVAL; }
+  for (int k = 0; k < count; ++k) {
+    if (list[k].n == 0) continue;
+    if (m_out[k] == nullptr || v_out[k] == nullptr) { set_detail("m_out and v_out of tensor %d are required", k); return FNO_EINVAL; }
+    if ((reinterpret_cast<uintptr_t>(m_out[k]) | reinterpret_cast<uintptr_t>(v_out[k])) & 3) { set_detail("outputs of tensor %d must be 4-byte aligned", k); return FNO_EINVAL; }
+  }
+  FNO_HIP(fno::launch_adamw_state_read(list.data(), (int)list.size(), m_out, v_out, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+} catch (const std::bad_alloc&) {
+  set_detail("out of host memory");
+  return FNO_EHIP;
 }
 
 int fno_timing_enable(int stage_mask) {

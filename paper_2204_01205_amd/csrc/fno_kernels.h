@@ -130,6 +130,44 @@ hipError_t launch_rel_l2(int64_t n, const float* pred, const float* target, floa
 hipError_t launch_adam(int64_t n, float* p, const float* g, float* m, float* v, double lr, double beta1,
                        double beta2, double eps, int step, hipStream_t s);
 
+// Group norm with an activation (fno_group_norm.hip).  x, y, gy, gx: float, or bf16 where bf16 is set; [B][C][P], or
+// [B][P][C] where last is set.  Outputs nullable.  ws: group_norm_workspace_bytes() of scratch.
+struct NormShape {
+  int B, C, G;
+  int64_t P;
+  bool last, bf16;
+  int act;             // 0 identity, 1 GELU, 2 SiLU
+  double eps;
+};
+constexpr int kMaxNormChannels = 1024;
+size_t group_norm_workspace_bytes(const NormShape& n);
+hipError_t launch_group_norm_fwd(const NormShape& n, const void* x, const float* gamma, const float* beta, void* y,
+                                 float* mean, float* rstd, void* ws, hipStream_t s);
+hipError_t launch_group_norm_bwd(const NormShape& n, const void* x, const float* gamma, const float* beta,
+                                 const float* mean, const float* rstd, const void* gy, void* gx, float* ggamma,
+                                 float* gbeta, int accumulate, void* ws, hipStream_t s);
+
+// AdamW over the tensors of a list, the norm of their gradients, and what 8-bit moments stand for (fno_adamw.hip).
+struct AdamwTensor {
+  float* p;
+  const float* g;
+  void *m, *v, *e;
+  int64_t n;
+  double decay;
+};
+struct AdamwStep {
+  int bits;
+  double lr, beta1, beta2, eps;
+  int step;
+  const float* norm;   // device scalar, nullable
+  double max_norm;
+  uint32_t seed;
+};
+hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwStep& st, hipStream_t s);
+size_t grad_norm_workspace_bytes(const AdamwTensor* t, int count);
+hipError_t launch_grad_norm(const AdamwTensor* t, int count, float* norm, void* ws, hipStream_t s);
+hipError_t launch_adamw_state_read(const AdamwTensor* t, int count, void* const* m_out, void* const* v_out, hipStream_t s);
+
 // Adjoints of the channel lift and of the two-layer projection.  ws: pointwise_bwd_workspace_bytes()
 // of scratch, 8-byte aligned.  Outputs nullable.
 size_t pointwise_bwd_workspace_bytes(int Ci, int H, int Co);

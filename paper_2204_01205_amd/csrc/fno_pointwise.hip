@@ -18,50 +18,6 @@ namespace {
 // over points and runs on the matrix cores: v_mfma_f32_4x4x1 block blk adds the outer product
 // gz[4To..4To+3][p] x[4Ti..4Ti+3][p] of its point p to its own 4x4 partial tile; the 16 blocks,
 // the waves and the thread blocks are summed at the end (per-wave partials in double, fixed order).
-// GELU and its slope: with a = |z| and t = 1 / (1 + 0.4 a) the upper tail is exp(-a^2 / 2) t P(t), the form of Abramowitz &
-// Stegun 7.1.26, whose exponential is the density up to a constant.  P has degree 5 (7.1.26: 4) and is fitted over [0, 13]
-// to 3.5e-8 of max(a, 1) T(a) and to 1.7e-3 of the tail T itself, whichever is less, so that units that are all but off
-// keep their slope.  Against float64, of the norm, with 7.1.26 in brackets: under N(0, 1) 4.8e-8 on z Phi(z) and 6.9e-8 on
-// the slope (8.8e-8, 1.1e-7), at z = -5 7e-6 and 5e-7 (1.1e-3, 5e-5), at -9 5e-4 and 7e-6 (1.2e-2, 1.7e-4).  A polynomial
-// for the tail's logarithm, fitted in absolute error, was off by 7e-3 and 3e-4 at -5, by more than the value at -9, and
-// grew with |z| beyond 1e20.
-__device__ __forceinline__ void gelu_and_grad_f(float z, float& val, float& grad) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.4f, 1.0f));
-  float q = fmaf(t, 5.5231631e-02f, -2.5018391e-01f);
-  q = fmaf(t, q, 3.3274594e-01f);
-  q = fmaf(t, q, 1.8495135e-02f);
-  q = fmaf(t, q, 1.8670905e-01f);
-  q = fmaf(t, q, 1.5700214e-01f);
-  q *= t;
-  const float e = __builtin_amdgcn_exp2f((z * z) * -0.72134752044f);    // exp(-z^2 / 2)
-  const float tail = q * e;
-  const float cdf = z < 0.f ? tail : 1.0f - tail;
-  val = z * cdf;
-  grad = fmaf(z, 0.39894228040143267794f * e, cdf);
-}
-
-// The same closer to float64 around zero: log2 of twice the tail is a q(a), q of degree 9 (largest
-// error of max(a, 1) T(a) 1.9e-10; a q(a) falls from 0 to minus infinity), so that its rounding shrinks with a.  20
-// instructions, where erff and expf took over 100 (both branches of erff run in a wave); against float64, of the norm under
-// N(0, 1): the slope 3.9e-8, value times slope 6.6e-8 (erff and expf 4.0e-8 and 7.2e-8); at z = -5 the slope 2e-6 (5e-4).
-__device__ __forceinline__ void gelu_and_grad_fine_f(float z, float& val, float& grad) {
-  const float a = fabsf(z);
-  float q = fmaf(a, -5.62642732e-08f, 1.38986923e-06f);
-  q = fmaf(a, q, -1.52123248e-05f);
-  q = fmaf(a, q, 9.45571737e-05f);
-  q = fmaf(a, q, -3.24071734e-04f);
-  q = fmaf(a, q, 6.31522853e-05f);
-  q = fmaf(a, q, 6.89695915e-03f);
-  q = fmaf(a, q, -5.24215102e-02f);
-  q = fmaf(a, q, -4.59223896e-01f);
-  q = fmaf(a, q, -1.15110409e+00f);
-  const float t = __builtin_amdgcn_exp2f(a * q);
-  const float pdf = __builtin_amdgcn_exp2f(fmaf(z * z, -0.72134752044f, -1.3257480647f));     // log2 of 1 / sqrt(2 pi)
-  const float cdf = z < 0.f ? 0.5f * t : fmaf(-0.5f, t, 1.0f);
-  val = z * cdf;
-  grad = fmaf(z, pdf, cdf);
-}
-
 template <int CT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void bwd_pointwise_mfma_kernel(
     const float* __restrict__ z, const float* __restrict__ gout, const float* __restrict__ x,
