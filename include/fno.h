@@ -239,7 +239,7 @@ enum { FNO_DTYPE_F32 = 0, FNO_DTYPE_BF16 = 1 };
 typedef struct {
   int64_t npoints;     /* P >= 0                                                      */
   double eps;          /* >= 0, finite                                                */
-  int32_t batch;       /* B >= 1                                                      */
+  int32_t batch;       /* B, 1 .. 65535, B C <= 2^23                                  */
   int32_t channels;    /* C, 1 .. 1024                                                */
   int32_t groups;      /* divides C                                                   */
   int32_t layout;      /* FNO_LAYOUT_*                                                */
