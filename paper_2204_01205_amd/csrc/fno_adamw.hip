@@ -8,11 +8,11 @@ namespace {
 
 typedef unsigned char u8;
 typedef unsigned short u16;
-typedef u8 v4u8 __attribute__((ext_vector_type(4)));
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kGroup = 256;            // values that share an exponent
 constexpr int kPerLaunch = 64;         // tensors whose addresses go with one launch's arguments (3.5 KB)
-constexpr long long kPiece = 4096;     // values that a block takes: of one tensor
+constexpr int kBlockValues = 4096;     // values that a block takes at a time: 16 a thread
 
 struct AdamwEntry {
   float* p;
@@ -26,6 +26,7 @@ struct AdamwEntry {
 struct AdamwList {
   AdamwEntry t[kPerLaunch];
   int count, base;     // tensors of this launch; place of the first one in the caller's list
+  long long piece;     // values of one tensor that a block takes: a multiple of kBlockValues
 };
 struct AdamwScalars {
   float beta1, omb1, beta2, omb2, eps, lr1, ic2, max_norm;   // lr1 = lr / (1 - beta1^t), ic2 = 1 / (1 - beta2^t)
@@ -43,6 +44,18 @@ __device__ __forceinline__ int tensor_of(const AdamwList& l, unsigned piece) {
   }
   return lo;
 }
+
+// Four floats, four codes or 8 bytes at an address that is 4-byte aligned; every value is touched once a step.
+__device__ __forceinline__ v4f load4(const float* p) {
+  typedef v4f loose __attribute__((aligned(4)));
+  return __builtin_nontemporal_load(reinterpret_cast<const loose*>(p));
+}
+__device__ __forceinline__ void store4(float* p, v4f v) {
+  typedef v4f loose __attribute__((aligned(4)));
+  __builtin_nontemporal_store(v, reinterpret_cast<loose*>(p));
+}
+__device__ __forceinline__ unsigned load_codes(const u8* p) { return __builtin_nontemporal_load(reinterpret_cast<const unsigned*>(p)); }
+__device__ __forceinline__ void store_codes(u8* p, unsigned v) { __builtin_nontemporal_store(v, reinterpret_cast<unsigned*>(p)); }
 
 __host__ __device__ __forceinline__ unsigned mix_bits(unsigned x) {
   x ^= x >> 16;
@@ -76,19 +89,48 @@ __device__ __forceinline__ float updated(const AdamwScalars& c, float keep, floa
   return p * keep - c.lr1 * m / (sqrtf(v * c.ic2) + c.eps);
 }
 
+// A thread takes 16 values at a time, four from each of four quarters of the block's, all asked for before the first is used.
 __global__ __launch_bounds__(kThreads) void adamw32_kernel(AdamwList l, AdamwScalars c) {
   const AdamwEntry& t = l.t[tensor_of(l, blockIdx.x)];
   float scale;
   if (!clip_scale(c, scale)) return;
-  const long long at = (long long)(blockIdx.x - t.first) * kPiece;
-  const long long end = at + kPiece < t.n ? at + kPiece : t.n;
-  float *m = static_cast<float*>(t.m), *v = static_cast<float*>(t.v);
+  const long long begin = (long long)(blockIdx.x - t.first) * l.piece;
+  const long long end = begin + l.piece < t.n ? begin + l.piece : t.n;
+  float *const m = static_cast<float*>(t.m), *const v = static_cast<float*>(t.v), *const p = t.p;
+  const float* const g = t.g;
+  long long at = begin;
+  for (; at + kBlockValues <= end; at += kBlockValues) {
+    v4f gq[4], mq[4], vq[4], pq[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long i = at + u * (kBlockValues / 4) + 4 * threadIdx.x;
+      gq[u] = load4(g + i);
+      mq[u] = load4(m + i);
+      vq[u] = load4(v + i);
+      pq[u] = load4(p + i);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long i = at + u * (kBlockValues / 4) + 4 * threadIdx.x;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float mi = mq[u][w], vi = vq[u][w];
+        moments(c, gq[u][w] * scale, mi, vi);
+        mq[u][w] = mi;
+        vq[u][w] = vi;
+        pq[u][w] = updated(c, t.keep, pq[u][w], mi, vi);
+      }
+      store4(m + i, mq[u]);
+      store4(v + i, vq[u]);
+      store4(p + i, pq[u]);
+    }
+  }
   for (long long i = at + threadIdx.x; i < end; i += kThreads) {
     float mi = m[i], vi = v[i];
-    moments(c, t.g[i] * scale, mi, vi);
+    moments(c, g[i] * scale, mi, vi);
     m[i] = mi;
     v[i] = vi;
-    t.p[i] = updated(c, t.keep, t.p[i], mi, vi);
+    p[i] = updated(c, t.keep, p[i], mi, vi);
   }
 }
 
@@ -125,66 +167,155 @@ __device__ __forceinline__ float decode_v(unsigned code, unsigned e) {
   const unsigned bits = e == 255u ? 0x7FC00000u : code == 0u ? 0u : (code << 20) + ((e - kSpanV) << 23);
   return __builtin_bit_cast(float, bits);
 }
+// the largest of a wave's values, in every lane
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp_max(unsigned v) {
+  return max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROWS, 0xF, false));
+}
 __device__ __forceinline__ unsigned wave_max(unsigned v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, off));
-  return v;
+  v = dpp_max<0xB1, 0xF>(v);           // lane ^ 1
+  v = dpp_max<0x4E, 0xF>(v);           // lane ^ 2
+  v = dpp_max<0x141, 0xF>(v);          // mirrored in eights
+  v = dpp_max<0x140, 0xF>(v);          // mirrored in rows of 16
+  v = dpp_max<0x142, 0xA>(v);          // last lane of a row to the next row
+  v = dpp_max<0x143, 0xC>(v);          // lane 31 to the upper half
+  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// A wave takes one block of 256 values at a time, four to a lane.
+// One block of 256 values in a wave, four to a lane: what stays in registers between its loads and its stores.
+struct Group8 {
+  v4f p, g;
+  unsigned m, v, e;    // codes; exponents, m's in the low byte
+};
+__device__ __forceinline__ void group_step(const AdamwScalars& c, float keep, float scale, unsigned block, int lane, Group8& q) {
+  const unsigned em = q.e & 255u, ev = q.e >> 8;
+  float mi[4], vi[4];
+  unsigned top_m = 0, top_v = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    mi[u] = decode_m((q.m >> (8 * u)) & 255u, em);
+    vi[u] = decode_v((q.v >> (8 * u)) & 255u, ev);
+    moments(c, q.g[u] * scale, mi[u], vi[u]);
+    q.p[u] = updated(c, keep, q.p[u], mi[u], vi[u]);
+    top_m = max(top_m, __builtin_bit_cast(unsigned, mi[u]) & 0x7FFFFFFFu);
+    top_v = max(top_v, __builtin_bit_cast(unsigned, vi[u]));
+  }
+  const unsigned nm = shared_exponent(wave_max(top_m), kSpanM), nv = shared_exponent(wave_max(top_v), kSpanV);
+  q.m = 0;
+  q.v = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const unsigned r = mix_bits(block + (unsigned)(4 * lane + u) * 0x9E3779B1u);
+    q.m |= encode_m(mi[u], nm, r & 0xFFFFu) << (8 * u);
+    q.v |= encode_v(vi[u], nv, r >> 16) << (8 * u);
+  }
+  if (nm == 255u) q.m = 0;             // (uniform)
+  if (nv == 255u) q.v = 0;
+  q.e = nm | nv << 8;
+}
+
+// A wave takes four blocks of 256 values at a time, all asked for before the first is used.
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScalars c) {
   const int k = tensor_of(l, blockIdx.x);
   const AdamwEntry& t = l.t[k];
   float scale;
   if (!clip_scale(c, scale)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned key = mix_bits(c.key ^ (unsigned)(l.base + k));
-  const long long first = (long long)(blockIdx.x - t.first) * (kPiece / kGroup), blocks = (t.n + kGroup - 1) / kGroup;
-  u8 *m = static_cast<u8*>(t.m), *v = static_cast<u8*>(t.v);
-  for (long long q = first + wave; q < first + kPiece / kGroup && q < blocks; q += kThreads / 64) {
-    const unsigned em = t.e[2 * q], ev = t.e[2 * q + 1];
-    const unsigned block = mix_bits(mix_bits((unsigned)q + key) + (unsigned)(q >> 32));
-    float mi[4], vi[4];
-    unsigned top_m = 0, top_v = 0;
+  const long long begin = (long long)(blockIdx.x - t.first) * l.piece;
+  const long long end = begin + l.piece < t.n ? begin + l.piece : t.n;
+  u8 *const m = static_cast<u8*>(t.m), *const v = static_cast<u8*>(t.v);
+  u16* const e = reinterpret_cast<u16*>(t.e);
+  auto random_of = [&](long long block) { return mix_bits(mix_bits((unsigned)block + key) + (unsigned)(block >> 32)); };
+  long long at = begin + wave * (kBlockValues / 4);
+  for (; at + 4 * kGroup <= end; at += kBlockValues) {
+    Group8 q[4];
+    const long long b0 = at / kGroup;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const long long i = q * kGroup + 4 * lane + u;
-      mi[u] = 0.f;
-      vi[u] = 0.f;
-      if (i < t.n) {
-        mi[u] = decode_m(m[i], em);
-        vi[u] = decode_v(v[i], ev);
-        moments(c, t.g[i] * scale, mi[u], vi[u]);
-        t.p[i] = updated(c, t.keep, t.p[i], mi[u], vi[u]);
-      }
-      top_m = max(top_m, __builtin_bit_cast(unsigned, mi[u]) & 0x7FFFFFFFu);
-      top_v = max(top_v, __builtin_bit_cast(unsigned, vi[u]) & 0x7FFFFFFFu);
+      const long long i = at + u * kGroup + 4 * lane;
+      q[u].p = load4(t.p + i);
+      q[u].g = load4(t.g + i);
+      q[u].m = load_codes(m + i);
+      q[u].v = load_codes(v + i);
+      q[u].e = e[b0 + u];
     }
-    const unsigned nm = shared_exponent(wave_max(top_m), kSpanM), nv = shared_exponent(wave_max(top_v), kSpanV);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const long long i = q * kGroup + 4 * lane + u;
-      const unsigned r = mix_bits(block + (unsigned)(4 * lane + u) * 0x9E3779B1u);
-      if (i < t.n) {
-        m[i] = nm == 255u ? 0 : (u8)encode_m(mi[u], nm, r & 0xFFFFu);
-        v[i] = nv == 255u ? 0 : (u8)encode_v(vi[u], nv, r >> 16);
-      }
+      const long long i = at + u * kGroup + 4 * lane;
+      group_step(c, t.keep, scale, random_of(b0 + u), lane, q[u]);
+      store4(t.p + i, q[u].p);
+      store_codes(m + i, q[u].m);
+      store_codes(v + i, q[u].v);
+      if (lane == 0) e[b0 + u] = (u16)q[u].e;
     }
-    if (lane == 0) { t.e[2 * q] = (u8)nm; t.e[2 * q + 1] = (u8)nv; }
+  }
+  // the tensor's last blocks, the very last one cut: values past the end are zeros that nobody stores
+  const long long stop = at + kBlockValues / 4 < end ? at + kBlockValues / 4 : end;
+  for (; at < stop; at += kGroup) {
+    Group8 q{};
+    const long long i = at + 4 * lane;
+    q.e = e[at / kGroup];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i + u >= end) continue;
+      q.p[u] = t.p[i + u];
+      q.g[u] = t.g[i + u];
+      q.m |= (unsigned)m[i + u] << (8 * u);
+      q.v |= (unsigned)v[i + u] << (8 * u);
+    }
+    group_step(c, t.keep, scale, random_of(at / kGroup), lane, q);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i + u >= end) continue;
+      t.p[i + u] = q.p[u];
+      m[i + u] = (u8)(q.m >> (8 * u));
+      v[i + u] = (u8)(q.v >> (8 * u));
+    }
+    if (lane == 0) e[at / kGroup] = (u16)q.e;
   }
 }
 
 // p and g of an entry hold the outputs here
 __global__ __launch_bounds__(kThreads) void adamw_read_kernel(AdamwList l) {
   const AdamwEntry& t = l.t[tensor_of(l, blockIdx.x)];
-  const long long at = (long long)(blockIdx.x - t.first) * kPiece;
-  const long long end = at + kPiece < t.n ? at + kPiece : t.n;
-  const u8 *m = static_cast<const u8*>(t.m), *v = static_cast<const u8*>(t.v);
-  u16 *mo = reinterpret_cast<u16*>(t.p), *vo = reinterpret_cast<u16*>(const_cast<float*>(t.g));
-  for (long long i = at + threadIdx.x; i < end; i += kThreads) {
-    const long long q = i / kGroup;
-    mo[i] = (u16)(__builtin_bit_cast(unsigned, decode_m(m[i], t.e[2 * q])) >> 16);
-    vo[i] = (u16)(__builtin_bit_cast(unsigned, decode_v(v[i], t.e[2 * q + 1])) >> 16);
+  const long long begin = (long long)(blockIdx.x - t.first) * l.piece;
+  const long long end = begin + l.piece < t.n ? begin + l.piece : t.n;
+  const u8 *const m = static_cast<const u8*>(t.m), *const v = static_cast<const u8*>(t.v);
+  const u16* const e = reinterpret_cast<const u16*>(t.e);
+  u16 *const mo = reinterpret_cast<u16*>(t.p), *const vo = reinterpret_cast<u16*>(const_cast<float*>(t.g));
+  typedef v2u loose __attribute__((aligned(4)));
+  auto put = [&](long long at, unsigned cm, unsigned cv, unsigned ex) {
+    unsigned a[4], b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      a[u] = __builtin_bit_cast(unsigned, decode_m((cm >> (8 * u)) & 255u, ex & 255u));
+      b[u] = __builtin_bit_cast(unsigned, decode_v((cv >> (8 * u)) & 255u, ex >> 8));
+    }
+    const v2u x = {a[0] >> 16 | (a[1] & 0xFFFF0000u), a[2] >> 16 | (a[3] & 0xFFFF0000u)};
+    const v2u y = {b[0] >> 16 | (b[1] & 0xFFFF0000u), b[2] >> 16 | (b[3] & 0xFFFF0000u)};
+    __builtin_nontemporal_store(x, reinterpret_cast<loose*>(mo + at));
+    __builtin_nontemporal_store(y, reinterpret_cast<loose*>(vo + at));
+  };
+  long long at = begin + 4 * threadIdx.x;
+  constexpr int U = kBlockValues / (4 * kThreads);
+  for (; at + (U - 1) * 4 * kThreads + 4 <= end; at += kBlockValues) {
+    unsigned cm[U], cv[U], ex[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      cm[u] = load_codes(m + at + u * 4 * kThreads);
+      cv[u] = load_codes(v + at + u * 4 * kThreads);
+      ex[u] = e[(at + u * 4 * kThreads) / kGroup];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) put(at + u * 4 * kThreads, cm[u], cv[u], ex[u]);
+  }
+  for (; at + 4 <= end; at += 4 * kThreads) put(at, load_codes(m + at), load_codes(v + at), e[at / kGroup]);
+  for (int u = 0; u < 4; ++u) {
+    if (at + u >= end) break;
+    const unsigned ex = e[at / kGroup];
+    mo[at + u] = (u16)(__builtin_bit_cast(unsigned, decode_m(m[at + u], ex & 255u)) >> 16);
+    vo[at + u] = (u16)(__builtin_bit_cast(unsigned, decode_v(v[at + u], ex >> 8)) >> 16);
   }
 }
 
@@ -194,45 +325,65 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   double s = 0.0;
-  for (int w = 0; w < kThreads / 64; ++w) s += red[w];
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) s += red[w];
   return s;
 }
 
+// A square of a float is exact in double, and so squares of the largest and the smallest floats are neither infinite nor zero.
 __global__ __launch_bounds__(kThreads) void grad_norm_partial_kernel(AdamwList l, double* part) {
   __shared__ double red[kThreads / 64];
   const AdamwEntry& t = l.t[tensor_of(l, blockIdx.x)];
-  const long long at = (long long)(blockIdx.x - t.first) * kPiece;
-  const long long end = at + kPiece < t.n ? at + kPiece : t.n;
-  double s = 0.0;
-  for (long long i = at + threadIdx.x; i < end; i += kThreads) s += (double)t.g[i] * (double)t.g[i];
-  s = block_sum(s, red);
-  if (threadIdx.x == 0) part[blockIdx.x] = s;
+  const long long begin = (long long)(blockIdx.x - t.first) * l.piece;
+  const long long end = begin + l.piece < t.n ? begin + l.piece : t.n;
+  const float* const g = t.g;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  long long at = begin;
+  for (; at + kBlockValues <= end; at += kBlockValues) {
+    v4f q[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = load4(g + at + u * (kBlockValues / 4) + 4 * threadIdx.x);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) s[w] = fma((double)q[u][w], (double)q[u][w], s[w]);
+  }
+  for (long long i = at + threadIdx.x; i < end; i += kThreads) s[0] = fma((double)g[i], (double)g[i], s[0]);
+  const double sum = block_sum((s[0] + s[1]) + (s[2] + s[3]), red);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
-__global__ __launch_bounds__(kThreads) void grad_norm_final_kernel(const double* part, long long count, float* norm) {
-  __shared__ double red[kThreads / 64];
+__global__ __launch_bounds__(1024) void grad_norm_final_kernel(const double* part, long long count, float* norm) {
+  __shared__ double red[1024 / 64];
   double s = 0.0;
-  for (long long i = threadIdx.x; i < count; i += kThreads) s += part[i];
+  for (long long i = threadIdx.x; i < count; i += 1024) s += part[i];
   s = block_sum(s, red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-long long pieces_of(int64_t n) { return (n + kPiece - 1) / kPiece; }
+// Values that a block takes: so many that all tensors together make about `blocks` blocks, and at least kBlockValues.
+long long piece_of(const AdamwTensor* t, int count, long long blocks) {
+  long long n = 0;
+  for (int k = 0; k < count; ++k) n += t[k].n;
+  const long long rounds = (n + blocks * kBlockValues - 1) / (blocks * kBlockValues);
+  return (rounds < 1 ? 1 : rounds) * kBlockValues;
+}
+long long pieces_of(int64_t n, long long piece) { return (n + piece - 1) / piece; }
 
-// Calls launch(list, pieces) for at most kPerLaunch tensors and 2^30 pieces at a time; tensors without values are left out.
+// Calls launch(list, pieces) for at most kPerLaunch tensors and 2^23 pieces at a time.
 template <class F>
-hipError_t over_tensors(const AdamwTensor* t, int count, double lr, F&& launch) {
+hipError_t over_tensors(const AdamwTensor* t, int count, double lr, long long piece, F&& launch) {
   AdamwList l;
   hipError_t e = hipSuccess;
   for (int k = 0; k < count && e == hipSuccess;) {
     l.count = 0;
     l.base = k;
+    l.piece = piece;
     long long pieces = 0;
     for (; k < count && k - l.base < kPerLaunch; ++k) {
-      if (pieces + pieces_of(t[k].n) > (1ll << 30) && pieces > 0) break;
+      if (pieces + pieces_of(t[k].n, piece) > (1ll << 23) && pieces > 0) break;
       // an empty tensor keeps its place (the random bits go by it) and starts where the next one does
       l.t[l.count++] = AdamwEntry{t[k].p, t[k].g, t[k].m, t[k].v, static_cast<u8*>(t[k].e), (long long)t[k].n, (unsigned)pieces,
                                   (float)(1.0 - lr * t[k].decay)};
-      pieces += pieces_of(t[k].n);
+      pieces += pieces_of(t[k].n, piece);
     }
     if (pieces > 0) {
       launch(l, pieces);
@@ -242,6 +393,9 @@ hipError_t over_tensors(const AdamwTensor* t, int count, double lr, F&& launch) 
   return e;
 }
 
+constexpr long long kStepBlocks = 1ll << 20;   // blocks of a step: more only where tensors are longer than 2^32 values
+constexpr long long kNormBlocks = 4096;        // partial sums of the norm, and one more for every tensor
+
 }  // namespace
 
 hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwStep& st, hipStream_t s) {
@@ -249,27 +403,28 @@ hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwStep& st, hi
   const AdamwScalars c{(float)st.beta1, (float)(1.0 - st.beta1), (float)st.beta2, (float)(1.0 - st.beta2), (float)st.eps,
                        (float)(st.lr / c1), (float)(1.0 / c2), (float)st.max_norm,
                        mix_bits(mix_bits(st.seed) ^ (unsigned)st.step), st.norm};
-  return over_tensors(t, count, st.lr, [&](const AdamwList& l, long long pieces) {
+  return over_tensors(t, count, st.lr, piece_of(t, count, kStepBlocks), [&](const AdamwList& l, long long pieces) {
     if (st.bits == 8) hipLaunchKernelGGL(adamw8_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
     else hipLaunchKernelGGL(adamw32_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
   });
 }
 
 size_t grad_norm_workspace_bytes(const AdamwTensor* t, int count) {
+  const long long piece = piece_of(t, count, kNormBlocks);
   long long pieces = 0;
-  for (int k = 0; k < count; ++k) pieces += pieces_of(t[k].n);
+  for (int k = 0; k < count; ++k) pieces += pieces_of(t[k].n, piece);
   return (size_t)(pieces > 0 ? pieces : 1) * sizeof(double);
 }
 
 hipError_t launch_grad_norm(const AdamwTensor* t, int count, float* norm, void* ws, hipStream_t s) {
   double* part = static_cast<double*>(ws);
   long long done = 0;
-  const hipError_t e = over_tensors(t, count, 0.0, [&](const AdamwList& l, long long pieces) {
+  const hipError_t e = over_tensors(t, count, 0.0, piece_of(t, count, kNormBlocks), [&](const AdamwList& l, long long pieces) {
     hipLaunchKernelGGL(grad_norm_partial_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, part + done);
     done += pieces;
   });
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(grad_norm_final_kernel, dim3(1), dim3(kThreads), 0, s, part, done, norm);
+  hipLaunchKernelGGL(grad_norm_final_kernel, dim3(1), dim3(1024), 0, s, part, done, norm);
   return hipGetLastError();
 }
 
@@ -282,7 +437,7 @@ hipError_t launch_adamw_state_read(const AdamwTensor* t, int count, void* const*
       o[j].p = static_cast<float*>(m_out[k + j]);
       o[j].g = static_cast<const float*>(v_out[k + j]);
     }
-    const hipError_t e = over_tensors(o, here, 0.0, [&](const AdamwList& l, long long pieces) {
+    const hipError_t e = over_tensors(o, here, 0.0, piece_of(o, here, kStepBlocks), [&](const AdamwList& l, long long pieces) {
       hipLaunchKernelGGL(adamw_read_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l);
     });
     if (e != hipSuccess) return e;
