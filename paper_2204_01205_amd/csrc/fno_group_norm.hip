@@ -144,9 +144,9 @@ __device__ __forceinline__ void sweep(long long begin, long long end, int tid, i
 // piece of one row (one channel), or whole short rows wave by wave, where gamma and beta come in.
 // ------------------------------------------------------------------------------------------
 
-// part[(bg, piece)] = (sum d, sum d^2)
+// part[(bg, piece)] = (sum d, sum d^2); stat[bg].hi = k, for the launches that follow, which may write over x
 template <class T>
-__global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs a, const T* x, double2* part) {
+__global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs a, const T* x, double2* part, Stat* stat) {
   constexpr int V = kVec<T>, U = 4;
   __shared__ double red[2 * kThreads / 64];
   const long long bg = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces, n = a.P * a.D;
@@ -175,25 +175,31 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs a, const T*
               [&](long long at) { add(load_pack(x + at)); },
               [&](long long at) { add1(load1(x + at)); });
   block_sum2(s, q, red);
-  if (threadIdx.x == 0) part[blockIdx.x] = make_double2(s, q);
+  if (threadIdx.x != 0) return;
+  part[blockIdx.x] = make_double2(s, q);
+  if (j == 0) stat[bg].hi = first;
 }
 
-// Adds the pieces of every (b, g): part[bg][piece] -> stat[bg], mean, rstd.
-template <class T, bool LAST>
-__global__ __launch_bounds__(kThreads) void norm_stat_kernel(NormArgs a, const T* x, const double2* part, Stat* stat, float* mean,
-                                                             float* rstd) {
-  __shared__ double red[2 * kThreads / 64];
+// The statistics of group bg from its pieces' sums, in every thread of a block; red: as for block_sum2.
+__device__ __forceinline__ Stat block_stat(const NormArgs& a, int pieces, const Stat* stat, const double2* part, long long bg,
+                                           float* mean, float* rstd, double* red) {
   double s = 0.0, q = 0.0;
-  for (int j = threadIdx.x; j < a.pieces; j += kThreads) {
-    const double2 p = part[(long long)blockIdx.x * a.pieces + j];
+  for (int j = threadIdx.x; j < pieces; j += kThreads) {
+    const double2 p = part[bg * pieces + j];
     s += p.x;
     q += p.y;
   }
   block_sum2(s, q, red);
-  if (threadIdx.x != 0) return;
-  const long long b = blockIdx.x / a.G, c = (long long)(blockIdx.x % a.G) * a.D;
-  const double first = a.P > 0 ? load1(x + (LAST ? b * a.P * a.C + c : (b * a.C + c) * a.P)) : 0.f;
-  stat[blockIdx.x] = stat_of(first, s, q, a, mean, rstd, blockIdx.x);
+  return stat_of(stat[bg].hi, s, q, a, mean, rstd, bg);
+}
+
+// Adds the pieces of every (b, g), a group a block.
+__global__ __launch_bounds__(kThreads) void norm_stat_kernel(NormArgs a, const double2* part, Stat* stat, float* mean, float* rstd) {
+  __shared__ double red[2 * kThreads / 64];
+  const bool tells = threadIdx.x == 0;
+  const Stat s = block_stat(a, a.pieces, stat, part, blockIdx.x, tells ? mean : nullptr, tells ? rstd : nullptr, red);
+  __syncthreads();
+  if (tells) stat[blockIdx.x] = s;
 }
 
 // What one channel's values go through
@@ -232,15 +238,25 @@ __device__ __forceinline__ void apply_range(const Affine& f, const T* x, T* y, l
               [&](long long at) { store1(y + at, normed<ACT>(f, load1(x + at))); });
 }
 
-// A piece of a row per block; short: a row per wave.
+// A piece of a row per block; short: a row per wave.  part: the sums of the group's `parts` pieces, few enough for every
+// block to add them itself (null: the statistics are in `stat`).
 template <class T, int ACT, bool SHORT>
 __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, const T* x, const float* gamma, const float* beta,
-                                                              const Stat* stat, T* y) {
+                                                              const Stat* stat, const double2* part, int parts, float* mean,
+                                                              float* rstd, T* y) {
+  __shared__ double red[2 * kThreads / 64];
   const long long row = SHORT ? (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6) : blockIdx.x / a.pieces;
   if (SHORT && row >= (long long)a.B * a.C) return;
   const int c = (int)(row % a.C);
-  const Affine f = affine_of(stat[row / a.D], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
   const long long j = SHORT ? 0 : blockIdx.x % a.pieces;
+  Stat st;
+  if (!SHORT && part != nullptr) {
+    const bool tells = j == 0 && c % a.D == 0 && threadIdx.x == 0;
+    st = block_stat(a, parts, stat, part, row / a.D, tells ? mean : nullptr, tells ? rstd : nullptr, red);
+  } else {
+    st = stat[row / a.D];
+  }
+  const Affine f = affine_of(st, gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
   const long long begin = row * a.P + j * a.per, end = SHORT || (j + 1) * a.per >= a.P ? (row + 1) * a.P : begin + a.per;
   if (SHORT) apply_range<T, ACT>(f, x, y, begin, end, threadIdx.x & 63, 64);
   else apply_range<T, ACT>(f, x, y, begin, end, threadIdx.x, kThreads);
@@ -312,28 +328,11 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, con
   }
 }
 
-// Blocks 0 .. B G - 1: m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the parameters'
-// gradients, a channel a wave.  part[(b, c)][piece].
-__global__ __launch_bounds__(kThreads) void norm_grad_fold_kernel(NormArgs a, const double2* part, const float* gamma, float2* m,
-                                                                  float* ggamma, float* gbeta, int accumulate) {
-  __shared__ double red[2 * kThreads / 64];
-  const long long groups = (long long)a.B * a.G;
-  double s1 = 0.0, s2 = 0.0;
-  if (blockIdx.x < groups) {
-    const long long count = (long long)a.D * a.pieces, at = blockIdx.x * count;
-    const int c0 = (int)(blockIdx.x % a.G) * a.D;
-    for (long long j = threadIdx.x; j < count; j += kThreads) {
-      const double2 p = part[at + j];
-      const double ga = gamma ? gamma[c0 + (int)(j / a.pieces)] : 1.f;
-      s1 = fma(ga, p.x, s1);
-      s2 = fma(ga, p.y, s2);
-    }
-    block_sum2(s1, s2, red);
-    if (threadIdx.x == 0) m[blockIdx.x] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
-    return;
-  }
-  const long long c = (blockIdx.x - groups) * (kThreads / 64) + (threadIdx.x >> 6);
+// A channel's parameter gradients, by a wave: sums over batch entries and pieces.  part[(b, c)][piece].
+__device__ __forceinline__ void param_grads(const NormArgs& a, const double2* part, long long c, float* ggamma, float* gbeta,
+                                            int accumulate) {
   if (c >= a.C) return;
+  double s1 = 0.0, s2 = 0.0;
   const long long count = (long long)a.B * a.pieces;
   for (long long j = threadIdx.x & 63; j < count; j += 64) {
     const double2 p = part[(j / a.pieces * a.C + c) * a.pieces + j % a.pieces];
@@ -341,10 +340,35 @@ __global__ __launch_bounds__(kThreads) void norm_grad_fold_kernel(NormArgs a, co
     s2 += p.y;
   }
   wave_sum2(s1, s2);
-  if ((threadIdx.x & 63) == 0) {
-    if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + s1 : s1);
-    if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + s2 : s2);
+  if ((threadIdx.x & 63) != 0) return;
+  if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + s1 : s1);
+  if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + s2 : s2);
+}
+// A thread's share of the sums of gamma gz and gamma gz xh over a group: thread `tid` of `threads`
+__device__ __forceinline__ void group_share(const NormArgs& a, const double2* part, const float* gamma, long long bg, int tid,
+                                            int threads, double& s1, double& s2) {
+  const long long count = (long long)a.D * a.pieces, at = bg * count;
+  const int c0 = (int)(bg % a.G) * a.D;
+  for (long long j = tid; j < count; j += threads) {
+    const double2 p = part[at + j];
+    const double ga = gamma ? gamma[c0 + (int)(j / a.pieces)] : 1.f;
+    s1 = fma(ga, p.x, s1);
+    s2 = fma(ga, p.y, s2);
   }
+}
+
+// Blocks 0 .. groups - 1 (B G, or none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the
+// parameters' gradients.
+__global__ __launch_bounds__(kThreads) void norm_grad_fold_kernel(NormArgs a, unsigned groups, const double2* part,
+                                                                  const float* gamma, float2* m, float* ggamma, float* gbeta,
+                                                                  int accumulate) {
+  __shared__ double red[2 * kThreads / 64];
+  if (blockIdx.x >= groups)
+    return param_grads(a, part, (long long)(blockIdx.x - groups) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+  double s1 = 0.0, s2 = 0.0;
+  group_share(a, part, gamma, blockIdx.x, threadIdx.x, kThreads, s1, s2);
+  block_sum2(s1, s2, red);
+  if (threadIdx.x == 0) m[blockIdx.x] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
 }
 
 template <int ACT>
@@ -354,17 +378,30 @@ __device__ __forceinline__ float grad_of(const Slope& k, float2 m, float x, floa
   return k.rstd * (fmaf(gz, k.gamma, -m.x) - xh * m.y);
 }
 
+// m null: every block adds its group's sums itself, and the blocks from `mine` on the parameters' gradients.
 template <class T, int ACT, bool SHORT>
-__global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(NormArgs a, const T* x, const T* gy, const float* gamma,
-                                                                   const float* beta, const float* mean, const float* rstd,
-                                                                   const float2* m, T* gx) {
+__global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(NormArgs a, unsigned mine, const T* x, const T* gy,
+                                                                   const float* gamma, const float* beta, const float* mean,
+                                                                   const float* rstd, const float2* m, const double2* part,
+                                                                   float* ggamma, float* gbeta, int accumulate, T* gx) {
   constexpr int V = kVec<T>, U = 2;
+  __shared__ double red[2 * kThreads / 64];
+  if (!SHORT && blockIdx.x >= mine)
+    return param_grads(a, part, (long long)(blockIdx.x - mine) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
   const long long row = SHORT ? (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6) : blockIdx.x / a.pieces;
   if (SHORT && row >= (long long)a.B * a.C) return;
   const int c = (int)(row % a.C);
   const long long bg = row / a.D;
   const Slope k{mean[bg], rstd[bg], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f};
-  const float2 mm = m[bg];
+  float2 mm;
+  if (SHORT || m != nullptr) {
+    mm = m[bg];
+  } else {
+    double s1 = 0.0, s2 = 0.0;
+    group_share(a, part, gamma, bg, threadIdx.x, kThreads, s1, s2);
+    block_sum2(s1, s2, red);
+    mm = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
+  }
   const long long j = SHORT ? 0 : blockIdx.x % a.pieces;
   const long long begin = row * a.P + j * a.per, end = SHORT || (j + 1) * a.per >= a.P ? (row + 1) * a.P : begin + a.per;
   auto put = [&](long long at, pack<T> px, pack<T> pg) {
@@ -444,9 +481,9 @@ __device__ __forceinline__ void tree_groups(double* lds, int G, int D) {
   }
 }
 
-// part[(b, g)][piece] = (sum d, sum d^2)
+// part[(b, g)][piece] = (sum d, sum d^2); stat[(b, g)].hi = k
 template <class T>
-__global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int active, const T* x, double* part) {
+__global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int active, const T* x, double* part, Stat* stat) {
   constexpr int V = kVec<T>, U = 4;
   extern __shared__ double lds[];
   const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
@@ -497,20 +534,46 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
       part[2 * (((long long)b * a.G + g) * a.pieces + j) + half] = lds[g * a.D];
     __syncthreads();
   }
+  if (j == 0)
+    for (int g = threadIdx.x; g < a.G; g += blockDim.x) stat[(long long)b * a.G + g].hi = a.P > 0 ? load1(x + base + g * a.D) : 0.f;
 }
 
+// part: the sums of the batch entry's pieces, few enough for every block to add them itself, a group a wave (null: the
+// statistics are in `stat`).
 template <class T, int ACT>
 __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int active, const T* x, const float* gamma,
-                                                               const float* beta, const Stat* stat, T* y) {
+                                                               const float* beta, const Stat* stat, const double2* part,
+                                                               float* mean, float* rstd, T* y) {
   constexpr int V = kVec<T>, U = 4;
+  extern __shared__ double lds[];
   const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
+  Stat* const mine = reinterpret_cast<Stat*>(lds);
+  if (part != nullptr) {
+    const bool tells = j == 0 && (threadIdx.x & 63) == 0;
+    for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
+      const long long bg = (long long)b * a.G + g;
+      double s = 0.0, q = 0.0;
+      for (int k = threadIdx.x & 63; k < a.pieces; k += 64) {
+        const double2 p = part[bg * a.pieces + k];
+        s += p.x;
+        q += p.y;
+      }
+      wave_sum2(s, q);
+      const Stat st = stat_of(stat[bg].hi, s, q, a, tells ? mean : nullptr, tells ? rstd : nullptr, bg);
+      if ((threadIdx.x & 63) == 0) mine[g] = st;
+    }
+    __syncthreads();
+  }
   const long long p0 = (long long)j * a.per, p1 = p0 + a.per < a.P ? p0 + a.per : a.P;
   const long long base = (long long)b * a.P * a.C;
   Affine f[V];
 #pragma unroll
   for (int u = 0; u < V; ++u) {
     const int c = ((int)threadIdx.x * V + u) % a.C;
-    f[u] = affine_of(stat[(long long)b * a.G + c / a.D], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
+    Stat st;
+    if (part != nullptr) st = mine[c / a.D];
+    else st = stat[(long long)b * a.G + c / a.D];
+    f[u] = affine_of(st, gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
   }
   auto put = [&](long long at, pack<T> k) {
     float v[V];
@@ -608,10 +671,25 @@ __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, in
 }
 
 template <class T, int ACT>
-__global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, int active, const T* x, const T* gy,
+__global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, unsigned mine, int active, const T* x, const T* gy,
                                                                     const float* gamma, const float* beta, const float* mean,
-                                                                    const float* rstd, const float2* m, T* gx) {
+                                                                    const float* rstd, const float2* m, const double2* part,
+                                                                    float* ggamma, float* gbeta, int accumulate, T* gx) {
   constexpr int V = kVec<T>, U = 2;
+  extern __shared__ double lds[];
+  if (blockIdx.x >= mine)
+    return param_grads(a, part, (long long)(blockIdx.x - mine) * (blockDim.x >> 6) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+  float2* const own = reinterpret_cast<float2*>(lds);
+  if (m == nullptr) {
+    const long long b0 = blockIdx.x / a.pieces * (long long)a.G;
+    for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
+      double s1 = 0.0, s2 = 0.0;
+      group_share(a, part, gamma, b0 + g, threadIdx.x & 63, 64, s1, s2);
+      wave_sum2(s1, s2);
+      if ((threadIdx.x & 63) == 0) own[g] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
+    }
+    __syncthreads();
+  }
   const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   const long long p0 = (long long)j * a.per, p1 = p0 + a.per < a.P ? p0 + a.per : a.P;
   const long long base = (long long)b * a.P * a.C;
@@ -619,7 +697,11 @@ __global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, 
   slopes_of<V>(a, b, gamma, beta, mean, rstd, k);
   float2 mm[V];
 #pragma unroll
-  for (int u = 0; u < V; ++u) mm[u] = m[(long long)b * a.G + (((int)threadIdx.x * V + u) % a.C) / a.D];
+  for (int u = 0; u < V; ++u) {
+    const int g = (((int)threadIdx.x * V + u) % a.C) / a.D;
+    if (m == nullptr) mm[u] = own[g];
+    else mm[u] = m[(long long)b * a.G + g];
+  }
   auto put = [&](long long at, pack<T> px, pack<T> pg) {
     float v[V], g[V];
     unpack(px, v);
@@ -646,6 +728,188 @@ __global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, 
                      for (int w = 0; w < V; ++w)
                        if (w == u) store1(gx + at, grad_of<ACT>(k[w], mm[w], v, g));
                    });
+}
+
+// ------------------------------------------------------------------------------------------
+// Groups that one block holds in its registers: one launch, x (and gy) read once.  A thread has 16 values of the group,
+// those of whole 16-byte runs where the runs stay within a point's channels of the group (channels first: always), else
+// every `threads`-th.  The adjoint's sums over a channel go through LDS.
+// ------------------------------------------------------------------------------------------
+constexpr int kSmallValues = 16;                          // of a thread
+constexpr int kSmallFwd = 1024 * kSmallValues, kSmallBwd = 8192;
+
+struct SmallArgs {
+  int n;                // values of the group
+  int run;              // 16-byte runs (1) or single values (0)
+  unsigned by;          // 2^32 / (channels first: P, channels last: D) + 1, for divisions of numbers below 2^14; 0: by one
+};
+__device__ __forceinline__ int over(unsigned e, unsigned by) { return by == 0 ? (int)e : (int)__umulhi(e, by); }
+
+// Calls f(k, e) for the thread's values, e their number in the group (below n).
+template <class T, class F>
+__device__ __forceinline__ void small_values(const SmallArgs& s, F&& f) {
+  constexpr int V = kVec<T>;
+#pragma unroll
+  for (int k = 0; k < kSmallValues; ++k) {
+    const int e = s.run ? ((k / V) * (int)blockDim.x + (int)threadIdx.x) * V + k % V : k * (int)blockDim.x + (int)threadIdx.x;
+    if (e < s.n) f(k, e);
+  }
+}
+template <bool LAST>
+__device__ __forceinline__ long long small_at(const NormArgs& a, const SmallArgs& s, int b, int g, int e) {
+  if (!LAST) return ((long long)b * a.C + (long long)g * a.D) * a.P + e;
+  const int p = over(e, s.by);
+  return ((long long)b * a.P + p) * a.C + g * a.D + (e - p * a.D);
+}
+template <bool LAST>
+__device__ __forceinline__ int small_channel(const NormArgs& a, const SmallArgs& s, int e) {
+  return LAST ? e - over(e, s.by) * a.D : over(e, s.by);
+}
+template <class T, bool LAST>
+__device__ __forceinline__ void small_load(const NormArgs& a, const SmallArgs& s, int b, int g, const T* x, float (&v)[kSmallValues]) {
+  constexpr int V = kVec<T>;
+  if (s.run) {
+    pack<T> q[kSmallValues / V];
+#pragma unroll
+    for (int k = 0; k < kSmallValues / V; ++k) {
+      const int e = (k * (int)blockDim.x + (int)threadIdx.x) * V;
+      q[k] = pack<T>{};
+      if (e + V <= s.n) q[k] = load_any(x + small_at<LAST>(a, s, b, g, e));
+    }
+#pragma unroll
+    for (int k = 0; k < kSmallValues / V; ++k) {
+      float w[V];
+      unpack(q[k], w);
+#pragma unroll
+      for (int u = 0; u < V; ++u) v[k * V + u] = w[u];
+      const int e = (k * (int)blockDim.x + (int)threadIdx.x) * V;
+      if (e < s.n && e + V > s.n) {                       // the group's last values, channels first
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+          if (e + u < s.n) v[k * V + u] = load1(x + small_at<LAST>(a, s, b, g, e + u));
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kSmallValues; ++k) {
+    const int e = k * (int)blockDim.x + (int)threadIdx.x;
+    v[k] = e < s.n ? load1(x + small_at<LAST>(a, s, b, g, e)) : 0.f;
+  }
+}
+template <class T, bool LAST>
+__device__ __forceinline__ void small_store(const NormArgs& a, const SmallArgs& s, int b, int g, T* y, const float (&v)[kSmallValues]) {
+  constexpr int V = kVec<T>;
+  if (s.run) {
+#pragma unroll
+    for (int k = 0; k < kSmallValues / V; ++k) {
+      const int e = (k * (int)blockDim.x + (int)threadIdx.x) * V;
+      float w[V];
+#pragma unroll
+      for (int u = 0; u < V; ++u) w[u] = v[k * V + u];
+      if (e + V <= s.n) {
+        store_any(y + small_at<LAST>(a, s, b, g, e), repack(w));
+      } else {
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+          if (e + u < s.n) store1(y + small_at<LAST>(a, s, b, g, e + u), w[u]);
+      }
+    }
+    return;
+  }
+  small_values<T>(s, [&](int k, int e) { store1(y + small_at<LAST>(a, s, b, g, e), v[k]); });
+}
+
+template <class T, int ACT, bool LAST>
+__global__ __launch_bounds__(1024) void norm_small_kernel(NormArgs a, SmallArgs s, const T* x, const float* gamma, const float* beta,
+                                                          T* y, float* mean, float* rstd) {
+  __shared__ double red[2 * 1024 / 64];
+  __shared__ float2 affine[kMaxNormChannels];
+  const int b = blockIdx.x / a.G, g = blockIdx.x % a.G;
+  float v[kSmallValues];
+  small_load<T, LAST>(a, s, b, g, x, v);
+  const float first = load1(x + small_at<LAST>(a, s, b, g, 0));
+  double sum = 0.0, square = 0.0;
+  small_values<T>(s, [&](int k, int) {
+    const double d = v[k] - first;
+    sum += d;
+    square = fma(d, d, square);
+  });
+  block_sum2(sum, square, red);
+  const bool tells = threadIdx.x == 0;
+  const Stat st = stat_of(first, sum, square, a, tells ? mean : nullptr, tells ? rstd : nullptr, blockIdx.x);
+  for (int d = threadIdx.x; d < a.D; d += blockDim.x) {
+    const Affine f = affine_of(st, gamma ? gamma[g * a.D + d] : 1.f, beta ? beta[g * a.D + d] : 0.f);
+    affine[d] = make_float2(f.scale, f.shift);
+  }
+  __syncthreads();
+  small_values<T>(s, [&](int k, int e) {
+    const float2 f = affine[small_channel<LAST>(a, s, e)];
+    v[k] = normed<ACT>(Affine{st.hi, f.x, f.y}, v[k]);
+  });
+  small_store<T, LAST>(a, s, b, g, y, v);
+}
+
+// part (B > 1) or ggamma and gbeta (B = 1) receive the channels' sums; lanes: how many add a channel's, a power of two.
+template <class T, int ACT, bool LAST>
+__global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, SmallArgs s, int lanes, const T* x, const T* gy,
+                                                               const float* gamma, const float* beta, const float* mean,
+                                                               const float* rstd, T* gx, double2* part, float* ggamma,
+                                                               float* gbeta, int accumulate) {
+  __shared__ double red[2 * 1024 / 64];
+  __shared__ float2 affine[kMaxNormChannels];
+  extern __shared__ double lds[];
+  const int b = blockIdx.x / a.G, g = blockIdx.x % a.G;
+  const bool params = part != nullptr || ggamma != nullptr || gbeta != nullptr;
+  float v[kSmallValues], w[kSmallValues];
+  small_load<T, LAST>(a, s, b, g, x, v);
+  small_load<T, LAST>(a, s, b, g, gy, w);
+  for (int d = threadIdx.x; d < a.D; d += blockDim.x)
+    affine[d] = make_float2(gamma ? gamma[g * a.D + d] : 1.f, beta ? beta[g * a.D + d] : 0.f);
+  const float mu = mean[blockIdx.x], rs = rstd[blockIdx.x];
+  float2* const product = reinterpret_cast<float2*>(lds);      // gz and gz xh of every value
+  __syncthreads();
+  double s1 = 0.0, s2 = 0.0;
+  small_values<T>(s, [&](int k, int e) {                  // v: xh, w: gamma gz
+    const float2 f = affine[small_channel<LAST>(a, s, e)];
+    float xh, gz;
+    terms<ACT>(Slope{mu, rs, f.x, f.y}, v[k], w[k], xh, gz);
+    v[k] = xh;
+    w[k] = gz * f.x;
+    s1 += w[k];
+    s2 = fma((double)w[k], (double)xh, s2);
+    if (params) product[e] = make_float2(gz, gz * xh);
+  });
+  block_sum2(s1, s2, red);
+  if (gx != nullptr) {
+    const float m1 = (float)(s1 * a.inv_n), m2 = (float)(s2 * a.inv_n);
+    small_values<T>(s, [&](int k, int) { w[k] = rs * ((w[k] - m1) - v[k] * m2); });
+    small_store<T, LAST>(a, s, b, g, gx, w);
+  }
+  if (!params) return;
+  const int lane = threadIdx.x & (lanes - 1), P = (int)a.P;
+  for (int d0 = 0; d0 < a.D; d0 += blockDim.x / lanes) {  // (the same number of turns for all lanes of a wave)
+    const int d = d0 + threadIdx.x / lanes;
+    double t1 = 0.0, t2 = 0.0;
+    if (d < a.D)
+      for (int p = lane; p < P; p += lanes) {
+        const float2 q = product[LAST ? p * a.D + d : d * P + p];
+        t1 += q.x;
+        t2 += q.y;
+      }
+    for (int off = lanes >> 1; off >= 1; off >>= 1) {
+      t1 += __shfl_xor(t1, off);
+      t2 += __shfl_xor(t2, off);
+    }
+    if (d >= a.D || lane != 0) continue;
+    const int c = g * a.D + d;
+    if (part != nullptr) {
+      part[(long long)b * a.C + c] = make_double2(t1, t2);
+    } else {
+      if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + t1 : t1);
+      if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + t2 : t2);
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -711,30 +975,56 @@ unsigned row_blocks(const NormArgs& a, bool short_rows) {
   return (unsigned)(short_rows ? (rows + kThreads / 64 - 1) / (kThreads / 64) : rows * a.pieces);
 }
 
+// Sums of pieces that every block of the next launch adds itself (16 or 32 KB from the L2 a block), sparing a launch
+constexpr long long kInlineParts = 1024;
+
+bool small_fits(const NormShape& n, int most) { return n.P > 0 && n.P <= most && n.P * (n.C / n.G) <= most; }
+SmallArgs small_args(const NormShape& n, int V) {
+  const int D = n.C / n.G;
+  const unsigned by = n.last ? (unsigned)D : (unsigned)n.P;
+  return SmallArgs{(int)(n.P * D), !n.last || D % V == 0 ? 1 : 0, by == 1 ? 0u : (unsigned)(0x100000000ull / by) + 1u};
+}
+// Threads for n values, 4 of them at least a thread where there are enough waves, 16 at most.
+int small_threads(int n) {
+  const int t = (n + 3) / 4 < 256 ? (n + 3) / 4 : (n + kSmallValues - 1) / kSmallValues < 256 ? 256 : (n + kSmallValues - 1) / kSmallValues;
+  return (t + 63) / 64 * 64;
+}
+
 template <class T, int ACT>
 hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* beta, T* y, float* mean, float* rstd,
                void* ws, hipStream_t s) {
   double2* part = static_cast<double2*>(ws);
   Stat* stat = reinterpret_cast<Stat*>(static_cast<char*>(ws) + norm_part_bytes(n));
   const int bg = n.B * n.G;
+  if (small_fits(n, kSmallFwd)) {
+    const NormArgs a = norm_args(n);
+    const SmallArgs k = small_args(n, kVec<T>);
+    if (n.last) hipLaunchKernelGGL((norm_small_kernel<T, ACT, true>), dim3(bg), dim3(small_threads(k.n)), 0, s, a, k, x, gamma, beta, y, mean, rstd);
+    else hipLaunchKernelGGL((norm_small_kernel<T, ACT, false>), dim3(bg), dim3(small_threads(k.n)), 0, s, a, k, x, gamma, beta, y, mean, rstd);
+    return hipGetLastError();
+  }
   if (n.last) {
     const NormArgs a = cut_points(n);
     const int active = active_threads(n.C, kVec<T>), threads = (active + 63) / 64 * 64;
+    const bool inside = (long long)n.G * a.pieces <= kInlineParts && n.P > 0;
     hipLaunchKernelGGL((norm_last_sum_kernel<T>), dim3((unsigned)(n.B * a.pieces)), dim3(threads),
-                       (size_t)active * kVec<T> * sizeof(double), s, a, active, x, reinterpret_cast<double*>(part));
-    hipLaunchKernelGGL((norm_stat_kernel<T, true>), dim3(bg), dim3(kThreads), 0, s, a, x, part, stat, mean, rstd);
+                       (size_t)active * kVec<T> * sizeof(double), s, a, active, x, reinterpret_cast<double*>(part), stat);
+    if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(bg), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
     if (n.P > 0)
-      hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT>), dim3((unsigned)(n.B * a.pieces)), dim3(threads), 0, s, a, active, x, gamma,
-                         beta, stat, y);
+      hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT>), dim3((unsigned)(n.B * a.pieces)), dim3(threads),
+                         inside ? n.G * sizeof(Stat) : 0, s, a, active, x, gamma, beta, stat, inside ? part : nullptr, mean, rstd, y);
     return hipGetLastError();
   }
   const NormArgs a = cut_groups(n), r = cut_rows(n);
-  hipLaunchKernelGGL((norm_sum_kernel<T>), dim3((unsigned)(bg * a.pieces)), dim3(kThreads), 0, s, a, x, part);
-  hipLaunchKernelGGL((norm_stat_kernel<T, false>), dim3(bg), dim3(kThreads), 0, s, a, x, part, stat, mean, rstd);
-  if (n.P < kShortRow)
-    hipLaunchKernelGGL((norm_apply_kernel<T, ACT, true>), dim3(row_blocks(r, true)), dim3(kThreads), 0, s, r, x, gamma, beta, stat, y);
+  const bool short_rows = n.P < kShortRow, inside = !short_rows && a.pieces <= kInlineParts / 4;
+  hipLaunchKernelGGL((norm_sum_kernel<T>), dim3((unsigned)(bg * a.pieces)), dim3(kThreads), 0, s, a, x, part, stat);
+  if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(bg), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
+  if (short_rows)
+    hipLaunchKernelGGL((norm_apply_kernel<T, ACT, true>), dim3(row_blocks(r, true)), dim3(kThreads), 0, s, r, x, gamma, beta, stat,
+                       nullptr, 0, mean, rstd, y);
   else
-    hipLaunchKernelGGL((norm_apply_kernel<T, ACT, false>), dim3(row_blocks(r, false)), dim3(kThreads), 0, s, r, x, gamma, beta, stat, y);
+    hipLaunchKernelGGL((norm_apply_kernel<T, ACT, false>), dim3(row_blocks(r, false)), dim3(kThreads), 0, s, r, x, gamma, beta, stat,
+                       inside ? part : nullptr, a.pieces, mean, rstd, y);
   return hipGetLastError();
 }
 
@@ -743,32 +1033,54 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
                const T* gy, T* gx, float* ggamma, float* gbeta, int accumulate, void* ws, hipStream_t s) {
   double2* part = static_cast<double2*>(ws);
   float2* m = reinterpret_cast<float2*>(static_cast<char*>(ws) + norm_part_bytes(n));
-  const unsigned fold = (unsigned)(n.B * n.G + (n.C + kThreads / 64 - 1) / (kThreads / 64));
-  if (n.last) {
-    const NormArgs a = cut_points(n);
-    const int active = active_threads(n.C, kVec<T>), threads = (active + 63) / 64 * 64;
-    const dim3 grid((unsigned)(n.B * a.pieces));
-    hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT>), grid, dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a, active,
-                       x, gy, gamma, beta, mean, rstd, reinterpret_cast<double*>(part));
-    hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold), dim3(kThreads), 0, s, a, part, gamma, m, ggamma, gbeta, accumulate);
-    if (gx != nullptr && n.P > 0)
-      hipLaunchKernelGGL((norm_last_grad_apply_kernel<T, ACT>), grid, dim3(threads), 0, s, a, active, x, gy, gamma, beta, mean, rstd, m,
-                         gx);
+  const bool params = ggamma != nullptr || gbeta != nullptr;
+  if (small_fits(n, kSmallBwd)) {
+    const NormArgs a = norm_args(n);
+    const SmallArgs k = small_args(n, kVec<T>);
+    int lanes = 1;
+    while (lanes < 64 && lanes < n.P) lanes *= 2;
+    const bool later = params && n.B > 1;
+    const size_t lds = params ? k.n * sizeof(float2) : 0;
+    auto launch = [&](auto last) {
+      hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.B * n.G), dim3(small_threads(k.n)), lds, s, a, k,
+                         lanes, x, gy, gamma, beta, mean, rstd, gx, later ? part : nullptr, ggamma, gbeta, accumulate);
+    };
+    if (n.last) launch(std::true_type());
+    else launch(std::false_type());
+    if (later)
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3((n.C + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s, a, 0u, part, gamma,
+                         m, ggamma, gbeta, accumulate);
     return hipGetLastError();
   }
-  const NormArgs r = cut_rows(n);
-  const bool short_rows = n.P < kShortRow;
-  const dim3 grid(row_blocks(r, short_rows));
-  if (short_rows)
-    hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, true>), grid, dim3(kThreads), 0, s, r, x, gy, gamma, beta, mean, rstd, part);
+  const bool short_rows = !n.last && n.P < kShortRow;
+  const NormArgs a = n.last ? cut_points(n) : cut_rows(n);
+  const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
+  const unsigned blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
+  const unsigned channel_blocks = (unsigned)((n.C + threads / 64 - 1) / (threads / 64));
+  if (n.last)
+    hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT>), dim3(blocks), dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a,
+                       active, x, gy, gamma, beta, mean, rstd, reinterpret_cast<double*>(part));
+  else if (short_rows)
+    hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, true>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd, part);
   else
-    hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, false>), grid, dim3(kThreads), 0, s, r, x, gy, gamma, beta, mean, rstd, part);
-  hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold), dim3(kThreads), 0, s, r, part, gamma, m, ggamma, gbeta, accumulate);
-  if (gx == nullptr) return hipGetLastError();
-  if (short_rows)
-    hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, true>), grid, dim3(kThreads), 0, s, r, x, gy, gamma, beta, mean, rstd, m, gx);
+    hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, false>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd, part);
+  const bool writes = gx != nullptr && n.P > 0;
+  const bool inside = writes && !short_rows && (long long)(n.last ? n.C : n.C / n.G) * a.pieces <= kInlineParts;
+  if (!inside)
+    hipLaunchKernelGGL(norm_grad_fold_kernel, dim3((unsigned)(n.B * n.G) + (n.C + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s,
+                       a, (unsigned)(n.B * n.G), part, gamma, m, ggamma, gbeta, accumulate);
+  if (!writes) return hipGetLastError();
+  const dim3 grid(blocks + (inside && params ? channel_blocks : 0));
+  const float2* means = inside ? nullptr : m;
+  if (n.last)
+    hipLaunchKernelGGL((norm_last_grad_apply_kernel<T, ACT>), grid, dim3(threads), inside ? n.G * sizeof(float2) : 0, s, a, blocks, active,
+                       x, gy, gamma, beta, mean, rstd, means, part, ggamma, gbeta, accumulate, gx);
+  else if (short_rows)
+    hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, true>), grid, dim3(kThreads), 0, s, a, blocks, x, gy, gamma, beta, mean, rstd, means,
+                       part, ggamma, gbeta, accumulate, gx);
   else
-    hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, false>), grid, dim3(kThreads), 0, s, r, x, gy, gamma, beta, mean, rstd, m, gx);
+    hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, false>), grid, dim3(kThreads), 0, s, a, blocks, x, gy, gamma, beta, mean, rstd, means,
+                       part, ggamma, gbeta, accumulate, gx);
   return hipGetLastError();
 }
 
