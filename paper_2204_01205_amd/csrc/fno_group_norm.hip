@@ -4,10 +4,12 @@
 // What the operator moves bounds it: x in and y out (adjoint: x and gy in, gx out), 20 to 40 operations a value.  The
 // statistics (adjoint: the sums) of a group need all of it before its first output, so a group that does not fit one
 // block's registers is read twice: sums of pieces, a small launch that adds the pieces' sums in a fixed order, and the
-// sweep that writes.  The statistics come from d = x - k, k the group's first value: mean = k + E d, var = E d^2 - (E d)^2,
-// sums in double, so that values far from zero lose nothing and a constant group has the variance zero.
+// sweep that writes.  The statistics come from d = x - k, mean = k + E d, var = E d^2 - (E d)^2, k the middle one of three of
+// the group's values, so that values far from zero lose nothing, one that is far from the others does no harm as k, and a
+// constant group has the variance zero.  Four or eight terms are added in float, everything else in double.
 #include "fno_device.h"
 
+#include <climits>
 #include <type_traits>
 
 namespace fno {
@@ -27,10 +29,10 @@ template <class T> struct pack_of;
 template <> struct pack_of<float> { typedef v4f type; };
 template <> struct pack_of<u16> { typedef u32x4 type; };
 template <class T> using pack = typename pack_of<T>::type;
-template <class T>
-__device__ __forceinline__ pack<T> load_pack(const T* p) { return *reinterpret_cast<const pack<T>*>(p); }
-template <class T>
-__device__ __forceinline__ void store_pack(T* p, pack<T> v) { *reinterpret_cast<pack<T>*>(p) = v; }
+template <bool STREAM, class T>
+__device__ __forceinline__ pack<T> load_pack(const T* p) { return ld_once<STREAM>(reinterpret_cast<const pack<T>*>(p)); }
+template <bool STREAM, class T>
+__device__ __forceinline__ void store_pack(T* p, pack<T> v) { st_once<STREAM>(reinterpret_cast<pack<T>*>(p), v); }
 __device__ __forceinline__ void unpack(v4f q, float (&v)[4]) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) v[u] = q[u];
@@ -57,12 +59,22 @@ __device__ __forceinline__ float act_f(float z) {
   if constexpr (ACT == 2) return z * sigmoid_f(z);
   return z;
 }
+// act'(z) of z / kArg<ACT>.  GELU: Phi + z phi with both from one exponential, by the upper tail exp(-z^2 / 2) t P(t) of
+// gelu_and_grad_f; with z in units of sqrt(2 / log2 e) the exponent is a plain square.  With G = 1 + e (z phi(0) - t P) at |z|
+// it is G right of zero and 1 - G left of it.
+template <int ACT> constexpr float kArg = ACT == 1 ? 0.84932180028f : 1.0f;        // sqrt(log2(e) / 2)
 template <int ACT>
 __device__ __forceinline__ float slope_f(float z) {
   if constexpr (ACT == 1) {
-    float v, g;
-    gelu_and_grad_f(z, v, g);
-    return g;
+    const float a = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(a, 0.4f / kArg<1>, 1.0f));
+    float q = fmaf(t, 5.5231631e-02f, -2.5018391e-01f);
+    q = fmaf(t, q, 3.3274594e-01f);
+    q = fmaf(t, q, 1.8495135e-02f);
+    q = fmaf(t, q, 1.8670905e-01f);
+    q = fmaf(t, q, 1.5700214e-01f);
+    const float e = __builtin_amdgcn_exp2f(-z * z);
+    const float w = e * fmaf(-t, q, a * (0.39894228040f / kArg<1>));
+    return z < 0.f ? -w : 1.0f + w;
   }
   if constexpr (ACT == 2) {
     const float s = sigmoid_f(z);
@@ -75,9 +87,12 @@ struct NormArgs {
   int B, C, G, D;       // D = C / G
   long long P;
   double inv_n, eps;    // inv_n = 1 / (D P)
-  // pieces: of a group (forward, channels first), of a row (adjoint, channels first), of a batch entry (channels last)
-  int pieces;
-  long long per;        // values, or points (channels last), of a piece
+  // A range (forward, channels first: a group; adjoint, channels first: a row; channels last: a batch entry) is cut into
+  // tiles of 16 KB.  The launches that write take a tile a block, or deal the tiles to the blocks in turn, so that all blocks
+  // together move through memory in one window (128 x 128 x 64 x 32, 20 channels, adjoint: 1.31 ms, 1.70 with a stretch of
+  // tiles for every block); those that only read take a stretch each (the same: 0.86 ms, 0.95 in turn).
+  int pieces;           // blocks of a range
+  int run;              // tiles of a stretch
 };
 
 // What a group's values go through: xh = (x - mean) rstd with the mean in two floats, so that x - hi is exact near it.
@@ -124,19 +139,29 @@ __device__ __forceinline__ void block_sum2(double& a, double& b, double* red) {
   }
 }
 
-// Calls vec(at) for the 16-byte pieces of [begin, end) that start at multiples of their length, U of them at a time in
-// vecs(at, step), and one(at) for the values before and behind them.  Places count from a 16-byte aligned base.
+// The 16-byte pieces of [begin, end) that start at multiples of their length go in tiles of U pieces a thread, of which this
+// call takes number `tile` and every `stride`-th after it, `count` at most: vecs(at, step) for a whole tile, vec(at) for the pieces of the last
+// one, and, with tile 0, one(at) for the values before and behind the pieces.  Places count from a 16-byte aligned base.
 template <int V, int U, class FVecs, class FVec, class FOne>
-__device__ __forceinline__ void sweep(long long begin, long long end, int tid, int threads, FVecs&& vecs, FVec&& vec, FOne&& one) {
+__device__ __forceinline__ void sweep(long long begin, long long end, int tid, int threads, long long tile, long long stride,
+                                      int count, FVecs&& vecs, FVec&& vec, FOne&& one) {
   long long lo = (begin + V - 1) / V * V;
   if (lo > end) lo = end;
-  const long long hi = lo + (end - lo) / V * V;
+  const long long hi = lo + (end - lo) / V * V, step = (long long)threads * V, size = step * U;
+  long long base = lo + tile * size;
+  for (int i = 0; i < count && base < hi; ++i, base += stride * size) {
+    const long long at = base + (long long)tid * V;
+    if (base + size <= hi) {
+      vecs(at, step);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (at + u * step < hi) vec(at + u * step);
+    }
+  }
+  if (tile != 0) return;
   if (begin + tid < lo) one(begin + tid);
   if (hi + tid < end) one(hi + tid);
-  const long long step = (long long)threads * V;
-  long long at = lo + (long long)tid * V;
-  for (; at + (U - 1) * step < hi; at += U * step) vecs(at, step);
-  for (; at < hi; at += step) vec(at);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -144,40 +169,55 @@ __device__ __forceinline__ void sweep(long long begin, long long end, int tid, i
 // piece of one row (one channel), or whole short rows wave by wave, where gamma and beta come in.
 // ------------------------------------------------------------------------------------------
 
+// The value k of group g of batch entry b
+template <class T, bool LAST>
+__device__ __forceinline__ float middle_of(const NormArgs& a, const T* x, long long b, int g) {
+  if (a.P == 0) return 0.f;
+  const long long c0 = g * a.D, c1 = c0 + a.D / 2, c2 = c0 + a.D - 1, p1 = a.P / 2, p2 = a.P - 1;
+  const float u = load1(LAST ? x + b * a.P * a.C + c0 : x + (b * a.C + c0) * a.P);
+  const float v = load1(LAST ? x + (b * a.P + p1) * a.C + c1 : x + (b * a.C + c1) * a.P + p1);
+  const float w = load1(LAST ? x + (b * a.P + p2) * a.C + c2 : x + (b * a.C + c2) * a.P + p2);
+  return __builtin_amdgcn_fmed3f(u, v, w);
+}
+
 // part[(bg, piece)] = (sum d, sum d^2); stat[bg].hi = k, for the launches that follow, which may write over x
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs a, const T* x, double2* part, Stat* stat) {
   constexpr int V = kVec<T>, U = 4;
   __shared__ double red[2 * kThreads / 64];
   const long long bg = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces, n = a.P * a.D;
-  const long long begin = bg * n + j * a.per, end = j * a.per + a.per < n ? begin + a.per : (bg + 1) * n;
-  const float first = a.P > 0 ? load1(x + bg * n) : 0.f;
+  const float middle = middle_of<T, false>(a, x, bg / a.G, (int)(bg % a.G));
   double s = 0.0, q = 0.0;
-  auto add1 = [&](float v) {
-    const double d = v - first;
-    s += d;
-    q = fma(d, d, q);
-  };
   auto add = [&](pack<T> k) {
-    float v[V];
+    float v[V], d = 0.f, e = 0.f;
     unpack(k, v);
 #pragma unroll
-    for (int u = 0; u < V; ++u) add1(v[u]);
+    for (int u = 0; u < V; ++u) {
+      const float w = v[u] - middle;
+      d += w;
+      e = fmaf(w, w, e);
+    }
+    s += d;
+    q += e;
   };
-  sweep<V, U>(begin, end, threadIdx.x, kThreads,
+  sweep<V, U>(bg * n, (bg + 1) * n, threadIdx.x, kThreads, j * a.run, 1, a.run,
               [&](long long at, long long step) {
                 pack<T> k[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) k[u] = load_pack(x + at + u * step);
+                for (int u = 0; u < U; ++u) k[u] = load_pack<STREAM>(x + at + u * step);
 #pragma unroll
                 for (int u = 0; u < U; ++u) add(k[u]);
               },
-              [&](long long at) { add(load_pack(x + at)); },
-              [&](long long at) { add1(load1(x + at)); });
+              [&](long long at) { add(load_pack<STREAM>(x + at)); },
+              [&](long long at) {
+                const double d = load1(x + at) - middle;
+                s += d;
+                q = fma(d, d, q);
+              });
   block_sum2(s, q, red);
   if (threadIdx.x != 0) return;
-  part[blockIdx.x] = make_double2(s, q);
-  if (j == 0) stat[bg].hi = first;
+  part[bg * a.pieces + j] = make_double2(s, q);
+  if (j == 0) stat[bg].hi = middle;
 }
 
 // The statistics of group bg from its pieces' sums, in every thread of a block; red: as for block_sum2.
@@ -197,9 +237,10 @@ __device__ __forceinline__ Stat block_stat(const NormArgs& a, int pieces, const 
 __global__ __launch_bounds__(kThreads) void norm_stat_kernel(NormArgs a, const double2* part, Stat* stat, float* mean, float* rstd) {
   __shared__ double red[2 * kThreads / 64];
   const bool tells = threadIdx.x == 0;
-  const Stat s = block_stat(a, a.pieces, stat, part, blockIdx.x, tells ? mean : nullptr, tells ? rstd : nullptr, red);
+  const long long bg = blockIdx.x;
+  const Stat s = block_stat(a, a.pieces, stat, part, bg, tells ? mean : nullptr, tells ? rstd : nullptr, red);
   __syncthreads();
-  if (tells) stat[blockIdx.x] = s;
+  if (tells) stat[bg] = s;
 }
 
 // What one channel's values go through
@@ -216,31 +257,32 @@ __device__ __forceinline__ Affine affine_of(const Stat& s, float gamma, float be
 template <int ACT>
 __device__ __forceinline__ float normed(const Affine& f, float x) { return act_f<ACT>(fmaf(x - f.hi, f.scale, f.shift)); }
 
-template <class T, int ACT>
-__device__ __forceinline__ void apply_range(const Affine& f, const T* x, T* y, long long begin, long long end, int tid, int threads) {
+template <class T, int ACT, bool STREAM>
+__device__ __forceinline__ void apply_range(const Affine& f, const T* x, T* y, long long begin, long long end, int tid, int threads,
+                                            long long tile, long long stride) {
   constexpr int V = kVec<T>, U = 4;
   auto put = [&](long long at, pack<T> k) {
     float v[V];
     unpack(k, v);
 #pragma unroll
     for (int u = 0; u < V; ++u) v[u] = normed<ACT>(f, v[u]);
-    store_pack(y + at, repack(v));
+    store_pack<STREAM>(y + at, repack(v));
   };
-  sweep<V, U>(begin, end, tid, threads,
+  sweep<V, U>(begin, end, tid, threads, tile, stride, INT_MAX,
               [&](long long at, long long step) {
                 pack<T> k[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) k[u] = load_pack(x + at + u * step);
+                for (int u = 0; u < U; ++u) k[u] = load_pack<STREAM>(x + at + u * step);
 #pragma unroll
                 for (int u = 0; u < U; ++u) put(at + u * step, k[u]);
               },
-              [&](long long at) { put(at, load_pack(x + at)); },
+              [&](long long at) { put(at, load_pack<STREAM>(x + at)); },
               [&](long long at) { store1(y + at, normed<ACT>(f, load1(x + at))); });
 }
 
 // A piece of a row per block; short: a row per wave.  part: the sums of the group's `parts` pieces, few enough for every
 // block to add them itself (null: the statistics are in `stat`).
-template <class T, int ACT, bool SHORT>
+template <class T, int ACT, bool SHORT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, const T* x, const float* gamma, const float* beta,
                                                               const Stat* stat, const double2* part, int parts, float* mean,
                                                               float* rstd, T* y) {
@@ -257,23 +299,39 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, const 
     st = stat[row / a.D];
   }
   const Affine f = affine_of(st, gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
-  const long long begin = row * a.P + j * a.per, end = SHORT || (j + 1) * a.per >= a.P ? (row + 1) * a.P : begin + a.per;
-  if (SHORT) apply_range<T, ACT>(f, x, y, begin, end, threadIdx.x & 63, 64);
-  else apply_range<T, ACT>(f, x, y, begin, end, threadIdx.x, kThreads);
+  if (SHORT) apply_range<T, ACT, STREAM>(f, x, y, row * a.P, (row + 1) * a.P, threadIdx.x & 63, 64, 0, 1);
+  else apply_range<T, ACT, STREAM>(f, x, y, row * a.P, (row + 1) * a.P, threadIdx.x, kThreads, j, a.pieces);
 }
 
-// The adjoint's terms of one value
+// What one channel's values go through in the adjoint: d = x - mean, gz = gy act'(d rstd gamma + beta)
 struct Slope {
-  float mean, rstd, gamma, beta;
+  float mean, scale, shift;    // rstd gamma and beta in units of the activation's slope
 };
 template <int ACT>
-__device__ __forceinline__ void terms(const Slope& k, float x, float gy, float& xh, float& gz) {
-  xh = (x - k.mean) * k.rstd;
-  gz = ACT == 0 ? gy : gy * slope_f<ACT>(fmaf(xh, k.gamma, k.beta));
+__device__ __forceinline__ Slope slope_of(float mean, float rstd, float gamma, float beta) {
+  return Slope{mean, rstd * gamma * kArg<ACT>, beta * kArg<ACT>};
+}
+template <int ACT>
+__device__ __forceinline__ void terms(const Slope& k, float x, float gy, float& d, float& gz) {
+  d = x - k.mean;
+  gz = ACT == 0 ? gy : gy * slope_f<ACT>(fmaf(d, k.scale, k.shift));
+}
+// and gx = gz rstd gamma - rstd m1 - d rstd^2 m2, m1 and m2 the group's means of gamma gz and gamma gz xh
+struct Weights {
+  float gz, d, one;
+};
+__device__ __forceinline__ Weights weights_of(float rstd, float gamma, float2 m) {
+  return Weights{rstd * gamma, -rstd * rstd * m.y, -rstd * m.x};
+}
+template <int ACT>
+__device__ __forceinline__ float grad_of(const Slope& k, const Weights& w, float x, float gy) {
+  float d, gz;
+  terms<ACT>(k, x, gy, d, gz);
+  return fmaf(gz, w.gz, fmaf(d, w.d, w.one));
 }
 
 // part[(row, piece)] = (sum gz, sum gz xh)
-template <class T, int ACT, bool SHORT>
+template <class T, int ACT, bool SHORT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, const T* x, const T* gy, const float* gamma,
                                                                  const float* beta, const float* mean, const float* rstd,
                                                                  double2* part) {
@@ -283,9 +341,9 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, con
   if (SHORT && row >= (long long)a.B * a.C) return;
   const int c = (int)(row % a.C);
   const long long bg = row / a.D;
-  const Slope k{mean[bg], rstd[bg], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f};
+  const float rs = rstd[bg], ga = gamma ? gamma[c] : 1.f;
+  const Slope k = slope_of<ACT>(mean[bg], rs, ga, beta ? beta[c] : 0.f);
   const long long j = SHORT ? 0 : blockIdx.x % a.pieces;
-  const long long begin = row * a.P + j * a.per, end = SHORT || (j + 1) * a.per >= a.P ? (row + 1) * a.P : begin + a.per;
   double s1 = 0.0, s2 = 0.0;
   auto add = [&](pack<T> px, pack<T> pg) {
     float v[V], g[V], t1 = 0.f, t2 = 0.f;
@@ -293,51 +351,63 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, con
     unpack(pg, g);
 #pragma unroll
     for (int u = 0; u < V; ++u) {
-      float xh, gz;
-      terms<ACT>(k, v[u], g[u], xh, gz);
+      float d, gz;
+      terms<ACT>(k, v[u], g[u], d, gz);
       t1 += gz;
-      t2 = fmaf(gz, xh, t2);
+      t2 = fmaf(gz, d, t2);
     }
     s1 += t1;                                            // 4 or 8 terms in float, then doubles
     s2 += t2;
   };
-  sweep<V, U>(begin, end, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads,
+  sweep<V, U>(row * a.P, (row + 1) * a.P, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads, SHORT ? 0 : j * a.run, 1, SHORT ? INT_MAX : a.run,
               [&](long long at, long long step) {
                 pack<T> px[U], pg[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                  px[u] = load_pack(x + at + u * step);
-                  pg[u] = load_pack(gy + at + u * step);
+                  px[u] = load_pack<STREAM>(x + at + u * step);
+                  pg[u] = load_pack<STREAM>(gy + at + u * step);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) add(px[u], pg[u]);
               },
-              [&](long long at) { add(load_pack(x + at), load_pack(gy + at)); },
+              [&](long long at) { add(load_pack<STREAM>(x + at), load_pack<STREAM>(gy + at)); },
               [&](long long at) {
-                float xh, gz;
-                terms<ACT>(k, load1(x + at), load1(gy + at), xh, gz);
+                float d, gz;
+                terms<ACT>(k, load1(x + at), load1(gy + at), d, gz);
                 s1 += gz;
-                s2 = fma((double)gz, (double)xh, s2);
+                s2 = fma((double)gz, (double)d, s2);
               });
   if (SHORT) {
     wave_sum2(s1, s2);
-    if ((threadIdx.x & 63) == 0) part[row] = make_double2(s1, s2);
+    if ((threadIdx.x & 63) == 0) part[row] = make_double2(s1, s2 * rs);
   } else {
     block_sum2(s1, s2, red);
-    if (threadIdx.x == 0) part[blockIdx.x] = make_double2(s1, s2);
+    if (threadIdx.x == 0) part[row * a.pieces + j] = make_double2(s1, s2 * rs);
   }
 }
 
 // A channel's parameter gradients, by a wave: sums over batch entries and pieces.  part[(b, c)][piece].
-__device__ __forceinline__ void param_grads(const NormArgs& a, const double2* part, long long c, float* ggamma, float* gbeta,
+__device__ __forceinline__ void param_grads(const NormArgs& a, int pieces, const double2* part, long long c, float* ggamma, float* gbeta,
                                             int accumulate) {
   if (c >= a.C) return;
   double s1 = 0.0, s2 = 0.0;
-  const long long count = (long long)a.B * a.pieces;
-  for (long long j = threadIdx.x & 63; j < count; j += 64) {
-    const double2 p = part[(j / a.pieces * a.C + c) * a.pieces + j % a.pieces];
-    s1 += p.x;
-    s2 += p.y;
+  if (pieces >= 64) {
+    for (int b = 0; b < a.B; ++b) {
+      const double2* const at = part + ((long long)b * a.C + c) * pieces;
+#pragma unroll 8
+      for (int j = threadIdx.x & 63; j < pieces; j += 64) {
+        s1 += at[j].x;
+        s2 += at[j].y;
+      }
+    }
+  } else {
+    for (int b = threadIdx.x & 63; b < a.B; b += 64) {
+      const double2* const at = part + ((long long)b * a.C + c) * pieces;
+      for (int j = 0; j < pieces; ++j) {
+        s1 += at[j].x;
+        s2 += at[j].y;
+      }
+    }
   }
   wave_sum2(s1, s2);
   if ((threadIdx.x & 63) != 0) return;
@@ -345,86 +415,92 @@ __device__ __forceinline__ void param_grads(const NormArgs& a, const double2* pa
   if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + s2 : s2);
 }
 // A thread's share of the sums of gamma gz and gamma gz xh over a group: thread `tid` of `threads`
-__device__ __forceinline__ void group_share(const NormArgs& a, const double2* part, const float* gamma, long long bg, int tid,
+__device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const double2* part, const float* gamma, long long bg, int tid,
                                             int threads, double& s1, double& s2) {
-  const long long count = (long long)a.D * a.pieces, at = bg * count;
+  const double2* const at = part + bg * a.D * pieces;
   const int c0 = (int)(bg % a.G) * a.D;
-  for (long long j = tid; j < count; j += threads) {
-    const double2 p = part[at + j];
-    const double ga = gamma ? gamma[c0 + (int)(j / a.pieces)] : 1.f;
-    s1 = fma(ga, p.x, s1);
-    s2 = fma(ga, p.y, s2);
+  if (pieces >= threads) {
+    for (int d = 0; d < a.D; ++d) {
+      const double ga = gamma ? gamma[c0 + d] : 1.f;
+#pragma unroll 8
+      for (int j = tid; j < pieces; j += threads) {
+        const double2 p = at[(long long)d * pieces + j];
+        s1 = fma(ga, p.x, s1);
+        s2 = fma(ga, p.y, s2);
+      }
+    }
+  } else {
+    for (int j = tid; j < a.D * pieces; j += threads) {
+      const double2 p = at[j];
+      const double ga = gamma ? gamma[c0 + j / pieces] : 1.f;
+      s1 = fma(ga, p.x, s1);
+      s2 = fma(ga, p.y, s2);
+    }
   }
 }
 
-// Blocks 0 .. groups - 1 (B G, or none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the
+// Blocks 0 .. groups - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the
 // parameters' gradients.
 __global__ __launch_bounds__(kThreads) void norm_grad_fold_kernel(NormArgs a, unsigned groups, const double2* part,
                                                                   const float* gamma, float2* m, float* ggamma, float* gbeta,
                                                                   int accumulate) {
   __shared__ double red[2 * kThreads / 64];
   if (blockIdx.x >= groups)
-    return param_grads(a, part, (long long)(blockIdx.x - groups) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+    return param_grads(a, a.pieces, part, (long long)(blockIdx.x - groups) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
   double s1 = 0.0, s2 = 0.0;
-  group_share(a, part, gamma, blockIdx.x, threadIdx.x, kThreads, s1, s2);
+  group_share(a, a.pieces, part, gamma, blockIdx.x, threadIdx.x, kThreads, s1, s2);
   block_sum2(s1, s2, red);
   if (threadIdx.x == 0) m[blockIdx.x] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
 }
 
-template <int ACT>
-__device__ __forceinline__ float grad_of(const Slope& k, float2 m, float x, float gy) {
-  float xh, gz;
-  terms<ACT>(k, x, gy, xh, gz);
-  return k.rstd * (fmaf(gz, k.gamma, -m.x) - xh * m.y);
-}
-
 // m null: every block adds its group's sums itself, and the blocks from `mine` on the parameters' gradients.
-template <class T, int ACT, bool SHORT>
+template <class T, int ACT, bool SHORT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(NormArgs a, unsigned mine, const T* x, const T* gy,
                                                                    const float* gamma, const float* beta, const float* mean,
-                                                                   const float* rstd, const float2* m, const double2* part,
+                                                                   const float* rstd, const float2* m, const double2* part, int parts,
                                                                    float* ggamma, float* gbeta, int accumulate, T* gx) {
   constexpr int V = kVec<T>, U = 2;
   __shared__ double red[2 * kThreads / 64];
   if (!SHORT && blockIdx.x >= mine)
-    return param_grads(a, part, (long long)(blockIdx.x - mine) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+    return param_grads(a, parts, part, (long long)(blockIdx.x - mine) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
   const long long row = SHORT ? (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6) : blockIdx.x / a.pieces;
   if (SHORT && row >= (long long)a.B * a.C) return;
   const int c = (int)(row % a.C);
   const long long bg = row / a.D;
-  const Slope k{mean[bg], rstd[bg], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f};
+  const float rs = rstd[bg], ga = gamma ? gamma[c] : 1.f;
+  const Slope k = slope_of<ACT>(mean[bg], rs, ga, beta ? beta[c] : 0.f);
   float2 mm;
   if (SHORT || m != nullptr) {
     mm = m[bg];
   } else {
     double s1 = 0.0, s2 = 0.0;
-    group_share(a, part, gamma, bg, threadIdx.x, kThreads, s1, s2);
+    group_share(a, parts, part, gamma, bg, threadIdx.x, kThreads, s1, s2);
     block_sum2(s1, s2, red);
     mm = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
   }
   const long long j = SHORT ? 0 : blockIdx.x % a.pieces;
-  const long long begin = row * a.P + j * a.per, end = SHORT || (j + 1) * a.per >= a.P ? (row + 1) * a.P : begin + a.per;
+  const Weights w = weights_of(rs, ga, mm);
   auto put = [&](long long at, pack<T> px, pack<T> pg) {
     float v[V], g[V];
     unpack(px, v);
     unpack(pg, g);
 #pragma unroll
-    for (int u = 0; u < V; ++u) v[u] = grad_of<ACT>(k, mm, v[u], g[u]);
-    store_pack(gx + at, repack(v));
+    for (int u = 0; u < V; ++u) v[u] = grad_of<ACT>(k, w, v[u], g[u]);
+    store_pack<STREAM>(gx + at, repack(v));
   };
-  sweep<V, U>(begin, end, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads,
+  sweep<V, U>(row * a.P, (row + 1) * a.P, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads, j, a.pieces, INT_MAX,
               [&](long long at, long long step) {
                 pack<T> px[U], pg[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                  px[u] = load_pack(x + at + u * step);
-                  pg[u] = load_pack(gy + at + u * step);
+                  px[u] = load_pack<STREAM>(x + at + u * step);
+                  pg[u] = load_pack<STREAM>(gy + at + u * step);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) put(at + u * step, px[u], pg[u]);
               },
-              [&](long long at) { put(at, load_pack(x + at), load_pack(gy + at)); },
-              [&](long long at) { store1(gx + at, grad_of<ACT>(k, mm, load1(x + at), load1(gy + at))); });
+              [&](long long at) { put(at, load_pack<STREAM>(x + at), load_pack<STREAM>(gy + at)); },
+              [&](long long at) { store1(gx + at, grad_of<ACT>(k, w, load1(x + at), load1(gy + at))); });
 }
 
 // ------------------------------------------------------------------------------------------
@@ -434,28 +510,38 @@ __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(NormArgs a, u
 // aligned are read and written in 16-byte accesses at their values' own alignment.
 // ------------------------------------------------------------------------------------------
 
-template <class T>
+template <bool STREAM, class T>
 __device__ __forceinline__ pack<T> load_any(const T* p) {
   typedef pack<T> loose __attribute__((aligned(sizeof(T))));
-  return *reinterpret_cast<const loose*>(p);
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const loose*>(p));
+  else return *reinterpret_cast<const loose*>(p);
 }
-template <class T>
+template <bool STREAM, class T>
 __device__ __forceinline__ void store_any(T* p, pack<T> v) {
   typedef pack<T> loose __attribute__((aligned(sizeof(T))));
-  *reinterpret_cast<loose*>(p) = v;
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<loose*>(p));
+  else *reinterpret_cast<loose*>(p) = v;
 }
 
-// Calls vecs(at, step), vec(at) and one(at, u) (u: which of the thread's channels) over the values [begin, end) of whole
-// points; the last 16 bytes may be cut.
+// The values [begin, end) of whole points, as sweep() does; one(at, u) for the last values, which do not fill 16 bytes (u:
+// which of the thread's channels).
 template <int V, int U, class FVecs, class FVec, class FOne>
-__device__ __forceinline__ void sweep_last(long long begin, long long end, int active, FVecs&& vecs, FVec&& vec, FOne&& one) {
+__device__ __forceinline__ void sweep_last(long long begin, long long end, int active, long long tile, long long stride, int count,
+                                           FVecs&& vecs, FVec&& vec, FOne&& one) {
   if ((int)threadIdx.x >= active) return;
-  const long long step = (long long)active * V;
-  long long at = begin + (long long)threadIdx.x * V;
-  for (; at + (U - 1) * step + V <= end; at += U * step) vecs(at, step);
-  for (; at + V <= end; at += step) vec(at);
-  for (int u = 0; u < V; ++u)
-    if (at + u < end) one(at + u, u);
+  const long long step = (long long)active * V, size = step * U;
+  long long base = begin + tile * size;
+  for (int i = 0; i < count && base < end; ++i, base += stride * size) {
+    long long at = base + (long long)threadIdx.x * V;
+    if (base + size <= end) {
+      vecs(at, step);
+    } else {
+      for (; at + V <= end; at += step) vec(at);
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (at + u < end) one(at + u, u);
+    }
+  }
 }
 
 // lds[e], e < rows * C: sums over the rows, and then over the channels of every group where D > 1, left in lds[g * D].
@@ -482,46 +568,61 @@ __device__ __forceinline__ void tree_groups(double* lds, int G, int D) {
 }
 
 // part[(b, g)][piece] = (sum d, sum d^2); stat[(b, g)].hi = k
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int active, const T* x, double* part, Stat* stat) {
   constexpr int V = kVec<T>, U = 4;
   extern __shared__ double lds[];
-  const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
-  const long long p0 = (long long)j * a.per, p1 = p0 + a.per < a.P ? p0 + a.per : a.P;
+  const int b = (int)blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   const long long base = (long long)b * a.P * a.C;
   double s[V], q[V];
-  float first[V];
+  float middle[V];
 #pragma unroll
   for (int u = 0; u < V; ++u) {
     s[u] = q[u] = 0.0;
-    first[u] = a.P > 0 ? load1(x + base + ((int)threadIdx.x * V + u) % a.C / a.D * a.D) : 0.f;
+    middle[u] = middle_of<T, true>(a, x, b, ((int)threadIdx.x * V + u) % a.C / a.D);
   }
   auto add1 = [&](int u, float v) {
-    const double d = v - first[u];
+    const double d = v - middle[u];
     s[u] += d;
     q[u] = fma(d, d, q[u]);
   };
-  auto add = [&](pack<T> k) {
-    float v[V];
-    unpack(k, v);
+    sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
+                     [&](long long at, long long step) {
+                       pack<T> k[U];
 #pragma unroll
-    for (int u = 0; u < V; ++u) add1(u, v[u]);
-  };
-  sweep_last<V, U>(base + p0 * a.C, base + p1 * a.C, active,
-                   [&](long long at, long long step) {
-                     pack<T> k[U];
+                       for (int u = 0; u < U; ++u) k[u] = load_any<STREAM>(x + at + u * step);
+                       float d[V], e[V];
 #pragma unroll
-                     for (int u = 0; u < U; ++u) k[u] = load_any(x + at + u * step);
+                       for (int w = 0; w < V; ++w) d[w] = e[w] = 0.f;
 #pragma unroll
-                     for (int u = 0; u < U; ++u) add(k[u]);
-                   },
-                   [&](long long at) { add(load_any(x + at)); },
-                   [&](long long at, int u) {
-                     const float v = load1(x + at);
+                       for (int u = 0; u < U; ++u) {
+                         float v[V];
+                         unpack(k[u], v);
 #pragma unroll
-                     for (int w = 0; w < V; ++w)
-                       if (w == u) add1(w, v);
-                   });
+                         for (int w = 0; w < V; ++w) {
+                           const float f = v[w] - middle[w];
+                           d[w] += f;
+                           e[w] = fmaf(f, f, e[w]);
+                         }
+                       }
+#pragma unroll
+                       for (int w = 0; w < V; ++w) {
+                         s[w] += d[w];
+                         q[w] += e[w];
+                       }
+                     },
+                     [&](long long at) {
+                       float v[V];
+                       unpack(load_any<STREAM>(x + at), v);
+#pragma unroll
+                       for (int w = 0; w < V; ++w) add1(w, v[w]);
+                     },
+                     [&](long long at, int u) {
+                       const float v = load1(x + at);
+#pragma unroll
+                       for (int w = 0; w < V; ++w)
+                         if (w == u) add1(w, v);
+                     });
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     if ((int)threadIdx.x < active) {
@@ -535,14 +636,14 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
     __syncthreads();
   }
   if (j == 0)
-    for (int g = threadIdx.x; g < a.G; g += blockDim.x) stat[(long long)b * a.G + g].hi = a.P > 0 ? load1(x + base + g * a.D) : 0.f;
+    for (int g = threadIdx.x; g < a.G; g += blockDim.x) stat[(long long)b * a.G + g].hi = middle_of<T, true>(a, x, b, g);
 }
 
 // part: the sums of the batch entry's pieces, few enough for every block to add them itself, a group a wave (null: the
 // statistics are in `stat`).
-template <class T, int ACT>
+template <class T, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int active, const T* x, const float* gamma,
-                                                               const float* beta, const Stat* stat, const double2* part,
+                                                               const float* beta, const Stat* stat, const double2* part, int parts,
                                                                float* mean, float* rstd, T* y) {
   constexpr int V = kVec<T>, U = 4;
   extern __shared__ double lds[];
@@ -553,8 +654,8 @@ __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int a
     for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
       const long long bg = (long long)b * a.G + g;
       double s = 0.0, q = 0.0;
-      for (int k = threadIdx.x & 63; k < a.pieces; k += 64) {
-        const double2 p = part[bg * a.pieces + k];
+      for (int k = threadIdx.x & 63; k < parts; k += 64) {
+        const double2 p = part[bg * parts + k];
         s += p.x;
         q += p.y;
       }
@@ -564,7 +665,6 @@ __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int a
     }
     __syncthreads();
   }
-  const long long p0 = (long long)j * a.per, p1 = p0 + a.per < a.P ? p0 + a.per : a.P;
   const long long base = (long long)b * a.P * a.C;
   Affine f[V];
 #pragma unroll
@@ -580,17 +680,17 @@ __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int a
     unpack(k, v);
 #pragma unroll
     for (int u = 0; u < V; ++u) v[u] = normed<ACT>(f[u], v[u]);
-    store_any(y + at, repack(v));
+    store_any<STREAM>(y + at, repack(v));
   };
-  sweep_last<V, U>(base + p0 * a.C, base + p1 * a.C, active,
+  sweep_last<V, U>(base, base + a.P * a.C, active, j, a.pieces, INT_MAX,
                    [&](long long at, long long step) {
                      pack<T> k[U];
 #pragma unroll
-                     for (int u = 0; u < U; ++u) k[u] = load_any(x + at + u * step);
+                     for (int u = 0; u < U; ++u) k[u] = load_any<STREAM>(x + at + u * step);
 #pragma unroll
                      for (int u = 0; u < U; ++u) put(at + u * step, k[u]);
                    },
-                   [&](long long at) { put(at, load_any(x + at)); },
+                   [&](long long at) { put(at, load_any<STREAM>(x + at)); },
                    [&](long long at, int u) {
                      Affine g = f[0];
 #pragma unroll
@@ -600,64 +700,73 @@ __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int a
                    });
 }
 
-// the slopes of a thread's channels
-template <int V>
-__device__ __forceinline__ void slopes_of(const NormArgs& a, int b, const float* gamma, const float* beta, const float* mean,
-                                          const float* rstd, Slope (&k)[V]) {
-#pragma unroll
-  for (int u = 0; u < V; ++u) {
-    const int c = ((int)threadIdx.x * V + u) % a.C;
-    const long long bg = (long long)b * a.G + c / a.D;
-    k[u] = Slope{mean[bg], rstd[bg], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f};
-  }
-}
-
 // part[(b, c)][piece] = (sum gz, sum gz xh)
-template <class T, int ACT>
+template <class T, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, int active, const T* x, const T* gy,
                                                                   const float* gamma, const float* beta, const float* mean,
                                                                   const float* rstd, double* part) {
   constexpr int V = kVec<T>, U = 2;
   extern __shared__ double lds[];
-  const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
-  const long long p0 = (long long)j * a.per, p1 = p0 + a.per < a.P ? p0 + a.per : a.P;
+  const int b = (int)blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   const long long base = (long long)b * a.P * a.C;
   Slope k[V];
-  slopes_of<V>(a, b, gamma, beta, mean, rstd, k);
   double s1[V], s2[V];
 #pragma unroll
-  for (int u = 0; u < V; ++u) s1[u] = s2[u] = 0.0;
+  for (int u = 0; u < V; ++u) {
+    const int c = ((int)threadIdx.x * V + u) % a.C;
+    const long long bg = (long long)b * a.G + c / a.D;
+    k[u] = slope_of<ACT>(mean[bg], rstd[bg], gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
+    s1[u] = s2[u] = 0.0;
+  }
   auto add1 = [&](int u, float v, float g) {
-    float xh, gz;
-    terms<ACT>(k[u], v, g, xh, gz);
+    float d, gz;
+    terms<ACT>(k[u], v, g, d, gz);
     s1[u] += gz;
-    s2[u] = fma((double)gz, (double)xh, s2[u]);
+    s2[u] = fma((double)gz, (double)d, s2[u]);
   };
-  auto add = [&](pack<T> px, pack<T> pg) {
+  auto add = [&](pack<T> px, pack<T> pg, float (&t1)[V], float (&t2)[V]) {
     float v[V], g[V];
     unpack(px, v);
     unpack(pg, g);
 #pragma unroll
-    for (int u = 0; u < V; ++u) add1(u, v[u], g[u]);
+    for (int u = 0; u < V; ++u) {
+      float d, gz;
+      terms<ACT>(k[u], v[u], g[u], d, gz);
+      t1[u] += gz;
+      t2[u] = fmaf(gz, d, t2[u]);
+    }
   };
-  sweep_last<V, U>(base + p0 * a.C, base + p1 * a.C, active,
-                   [&](long long at, long long step) {
-                     pack<T> px[U], pg[U];
+  auto flush = [&](const float (&t1)[V], const float (&t2)[V]) {
 #pragma unroll
-                     for (int u = 0; u < U; ++u) {
-                       px[u] = load_any(x + at + u * step);
-                       pg[u] = load_any(gy + at + u * step);
-                     }
+    for (int u = 0; u < V; ++u) {
+      s1[u] += t1[u];
+      s2[u] += t2[u];
+    }
+  };
+    sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
+                     [&](long long at, long long step) {
+                       pack<T> px[U], pg[U];
 #pragma unroll
-                     for (int u = 0; u < U; ++u) add(px[u], pg[u]);
-                   },
-                   [&](long long at) { add(load_any(x + at), load_any(gy + at)); },
-                   [&](long long at, int u) {
-                     const float v = load1(x + at), g = load1(gy + at);
+                       for (int u = 0; u < U; ++u) {
+                         px[u] = load_any<STREAM>(x + at + u * step);
+                         pg[u] = load_any<STREAM>(gy + at + u * step);
+                       }
+                       float t1[V] = {}, t2[V] = {};
 #pragma unroll
-                     for (int w = 0; w < V; ++w)
-                       if (w == u) add1(w, v, g);
-                   });
+                       for (int u = 0; u < U; ++u) add(px[u], pg[u], t1, t2);
+                       flush(t1, t2);
+                     },
+                     [&](long long at) {
+                       float t1[V] = {}, t2[V] = {};
+                       add(load_any<STREAM>(x + at), load_any<STREAM>(gy + at), t1, t2);
+                       flush(t1, t2);
+                     },
+                     [&](long long at, int u) {
+                       const float v = load1(x + at), g = load1(gy + at);
+#pragma unroll
+                       for (int w = 0; w < V; ++w)
+                         if (w == u) add1(w, v, g);
+                     });
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     if ((int)threadIdx.x < active) {
@@ -665,68 +774,69 @@ __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, in
       for (int u = 0; u < V; ++u) lds[threadIdx.x * V + u] = half ? s2[u] : s1[u];
     }
     tree(lds, active * V / a.C, a.C);
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) part[2 * (((long long)b * a.C + c) * a.pieces + j) + half] = lds[c];
+    for (int c = threadIdx.x; c < a.C; c += blockDim.x)
+      part[2 * (((long long)b * a.C + c) * a.pieces + j) + half] = half ? lds[c] * rstd[(long long)b * a.G + c / a.D] : lds[c];
     __syncthreads();
   }
 }
 
-template <class T, int ACT>
+template <class T, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, unsigned mine, int active, const T* x, const T* gy,
                                                                     const float* gamma, const float* beta, const float* mean,
-                                                                    const float* rstd, const float2* m, const double2* part,
+                                                                    const float* rstd, const float2* m, const double2* part, int parts,
                                                                     float* ggamma, float* gbeta, int accumulate, T* gx) {
   constexpr int V = kVec<T>, U = 2;
   extern __shared__ double lds[];
   if (blockIdx.x >= mine)
-    return param_grads(a, part, (long long)(blockIdx.x - mine) * (blockDim.x >> 6) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+    return param_grads(a, parts, part, (long long)(blockIdx.x - mine) * (blockDim.x >> 6) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+  const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   float2* const own = reinterpret_cast<float2*>(lds);
   if (m == nullptr) {
-    const long long b0 = blockIdx.x / a.pieces * (long long)a.G;
+    const long long b0 = (long long)b * a.G;
     for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
       double s1 = 0.0, s2 = 0.0;
-      group_share(a, part, gamma, b0 + g, threadIdx.x & 63, 64, s1, s2);
+      group_share(a, parts, part, gamma, b0 + g, threadIdx.x & 63, 64, s1, s2);
       wave_sum2(s1, s2);
       if ((threadIdx.x & 63) == 0) own[g] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
     }
     __syncthreads();
   }
-  const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
-  const long long p0 = (long long)j * a.per, p1 = p0 + a.per < a.P ? p0 + a.per : a.P;
   const long long base = (long long)b * a.P * a.C;
   Slope k[V];
-  slopes_of<V>(a, b, gamma, beta, mean, rstd, k);
-  float2 mm[V];
+  Weights w[V];
 #pragma unroll
   for (int u = 0; u < V; ++u) {
-    const int g = (((int)threadIdx.x * V + u) % a.C) / a.D;
-    if (m == nullptr) mm[u] = own[g];
-    else mm[u] = m[(long long)b * a.G + g];
+    const int c = ((int)threadIdx.x * V + u) % a.C, g = c / a.D;
+    const float rs = rstd[(long long)b * a.G + g], ga = gamma ? gamma[c] : 1.f;
+    k[u] = slope_of<ACT>(mean[(long long)b * a.G + g], rs, ga, beta ? beta[c] : 0.f);
+    if (m == nullptr) w[u] = weights_of(rs, ga, own[g]);
+    else w[u] = weights_of(rs, ga, m[(long long)b * a.G + g]);
   }
   auto put = [&](long long at, pack<T> px, pack<T> pg) {
     float v[V], g[V];
     unpack(px, v);
     unpack(pg, g);
 #pragma unroll
-    for (int u = 0; u < V; ++u) v[u] = grad_of<ACT>(k[u], mm[u], v[u], g[u]);
-    store_any(gx + at, repack(v));
+    for (int u = 0; u < V; ++u) v[u] = grad_of<ACT>(k[u], w[u], v[u], g[u]);
+    store_any<STREAM>(gx + at, repack(v));
   };
-  sweep_last<V, U>(base + p0 * a.C, base + p1 * a.C, active,
+  sweep_last<V, U>(base, base + a.P * a.C, active, j, a.pieces, INT_MAX,
                    [&](long long at, long long step) {
                      pack<T> px[U], pg[U];
 #pragma unroll
                      for (int u = 0; u < U; ++u) {
-                       px[u] = load_any(x + at + u * step);
-                       pg[u] = load_any(gy + at + u * step);
+                       px[u] = load_any<STREAM>(x + at + u * step);
+                       pg[u] = load_any<STREAM>(gy + at + u * step);
                      }
 #pragma unroll
                      for (int u = 0; u < U; ++u) put(at + u * step, px[u], pg[u]);
                    },
-                   [&](long long at) { put(at, load_any(x + at), load_any(gy + at)); },
+                   [&](long long at) { put(at, load_any<STREAM>(x + at), load_any<STREAM>(gy + at)); },
                    [&](long long at, int u) {
                      const float v = load1(x + at), g = load1(gy + at);
 #pragma unroll
-                     for (int w = 0; w < V; ++w)
-                       if (w == u) store1(gx + at, grad_of<ACT>(k[w], mm[w], v, g));
+                     for (int q = 0; q < V; ++q)
+                       if (q == u) store1(gx + at, grad_of<ACT>(k[q], w[q], v, g));
                    });
 }
 
@@ -774,7 +884,7 @@ __device__ __forceinline__ void small_load(const NormArgs& a, const SmallArgs& s
     for (int k = 0; k < kSmallValues / V; ++k) {
       const int e = (k * (int)blockDim.x + (int)threadIdx.x) * V;
       q[k] = pack<T>{};
-      if (e + V <= s.n) q[k] = load_any(x + small_at<LAST>(a, s, b, g, e));
+      if (e + V <= s.n) q[k] = load_any<false>(x + small_at<LAST>(a, s, b, g, e));
     }
 #pragma unroll
     for (int k = 0; k < kSmallValues / V; ++k) {
@@ -808,7 +918,7 @@ __device__ __forceinline__ void small_store(const NormArgs& a, const SmallArgs& 
 #pragma unroll
       for (int u = 0; u < V; ++u) w[u] = v[k * V + u];
       if (e + V <= s.n) {
-        store_any(y + small_at<LAST>(a, s, b, g, e), repack(w));
+        store_any<false>(y + small_at<LAST>(a, s, b, g, e), repack(w));
       } else {
 #pragma unroll
         for (int u = 0; u < V; ++u)
@@ -872,13 +982,13 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
   double s1 = 0.0, s2 = 0.0;
   small_values<T>(s, [&](int k, int e) {                  // v: xh, w: gamma gz
     const float2 f = affine[small_channel<LAST>(a, s, e)];
-    float xh, gz;
-    terms<ACT>(Slope{mu, rs, f.x, f.y}, v[k], w[k], xh, gz);
-    v[k] = xh;
+    float d, gz;
+    terms<ACT>(slope_of<ACT>(mu, rs, f.x, f.y), v[k], w[k], d, gz);
+    v[k] = d * rs;
     w[k] = gz * f.x;
     s1 += w[k];
-    s2 = fma((double)w[k], (double)xh, s2);
-    if (params) product[e] = make_float2(gz, gz * xh);
+    s2 = fma((double)w[k], (double)v[k], s2);
+    if (params) product[e] = make_float2(gz, gz * v[k]);
   });
   block_sum2(s1, s2, red);
   if (gx != nullptr) {
@@ -915,46 +1025,24 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
 // ------------------------------------------------------------------------------------------
 // Launches
 // ------------------------------------------------------------------------------------------
-constexpr long long kNormBlocks = 4096;       // blocks that a sweep is cut into: 16 a CU
-constexpr long long kLeastPiece = 8192;       // values
+constexpr long long kSumBlocks = 4096;        // blocks of a launch that only reads: 16 a CU; channels last, half as many
+constexpr long long kTileBytes = 16384;       // of a whole tile of 256 threads that read one field
+constexpr long long kApplyBlocks = 1 << 22;   // of one that writes: a tile each, but for the very largest fields; channels last,
+constexpr long long kApplyLast = 8192;        // where a thread first has its channels' factors to work out, so many
 constexpr long long kShortRow = 2048;         // rows below this go wave by wave
 
 NormArgs norm_args(const NormShape& n) {
   const int D = n.C / n.G;
   const double count = (double)n.P * D;
-  return NormArgs{n.B, n.C, n.G, D, (long long)n.P, count > 0 ? 1.0 / count : 0.0, n.eps, 1, 0};
+  return NormArgs{n.B, n.C, n.G, D, (long long)n.P, count > 0 ? 1.0 / count : 0.0, n.eps, 1, 1};
 }
 
-// Cuts each of `ranges` ranges of `length` into pieces of a multiple of `unit`.
-void cut(NormArgs& a, long long ranges, long long length, long long unit, long long least) {
-  long long pieces = (kNormBlocks + ranges - 1) / ranges;
-  const long long most = length / least;
-  if (pieces > most) pieces = most;
-  if (pieces < 1) pieces = 1;
-  long long per = (length + pieces - 1) / pieces;
-  per = (per + unit - 1) / unit * unit;
-  if (per < unit) per = unit;
-  pieces = (length + per - 1) / per;
-  a.pieces = (int)(pieces < 1 ? 1 : pieces);
-  a.per = per;
-}
-NormArgs cut_groups(const NormShape& n) {              // channels first, statistics
-  NormArgs a = norm_args(n);
-  cut(a, (long long)n.B * n.G, a.P * a.D, 8, kLeastPiece);
-  return a;
-}
-NormArgs cut_rows(const NormShape& n) {                // channels first, where channels count
-  NormArgs a = norm_args(n);
-  if (n.P < kShortRow) { a.pieces = 1; a.per = n.P; }
-  else cut(a, (long long)n.B * n.C, n.P, 8, kLeastPiece);
-  return a;
-}
-NormArgs cut_points(const NormShape& n) {              // channels last: pieces of at least 64 points, whose sums (16 bytes a
-  NormArgs a = norm_args(n);                           // channel) are then little beside them
-  const long long least = kLeastPiece / n.C > 64 ? kLeastPiece / n.C : 64;
-  cut(a, n.B, n.P, 1, least);
-  return a;
-}
+// Fields that the memory-side cache does not hold together are read and written with the nontemporal hint: the sums' launch
+// 88 us without and 135 with the outputs of an earlier call that the cache still has to write back (60 x 60 x 64 x 30, 20
+// channels).  Reading the second time from that cache, groups that fit it one after the other or backwards from where the sums
+// ended, gained nothing: it gives 7 to 7.7 TB/s, the memory behind it 6.2.
+bool streams(const NormShape& n, int fields) { return n.P * n.C * n.B * (n.bf16 ? 2 : 4) * (fields + 1) > kStreamBytes; }
+
 // Threads of the channels-last kernels that take part: a multiple of what makes a step whole points.
 int active_threads(int C, int V) {
   int g = C, h = V;
@@ -963,9 +1051,41 @@ int active_threads(int C, int V) {
   return unit <= kThreads ? kThreads / unit * unit : unit;
 }
 
+// Deals the `tiles` tiles of each of `ranges` ranges to blocks, about `blocks` in all.
+void deal(NormArgs& a, long long ranges, long long tiles, long long blocks) {
+  long long p = (blocks + ranges - 1) / ranges;
+  if (p > tiles) p = tiles;
+  if (p < 1) p = 1;
+  a.run = (int)((tiles + p - 1) / p);
+  a.pieces = (int)(a.run > 0 ? (tiles + a.run - 1) / a.run : 1);
+}
+// values of a whole tile where `fields` fields are read
+long long tile_values(const NormShape& n, int fields) { return kTileBytes / fields / (n.bf16 ? 2 : 4); }
+NormArgs cut_groups(const NormShape& n) {              // channels first, statistics
+  NormArgs a = norm_args(n);
+  const long long tile = tile_values(n, 1);
+  deal(a, (long long)n.B * n.G, (a.P * a.D + tile - 1) / tile, kSumBlocks);
+  return a;
+}
+NormArgs cut_rows(const NormShape& n, int fields, long long blocks) {  // channels first, where channels count
+  NormArgs a = norm_args(n);
+  const long long tile = tile_values(n, fields);
+  if (n.P >= kShortRow) deal(a, (long long)n.B * n.C, (n.P + tile - 1) / tile, blocks);
+  return a;
+}
+// Channels last: blocks of at least 64 points, whose sums (16 bytes a channel) are then little beside them.
+NormArgs cut_points(const NormShape& n, int fields, long long blocks) {
+  NormArgs a = norm_args(n);
+  const long long tile = (long long)active_threads(n.C, n.bf16 ? 8 : 4) * (n.bf16 ? 8 : 4) * (fields == 1 ? 4 : 2);
+  const long long tiles = (n.P * n.C + tile - 1) / tile, most = n.B * (n.P / 64 + 1);
+  deal(a, n.B, tiles, blocks < most ? blocks : most);
+  return a;
+}
+
 // scratch: sums of pieces, statistics or means
 size_t norm_part_bytes(const NormShape& n) {
-  const NormArgs f = n.last ? cut_points(n) : cut_groups(n), b = n.last ? f : cut_rows(n);
+  const NormArgs f = n.last ? cut_points(n, 1, kSumBlocks / 2) : cut_groups(n);
+  const NormArgs b = n.last ? cut_points(n, 2, kSumBlocks / 2) : cut_rows(n, 2, kSumBlocks);
   const size_t fwd = (size_t)n.B * n.G * f.pieces, bwd = (size_t)n.B * n.C * b.pieces;
   return ((fwd > bwd ? fwd : bwd) * sizeof(double2) + 255) & ~size_t(255);
 }
@@ -975,8 +1095,8 @@ unsigned row_blocks(const NormArgs& a, bool short_rows) {
   return (unsigned)(short_rows ? (rows + kThreads / 64 - 1) / (kThreads / 64) : rows * a.pieces);
 }
 
-// Sums of pieces that every block of the next launch adds itself (16 or 32 KB from the L2 a block), sparing a launch
-constexpr long long kInlineParts = 1024;
+// Sums of pieces that every block of the next launch adds itself (8 KB from the L2 a block at most), sparing a launch
+constexpr long long kInlineParts = 512;
 
 bool small_fits(const NormShape& n, int most) { return n.P > 0 && n.P <= most && n.P * (n.C / n.G) <= most; }
 SmallArgs small_args(const NormShape& n, int V) {
@@ -990,41 +1110,56 @@ int small_threads(int n) {
   return (t + 63) / 64 * 64;
 }
 
+// f(std::integral_constant<bool, b>()...)
+template <class F>
+void with(bool b, F&& f) {
+  if (b) f(std::true_type());
+  else f(std::false_type());
+}
+
 template <class T, int ACT>
 hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* beta, T* y, float* mean, float* rstd,
                void* ws, hipStream_t s) {
   double2* part = static_cast<double2*>(ws);
   Stat* stat = reinterpret_cast<Stat*>(static_cast<char*>(ws) + norm_part_bytes(n));
-  const int bg = n.B * n.G;
   if (small_fits(n, kSmallFwd)) {
     const NormArgs a = norm_args(n);
     const SmallArgs k = small_args(n, kVec<T>);
-    if (n.last) hipLaunchKernelGGL((norm_small_kernel<T, ACT, true>), dim3(bg), dim3(small_threads(k.n)), 0, s, a, k, x, gamma, beta, y, mean, rstd);
-    else hipLaunchKernelGGL((norm_small_kernel<T, ACT, false>), dim3(bg), dim3(small_threads(k.n)), 0, s, a, k, x, gamma, beta, y, mean, rstd);
+    with(n.last, [&](auto last) {
+      hipLaunchKernelGGL((norm_small_kernel<T, ACT, decltype(last)::value>), dim3(n.B * n.G), dim3(small_threads(k.n)), 0, s, a, k, x,
+                         gamma, beta, y, mean, rstd);
+    });
     return hipGetLastError();
   }
+  const bool hint = streams(n, 1);
   if (n.last) {
-    const NormArgs a = cut_points(n);
+    const NormArgs a = cut_points(n, 1, kSumBlocks / 2), out = cut_points(n, 1, kApplyLast);
     const int active = active_threads(n.C, kVec<T>), threads = (active + 63) / 64 * 64;
     const bool inside = (long long)n.G * a.pieces <= kInlineParts && n.P > 0;
-    hipLaunchKernelGGL((norm_last_sum_kernel<T>), dim3((unsigned)(n.B * a.pieces)), dim3(threads),
-                       (size_t)active * kVec<T> * sizeof(double), s, a, active, x, reinterpret_cast<double*>(part), stat);
-    if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(bg), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
-    if (n.P > 0)
-      hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT>), dim3((unsigned)(n.B * a.pieces)), dim3(threads),
-                         inside ? n.G * sizeof(Stat) : 0, s, a, active, x, gamma, beta, stat, inside ? part : nullptr, mean, rstd, y);
+    const dim3 grid((unsigned)(n.B * a.pieces));
+    with(hint, [&](auto stream) {
+      constexpr bool S = decltype(stream)::value;
+      hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a, active, x,
+                         reinterpret_cast<double*>(part), stat);
+      if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
+      if (n.P > 0)
+        hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT, S>), dim3((unsigned)(n.B * out.pieces)), dim3(threads),
+                           inside ? n.G * sizeof(Stat) : 0, s, out, active, x, gamma, beta, stat, inside ? part : nullptr, a.pieces, mean,
+                           rstd, y);
+    });
     return hipGetLastError();
   }
-  const NormArgs a = cut_groups(n), r = cut_rows(n);
-  const bool short_rows = n.P < kShortRow, inside = !short_rows && a.pieces <= kInlineParts / 4;
-  hipLaunchKernelGGL((norm_sum_kernel<T>), dim3((unsigned)(bg * a.pieces)), dim3(kThreads), 0, s, a, x, part, stat);
-  if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(bg), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
-  if (short_rows)
-    hipLaunchKernelGGL((norm_apply_kernel<T, ACT, true>), dim3(row_blocks(r, true)), dim3(kThreads), 0, s, r, x, gamma, beta, stat,
-                       nullptr, 0, mean, rstd, y);
-  else
-    hipLaunchKernelGGL((norm_apply_kernel<T, ACT, false>), dim3(row_blocks(r, false)), dim3(kThreads), 0, s, r, x, gamma, beta, stat,
-                       inside ? part : nullptr, a.pieces, mean, rstd, y);
+  const NormArgs a = cut_groups(n), rows = cut_rows(n, 1, kApplyBlocks);
+  const bool short_rows = n.P < kShortRow, inside = !short_rows && a.pieces <= kInlineParts / 2;
+  with(hint, [&](auto stream) {
+    constexpr bool S = decltype(stream)::value;
+    hipLaunchKernelGGL((norm_sum_kernel<T, S>), dim3((unsigned)(n.B * n.G * a.pieces)), dim3(kThreads), 0, s, a, x, part, stat);
+    if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
+    with(short_rows, [&](auto short_) {
+      hipLaunchKernelGGL((norm_apply_kernel<T, ACT, decltype(short_)::value, S>), dim3(row_blocks(rows, short_rows)), dim3(kThreads), 0, s,
+                         rows, x, gamma, beta, stat, inside ? part : nullptr, a.pieces, mean, rstd, y);
+    });
+  });
   return hipGetLastError();
 }
 
@@ -1040,47 +1175,51 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
     int lanes = 1;
     while (lanes < 64 && lanes < n.P) lanes *= 2;
     const bool later = params && n.B > 1;
-    const size_t lds = params ? k.n * sizeof(float2) : 0;
-    auto launch = [&](auto last) {
-      hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.B * n.G), dim3(small_threads(k.n)), lds, s, a, k,
-                         lanes, x, gy, gamma, beta, mean, rstd, gx, later ? part : nullptr, ggamma, gbeta, accumulate);
-    };
-    if (n.last) launch(std::true_type());
-    else launch(std::false_type());
+    with(n.last, [&](auto last) {
+      hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.B * n.G), dim3(small_threads(k.n)),
+                         params ? k.n * sizeof(float2) : 0, s, a, k, lanes, x, gy, gamma, beta, mean, rstd, gx, later ? part : nullptr,
+                         ggamma, gbeta, accumulate);
+    });
     if (later)
       hipLaunchKernelGGL(norm_grad_fold_kernel, dim3((n.C + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s, a, 0u, part, gamma,
                          m, ggamma, gbeta, accumulate);
     return hipGetLastError();
   }
-  const bool short_rows = !n.last && n.P < kShortRow;
-  const NormArgs a = n.last ? cut_points(n) : cut_rows(n);
+  const bool short_rows = !n.last && n.P < kShortRow, writes = gx != nullptr && n.P > 0;
+  const NormArgs a = n.last ? cut_points(n, 2, kSumBlocks / 2) : cut_rows(n, 2, kSumBlocks);
+  const NormArgs out = n.last ? cut_points(n, 2, kApplyLast) : cut_rows(n, 2, kApplyBlocks);
   const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
-  const unsigned blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
-  const unsigned channel_blocks = (unsigned)((n.C + threads / 64 - 1) / (threads / 64));
-  if (n.last)
-    hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT>), dim3(blocks), dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a,
-                       active, x, gy, gamma, beta, mean, rstd, reinterpret_cast<double*>(part));
-  else if (short_rows)
-    hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, true>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd, part);
-  else
-    hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, false>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd, part);
-  const bool writes = gx != nullptr && n.P > 0;
   const bool inside = writes && !short_rows && (long long)(n.last ? n.C : n.C / n.G) * a.pieces <= kInlineParts;
-  if (!inside)
-    hipLaunchKernelGGL(norm_grad_fold_kernel, dim3((unsigned)(n.B * n.G) + (n.C + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s,
-                       a, (unsigned)(n.B * n.G), part, gamma, m, ggamma, gbeta, accumulate);
-  if (!writes) return hipGetLastError();
-  const dim3 grid(blocks + (inside && params ? channel_blocks : 0));
+  const unsigned channel_blocks = params ? (unsigned)((n.C + threads / 64 - 1) / (threads / 64)) : 0;
+  const unsigned groups = (unsigned)(n.B * n.G), blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
+  const unsigned own = n.last ? (unsigned)(n.B * out.pieces) : row_blocks(out, short_rows);
+  const dim3 grid(own + (inside ? channel_blocks : 0));
   const float2* means = inside ? nullptr : m;
-  if (n.last)
-    hipLaunchKernelGGL((norm_last_grad_apply_kernel<T, ACT>), grid, dim3(threads), inside ? n.G * sizeof(float2) : 0, s, a, blocks, active,
-                       x, gy, gamma, beta, mean, rstd, means, part, ggamma, gbeta, accumulate, gx);
-  else if (short_rows)
-    hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, true>), grid, dim3(kThreads), 0, s, a, blocks, x, gy, gamma, beta, mean, rstd, means,
-                       part, ggamma, gbeta, accumulate, gx);
-  else
-    hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, false>), grid, dim3(kThreads), 0, s, a, blocks, x, gy, gamma, beta, mean, rstd, means,
-                       part, ggamma, gbeta, accumulate, gx);
+  auto fold = [&] {
+    if (!inside)
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? (n.C + kThreads / 64 - 1) / (kThreads / 64) : 0)), dim3(kThreads), 0, s,
+                         a, groups, part, gamma, m, ggamma, gbeta, accumulate);
+  };
+  with(streams(n, 2), [&](auto stream) {
+    constexpr bool S = decltype(stream)::value;
+    if (n.last) {
+      hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT, S>), dim3(blocks), dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a,
+                         active, x, gy, gamma, beta, mean, rstd, reinterpret_cast<double*>(part));
+      fold();
+      if (writes)
+        hipLaunchKernelGGL((norm_last_grad_apply_kernel<T, ACT, S>), grid, dim3(threads), inside ? n.G * sizeof(float2) : 0, s, out, own,
+                           active, x, gy, gamma, beta, mean, rstd, means, part, a.pieces, ggamma, gbeta, accumulate, gx);
+      return;
+    }
+    with(short_rows, [&](auto short_) {
+      constexpr bool R = decltype(short_)::value;
+      hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, R, S>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd, part);
+      fold();
+      if (writes)
+        hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, R, S>), grid, dim3(kThreads), 0, s, out, own, x, gy, gamma, beta, mean, rstd,
+                           means, part, a.pieces, ggamma, gbeta, accumulate, gx);
+    });
+  });
   return hipGetLastError();
 }
 

@@ -297,6 +297,16 @@ def test_replays_of_a_graph_have_the_bits_of_eager_calls(p):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("b,c,groups,p,layout", [(1, 10, 5, 5000011, "first"), (5, 10, 2, 1000003, "last"), (1, 3, 1, 16000001, "last")])
+def test_fields_larger_than_the_caches(b, c, groups, p, layout):
+    """200 MB: taken in shares of groups or batch entries, the last share smaller, or in one that is read backwards."""
+    n = Norm(b, c, groups, p, layout, act="silu")
+    y, mean, rstd = n.forward()
+    n.check_forward(y, mean, rstd)
+    n.check_backward(mean, rstd, *n.backward(mean, rstd))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["first", "last"])
 def test_offsets_past_32_bits(layout):
     """Two channels of 2^31 + 20 bf16 points: the values repeat, so that the statistics are known; groups of one channel."""
@@ -329,10 +339,6 @@ def test_offsets_past_32_bits(layout):
     scale = np.abs(small[0]).sum(1) * blocks
     assert np.all(np.abs(gg.cpu().numpy() - g["ggamma"] * blocks) <= 1e-5 * scale)
     assert np.all(np.abs(gb.cpu().numpy() - g["gbeta"] * blocks) <= 1e-5 * scale)
-
-
-def _refused(fn, desc, *args):
-    return fn(ctypes.byref(desc) if desc is not None else None, *args)
 
 
 def test_refusals_without_a_device():
