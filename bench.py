@@ -33,6 +33,11 @@ def parse():
     ap.add_argument("--network", action="store_true",
                     help="time one training step of the whole network of the workload (cfg3: lift, blocks, "
                          "projection, relative L2 loss, backward, Adam) instead of one block")
+    ap.add_argument("--group-norm", type=int, default=0, metavar="GROUPS",
+                    help="with --network: blocks without an activation, each followed by a group norm with GELU")
+    ap.add_argument("--optimizer", choices=("adam", "adamw", "adamw8"), default="adam",
+                    help="with --network: Adam tensor by tensor, or AdamW over all tensors with clipping by the norm of all "
+                         "gradients, moments in 32 or in 8 bits")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="only run plain device copies of 4 GiB (reference reading for rocprofv3 --pmc "
                          "FETCH_SIZE / WRITE_SIZE), then exit")
@@ -158,10 +163,27 @@ def network_step_bench(args, torch, B, synth):
                       dtype=torch.float32, device="cuda")
     loss = torch.empty(1, device="cuda")
     params = [lw, lb, w1, b1, w2, b2] + [t for blk in blocks for t in blk]
+    groups = args.group_norm
+    if groups:                                 # the norms' parameters and what they keep for the backward pass
+        bare = B.make_desc(batch, width, width, grid, modes, 0, B.FNO_ACT_IDENTITY)
+        ndesc = B.make_norm_desc(batch, width, groups, npts, activation=B.FNO_ACT_GELU)
+        nws = B.alloc_norm_workspace(ndesc)
+        affine = [(1 + 0.1 * rn(width), 0.1 * rn(width)) for _ in range(nblocks)]
+        stats = [(torch.empty(batch, groups, device="cuda"), torch.empty(batch, groups, device="cuda"))
+                 for _ in range(nblocks)]
+        params += [t for pair in affine for t in pair]
     flat = [torch.view_as_real(p).reshape(-1) if p.is_complex() else p.reshape(-1) for p in params]
     grads = [torch.empty_like(p) for p in params]
     gflat = [torch.view_as_real(t).reshape(-1) if t.is_complex() else t.reshape(-1) for t in grads]
-    moms = [(torch.zeros_like(f), torch.zeros_like(f)) for f in flat]
+    if args.optimizer == "adam":
+        moms = [(torch.zeros_like(f), torch.zeros_like(f)) for f in flat]
+    else:
+        kind = torch.uint8 if args.optimizer == "adamw8" else torch.float32
+        mom, sq = ([torch.zeros(f.numel(), dtype=kind, device="cuda") for f in flat] for _ in range(2))
+        exps = [torch.zeros(B.adamw_exps_shape(f.numel()), dtype=torch.uint8, device="cuda") for f in flat]
+        tensors = B.make_adamw_tensors(flat, gflat, mom, sq, exps if args.optimizer == "adamw8" else None,
+                                       [0.01 if p.dim() > 1 else 0.0 for p in params])
+        gnorm, gws = torch.empty(1, device="cuda"), B.alloc_grad_norm_workspace(tensors)
     glw, glb, gw1, gb1, gw2, gb2 = grads[:6]
     gblk = [tuple(grads[6 + 3 * k: 9 + 3 * k]) for k in range(nblocks)]
     state = {"step": 0}
@@ -169,7 +191,12 @@ def network_step_bench(args, torch, B, synth):
     def forward():
         B.fno_pointwise_linear(batch, c_in, width, npts, a, lw, lb, vs[0])
         for k, (R, W, b) in enumerate(blocks):
-            B.fno_block_fwd(desc, vs[k & 1], R, W, b, vs[(k + 1) & 1], None, None, ws)
+            v, out = vs[k & 1], vs[(k + 1) & 1]
+            if groups:
+                B.fno_block_fwd(bare, v, R, W, b, out, None, None, ws)
+                B.fno_group_norm_fwd(ndesc, out, *affine[k], out, None, None, nws)
+            else:
+                B.fno_block_fwd(desc, v, R, W, b, out, None, None, ws)
         B.fno_pointwise_mlp2(batch, width, hidden, 1, npts, vs[nblocks & 1], w1, b1, w2, b2, u)
 
     def step():
@@ -178,16 +205,28 @@ def network_step_bench(args, torch, B, synth):
         state["step"] += 1
         B.fno_pointwise_linear(batch, c_in, width, npts, a, lw, lb, vs[0])
         for k, (R, W, b) in enumerate(blocks):
-            B.fno_block_fwd(desc, vs[k], R, W, b, vs[k + 1], zs[k], xhs[k], ws)
+            if groups:
+                B.fno_block_fwd(bare, vs[k], R, W, b, zs[k], None, xhs[k], ws)
+                B.fno_group_norm_fwd(ndesc, zs[k], *affine[k], vs[k + 1], *stats[k], nws)
+            else:
+                B.fno_block_fwd(desc, vs[k], R, W, b, vs[k + 1], zs[k], xhs[k], ws)
         B.fno_pointwise_mlp2(batch, width, hidden, 1, npts, vs[-1], w1, b1, w2, b2, u)
         B.fno_rel_l2_loss(u.numel(), u, y, loss, gu, lws)
         B.fno_pointwise_mlp2_bwd(batch, width, hidden, 1, npts, vs[-1], w1, b1, w2, gu, gva, gw1, gb1, gw2, gb2, pws)
         gin, gout = gva, gvb
         for k in reversed(range(nblocks)):
             R, W, b = blocks[k]
-            B.fno_block_bwd(desc, vs[k], R, W, zs[k], xhs[k], gin, gout, gblk[k][0], gblk[k][1], gblk[k][2], ws)
+            if groups:
+                at = 6 + 3 * nblocks + 2 * k
+                B.fno_group_norm_bwd(ndesc, zs[k], *affine[k], *stats[k], gin, gin, grads[at], grads[at + 1], nws)
+            B.fno_block_bwd(bare if groups else desc, vs[k], R, W, zs[k], xhs[k], gin, gout, gblk[k][0], gblk[k][1],
+                            gblk[k][2], ws)
             gin, gout = gout, gin
         B.fno_pointwise_linear_bwd(batch, c_in, width, npts, a, lw, gin, None, glw, glb, pws)
+        if args.optimizer != "adam":
+            B.fno_grad_norm(tensors, gnorm, gws)
+            B.fno_adamw_step(tensors, 1e-3, 0.9, 0.999, 1e-8, state["step"], grad_norm=gnorm, max_norm=1.0, seed=0)
+            return
         for f, gf, (m, v) in zip(flat, gflat, moms):
             B.fno_adam_step(f.numel(), f, gf, m, v, 1e-3, 0.9, 0.999, 1e-8, state["step"])
 
@@ -200,6 +239,8 @@ def network_step_bench(args, torch, B, synth):
     torch.cuda.synchronize()
     ms = 1e3 * (time.perf_counter() - t0) / args.steps
     pc = float(batch) * width * npts
+    step_text = {"adam": "Adam", "adamw": "AdamW with clipping", "adamw8": "AdamW with clipping, moments in 8 bits"}
+    norm_text = f", group norm of {groups} groups behind every block" if groups else ""
     print(json.dumps({
         "metric": "FNO spectral layer Gpoint-channels/s + achieved HBM GB/s on 1 MI355X",
         "value": nblocks * pc / (ms * 1e-3) / 1e9, "unit": "Gpoint-channels/s", "n_gpus": 1, "steps": args.steps,
@@ -207,7 +248,8 @@ def network_step_bench(args, torch, B, synth):
         "vs_baseline": None, "dtype": "f32", "data": "synthetic",
         "config": {"workload": f"{args.config} network {'forward' if args.forward_only else 'training step'}: lift "
                                f"{c_in}->{width}, {nblocks} blocks, projection {width}->{hidden}->1"
-                               f"{'' if args.forward_only else ', relative L2 loss, backward, Adam'}; batch {batch}, grid "
+                               f"{norm_text}{'' if args.forward_only else ', relative L2 loss, backward, ' + step_text[args.optimizer]}"
+                               f"; batch {batch}, grid "
                                f"{grid[0]}x{grid[1]}x{grid[2]}x{grid[3]}; value counts the point-channels of the "
                                f"{nblocks} blocks once per step",
                    "global_batch": batch, "parallelism": "single GPU"},
