@@ -544,49 +544,74 @@ __device__ __forceinline__ void sweep_last(long long begin, long long end, int a
   }
 }
 
-// lds[e], e < rows * C: sums over the rows, and then over the channels of every group where D > 1, left in lds[g * D].
-__device__ __forceinline__ void tree(double* lds, int rows, int width) {
-  while (rows > 1) {
-    const int h = (rows + 1) >> 1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < (rows - h) * width; i += blockDim.x) lds[i] += lds[i + h * width];
-    rows = h;
+// Adds the pairs of a block's threads by channel: lds[r C + c], r < rows, as every active thread left its V behind those of the
+// thread before.  First k threads for every channel, then their k sums in turn or, where they are many, as a tree.  Returns
+// where the C sums are, in front of every thread.
+__device__ __forceinline__ double2* channel_sums(double2* lds, int rows, int C) {
+  double2* const sums = lds + rows * C;
+  int k = (int)blockDim.x / C;
+  if (k < 1) k = 1;
+  if (k > rows) k = rows;
+  __syncthreads();
+  for (int t = threadIdx.x; t < C * k; t += blockDim.x) {
+    const int c = t % C;
+    double2 s = make_double2(0.0, 0.0);
+    for (int r = t / C; r < rows; r += k) {
+      s.x += lds[r * C + c].x;
+      s.y += lds[r * C + c].y;
+    }
+    sums[t] = s;
   }
   __syncthreads();
-}
-__device__ __forceinline__ void tree_groups(double* lds, int G, int D) {
-  int n = D;
-  while (n > 1) {
-    const int h = (n + 1) >> 1;
-    for (int i = threadIdx.x; i < G * (n - h); i += blockDim.x) {
-      const int g = i / (n - h), d = i % (n - h);
-      lds[g * D + d] += lds[g * D + d + h];
+  while (k > 16) {
+    const int h = (k + 1) >> 1;
+    for (int t = threadIdx.x; t < (k - h) * C; t += blockDim.x) {
+      sums[t].x += sums[t + h * C].x;
+      sums[t].y += sums[t + h * C].y;
     }
-    n = h;
+    k = h;
     __syncthreads();
   }
+  if (k > 1) {
+    for (int c = threadIdx.x; c < C; c += blockDim.x) {
+      double2 s = sums[c];
+      for (int r = 1; r < k; ++r) {
+        s.x += sums[r * C + c].x;
+        s.y += sums[r * C + c].y;
+      }
+      sums[c] = s;
+    }
+    __syncthreads();
+  }
+  return sums;
 }
 
 // part[(b, g)][piece] = (sum d, sum d^2); stat[(b, g)].hi = k
 template <class T, bool STREAM>
-__global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int active, const T* x, double* part, Stat* stat) {
+__global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int active, const T* x, double2* part, Stat* stat) {
   constexpr int V = kVec<T>, U = 4;
-  extern __shared__ double lds[];
+  extern __shared__ double2 pairs[];
+  __shared__ float middles[kMaxNormChannels];
   const int b = (int)blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   const long long base = (long long)b * a.P * a.C;
   double s[V], q[V];
   float middle[V];
+  for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
+    middles[g] = middle_of<T, true>(a, x, b, g);
+    if (j == 0) stat[(long long)b * a.G + g].hi = middles[g];
+  }
+  __syncthreads();
 #pragma unroll
   for (int u = 0; u < V; ++u) {
     s[u] = q[u] = 0.0;
-    middle[u] = middle_of<T, true>(a, x, b, ((int)threadIdx.x * V + u) % a.C / a.D);
+    middle[u] = middles[((int)threadIdx.x * V + u) % a.C / a.D];
   }
   auto add1 = [&](int u, float v) {
     const double d = v - middle[u];
     s[u] += d;
     q[u] = fma(d, d, q[u]);
   };
-    sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
+  sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
                      [&](long long at, long long step) {
                        pack<T> k[U];
 #pragma unroll
@@ -623,20 +648,32 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
                        for (int w = 0; w < V; ++w)
                          if (w == u) add1(w, v);
                      });
+  if ((int)threadIdx.x < active) {
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    if ((int)threadIdx.x < active) {
-#pragma unroll
-      for (int u = 0; u < V; ++u) lds[threadIdx.x * V + u] = half ? q[u] : s[u];
-    }
-    tree(lds, active * V / a.C, a.C);
-    tree_groups(lds, a.G, a.D);
-    for (int g = threadIdx.x; g < a.G; g += blockDim.x)
-      part[2 * (((long long)b * a.G + g) * a.pieces + j) + half] = lds[g * a.D];
-    __syncthreads();
+    for (int u = 0; u < V; ++u) pairs[threadIdx.x * V + u] = make_double2(s[u], q[u]);
   }
-  if (j == 0)
-    for (int g = threadIdx.x; g < a.G; g += blockDim.x) stat[(long long)b * a.G + g].hi = middle_of<T, true>(a, x, b, g);
+  const double2* const sums = channel_sums(pairs, active * V / a.C, a.C);
+  double2* const to = part + (long long)b * a.G * a.pieces + j;
+  if (a.D <= 32) {
+    for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
+      double2 m = sums[g * a.D];
+      for (int d = 1; d < a.D; ++d) {
+        m.x += sums[g * a.D + d].x;
+        m.y += sums[g * a.D + d].y;
+      }
+      to[(long long)g * a.pieces] = m;
+    }
+  } else {
+    for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
+      double2 m = make_double2(0.0, 0.0);
+      for (int d = threadIdx.x & 63; d < a.D; d += 64) {
+        m.x += sums[g * a.D + d].x;
+        m.y += sums[g * a.D + d].y;
+      }
+      wave_sum2(m.x, m.y);
+      if ((threadIdx.x & 63) == 0) to[(long long)g * a.pieces] = m;
+    }
+  }
 }
 
 // part: the sums of the batch entry's pieces, few enough for every block to add them itself, a group a wave (null: the
@@ -704,9 +741,9 @@ __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int a
 template <class T, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, int active, const T* x, const T* gy,
                                                                   const float* gamma, const float* beta, const float* mean,
-                                                                  const float* rstd, double* part) {
+                                                                  const float* rstd, double2* part) {
   constexpr int V = kVec<T>, U = 2;
-  extern __shared__ double lds[];
+  extern __shared__ double2 pairs[];
   const int b = (int)blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   const long long base = (long long)b * a.P * a.C;
   Slope k[V];
@@ -743,7 +780,7 @@ __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, in
       s2[u] += t2[u];
     }
   };
-    sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
+  sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
                      [&](long long at, long long step) {
                        pack<T> px[U], pg[U];
 #pragma unroll
@@ -767,17 +804,13 @@ __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, in
                        for (int w = 0; w < V; ++w)
                          if (w == u) add1(w, v, g);
                      });
+  if ((int)threadIdx.x < active) {
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    if ((int)threadIdx.x < active) {
-#pragma unroll
-      for (int u = 0; u < V; ++u) lds[threadIdx.x * V + u] = half ? s2[u] : s1[u];
-    }
-    tree(lds, active * V / a.C, a.C);
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x)
-      part[2 * (((long long)b * a.C + c) * a.pieces + j) + half] = half ? lds[c] * rstd[(long long)b * a.G + c / a.D] : lds[c];
-    __syncthreads();
+    for (int u = 0; u < V; ++u) pairs[threadIdx.x * V + u] = make_double2(s1[u], s2[u]);
   }
+  const double2* const sums = channel_sums(pairs, active * V / a.C, a.C);
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x)
+    part[((long long)b * a.C + c) * a.pieces + j] = make_double2(sums[c].x, sums[c].y * rstd[(long long)b * a.G + c / a.D]);
 }
 
 template <class T, int ACT, bool STREAM>
@@ -1028,6 +1061,7 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
 constexpr long long kSumBlocks = 4096;        // blocks of a launch that only reads: 16 a CU; channels last, half as many
 constexpr long long kTileBytes = 16384;       // of a whole tile of 256 threads that read one field
 constexpr long long kApplyBlocks = 1 << 22;   // of one that writes: a tile each, but for the very largest fields; channels last,
+constexpr long long kApplyInside = 2048;      // where every block first adds the sums of pieces
 constexpr long long kApplyLast = 8192;        // where a thread first has its channels' factors to work out, so many
 constexpr long long kShortRow = 2048;         // rows below this go wave by wave
 
@@ -1080,6 +1114,11 @@ NormArgs cut_points(const NormShape& n, int fields, long long blocks) {
   const long long tiles = (n.P * n.C + tile - 1) / tile, most = n.B * (n.P / 64 + 1);
   deal(a, n.B, tiles, blocks < most ? blocks : most);
   return a;
+}
+
+// LDS of the channels-last sums: a pair for every value of the active threads, one more for every thread or channel
+size_t pair_bytes(const NormShape& n, int active, int threads) {
+  return ((size_t)active * (n.bf16 ? 8 : 4) + (threads > n.C ? threads : n.C)) * sizeof(double2);
 }
 
 // scratch: sums of pieces, statistics or means
@@ -1139,8 +1178,7 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     const dim3 grid((unsigned)(n.B * a.pieces));
     with(hint, [&](auto stream) {
       constexpr bool S = decltype(stream)::value;
-      hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a, active, x,
-                         reinterpret_cast<double*>(part), stat);
+      hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), pair_bytes(n, active, threads), s, a, active, x, part, stat);
       if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
       if (n.P > 0)
         hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT, S>), dim3((unsigned)(n.B * out.pieces)), dim3(threads),
@@ -1149,8 +1187,9 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     });
     return hipGetLastError();
   }
-  const NormArgs a = cut_groups(n), rows = cut_rows(n, 1, kApplyBlocks);
+  const NormArgs a = cut_groups(n);
   const bool short_rows = n.P < kShortRow, inside = !short_rows && a.pieces <= kInlineParts / 2;
+  const NormArgs rows = cut_rows(n, 1, inside ? kApplyInside : kApplyBlocks);
   with(hint, [&](auto stream) {
     constexpr bool S = decltype(stream)::value;
     hipLaunchKernelGGL((norm_sum_kernel<T, S>), dim3((unsigned)(n.B * n.G * a.pieces)), dim3(kThreads), 0, s, a, x, part, stat);
@@ -1187,9 +1226,9 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   }
   const bool short_rows = !n.last && n.P < kShortRow, writes = gx != nullptr && n.P > 0;
   const NormArgs a = n.last ? cut_points(n, 2, kSumBlocks / 2) : cut_rows(n, 2, kSumBlocks);
-  const NormArgs out = n.last ? cut_points(n, 2, kApplyLast) : cut_rows(n, 2, kApplyBlocks);
-  const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
+    const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
   const bool inside = writes && !short_rows && (long long)(n.last ? n.C : n.C / n.G) * a.pieces <= kInlineParts;
+  const NormArgs out = n.last ? cut_points(n, 2, kApplyLast) : cut_rows(n, 2, inside ? kApplyInside : kApplyBlocks);
   const unsigned channel_blocks = params ? (unsigned)((n.C + threads / 64 - 1) / (threads / 64)) : 0;
   const unsigned groups = (unsigned)(n.B * n.G), blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
   const unsigned own = n.last ? (unsigned)(n.B * out.pieces) : row_blocks(out, short_rows);
@@ -1203,8 +1242,8 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   with(streams(n, 2), [&](auto stream) {
     constexpr bool S = decltype(stream)::value;
     if (n.last) {
-      hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT, S>), dim3(blocks), dim3(threads), (size_t)active * kVec<T> * sizeof(double), s, a,
-                         active, x, gy, gamma, beta, mean, rstd, reinterpret_cast<double*>(part));
+      hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT, S>), dim3(blocks), dim3(threads), pair_bytes(n, active, threads), s, a,
+                         active, x, gy, gamma, beta, mean, rstd, part);
       fold();
       if (writes)
         hipLaunchKernelGGL((norm_last_grad_apply_kernel<T, ACT, S>), grid, dim3(threads), inside ? n.G * sizeof(float2) : 0, s, out, own,
