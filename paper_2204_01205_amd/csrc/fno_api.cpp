@@ -355,8 +355,8 @@ int norm_shape(const fno_norm_desc* d, fno::NormShape* n) {
   if (d->flags & ~FNO_FLAG_ACCUMULATE_GRADS) { set_detail("unknown flag bits"); return FNO_EINVAL; }
   if (!(d->eps >= 0.0) || !std::isfinite(d->eps)) { set_detail("eps must be finite and at least 0"); return FNO_EINVAL; }
   if (d->channels > fno::kMaxNormChannels || d->batch > 65535 || (int64_t)d->batch * d->channels > ((int64_t)1 << 23) ||
-      d->npoints > ((int64_t)1 << 40)) {
-    set_detail("group_norm covers channels <= %d, batch <= 65535, batch * channels <= 2^23, npoints <= 2^40", fno::kMaxNormChannels);
+      d->npoints > ((int64_t)1 << 40) || (double)d->batch * d->channels * (double)d->npoints > 17592186044416.0) {
+    set_detail("group_norm covers channels <= %d, batch <= 65535, batch * channels <= 2^23, 2^44 values", fno::kMaxNormChannels);
     return FNO_EUNSUPPORTED;
   }
   *n = fno::NormShape{d->batch, d->channels, d->groups, d->npoints, d->layout == FNO_LAYOUT_CHANNELS_LAST,

@@ -140,8 +140,9 @@ __device__ __forceinline__ void block_sum2(double& a, double& b, double* red) {
 }
 
 // The 16-byte pieces of [begin, end) that start at multiples of their length go in tiles of U pieces a thread, of which this
-// call takes number `tile` and every `stride`-th after it, `count` at most: vecs(at, step) for a whole tile, vec(at) for the pieces of the last
-// one, and, with tile 0, one(at) for the values before and behind the pieces.  Places count from a 16-byte aligned base.
+// call takes number `tile` and every `stride`-th after it, `count` at most: vecs(at, step) for a whole tile, vec(at) for the
+// pieces of the last one, and, with tile 0, one(at) for the values before and behind the pieces.  Places count from a 16-byte
+// aligned base.
 template <int V, int U, class FVecs, class FVec, class FOne>
 __device__ __forceinline__ void sweep(long long begin, long long end, int tid, int threads, long long tile, long long stride,
                                       int count, FVecs&& vecs, FVec&& vec, FOne&& one) {
@@ -359,7 +360,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, con
     s1 += t1;                                            // 4 or 8 terms in float, then doubles
     s2 += t2;
   };
-  sweep<V, U>(row * a.P, (row + 1) * a.P, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads, SHORT ? 0 : j * a.run, 1, SHORT ? INT_MAX : a.run,
+  sweep<V, U>(row * a.P, (row + 1) * a.P, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads,
+              SHORT ? 0 : j * a.run, 1, SHORT ? INT_MAX : a.run,
               [&](long long at, long long step) {
                 pack<T> px[U], pg[U];
 #pragma unroll
@@ -387,27 +389,17 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, con
 }
 
 // A channel's parameter gradients, by a wave: sums over batch entries and pieces.  part[(b, c)][piece].
-__device__ __forceinline__ void param_grads(const NormArgs& a, int pieces, const double2* part, long long c, float* ggamma, float* gbeta,
-                                            int accumulate) {
+__device__ __forceinline__ void param_grads(const NormArgs& a, int pieces, const double2* part, long long c, float* ggamma,
+                                            float* gbeta, int accumulate) {
   if (c >= a.C) return;
   double s1 = 0.0, s2 = 0.0;
-  if (pieces >= 64) {
-    for (int b = 0; b < a.B; ++b) {
-      const double2* const at = part + ((long long)b * a.C + c) * pieces;
+  const int count = a.B * pieces;
 #pragma unroll 8
-      for (int j = threadIdx.x & 63; j < pieces; j += 64) {
-        s1 += at[j].x;
-        s2 += at[j].y;
-      }
-    }
-  } else {
-    for (int b = threadIdx.x & 63; b < a.B; b += 64) {
-      const double2* const at = part + ((long long)b * a.C + c) * pieces;
-      for (int j = 0; j < pieces; ++j) {
-        s1 += at[j].x;
-        s2 += at[j].y;
-      }
-    }
+  for (int q = threadIdx.x & 63; q < count; q += 64) {
+    const int b = q / pieces;
+    const double2 p = part[((long long)b * a.C + c) * pieces + (q - b * pieces)];
+    s1 += p.x;
+    s2 += p.y;
   }
   wave_sum2(s1, s2);
   if ((threadIdx.x & 63) != 0) return;
@@ -415,8 +407,8 @@ __device__ __forceinline__ void param_grads(const NormArgs& a, int pieces, const
   if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + s2 : s2);
 }
 // A thread's share of the sums of gamma gz and gamma gz xh over a group: thread `tid` of `threads`
-__device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const double2* part, const float* gamma, long long bg, int tid,
-                                            int threads, double& s1, double& s2) {
+__device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const double2* part, const float* gamma, long long bg,
+                                            int tid, int threads, double& s1, double& s2) {
   const double2* const at = part + bg * a.D * pieces;
   const int c0 = (int)(bg % a.G) * a.D;
   if (pieces >= threads) {
@@ -430,6 +422,7 @@ __device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const
       }
     }
   } else {
+#pragma unroll 4
     for (int j = tid; j < a.D * pieces; j += threads) {
       const double2 p = at[j];
       const double ga = gamma ? gamma[c0 + j / pieces] : 1.f;
@@ -439,16 +432,18 @@ __device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const
   }
 }
 
+constexpr int kFoldThreads = 1024;     // one block has a group's tens of thousands of sums to add
 // Blocks 0 .. groups - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the
 // parameters' gradients.
-__global__ __launch_bounds__(kThreads) void norm_grad_fold_kernel(NormArgs a, unsigned groups, const double2* part,
+__global__ __launch_bounds__(kFoldThreads) void norm_grad_fold_kernel(NormArgs a, unsigned groups, const double2* part,
                                                                   const float* gamma, float2* m, float* ggamma, float* gbeta,
                                                                   int accumulate) {
-  __shared__ double red[2 * kThreads / 64];
+  __shared__ double red[2 * kFoldThreads / 64];
   if (blockIdx.x >= groups)
-    return param_grads(a, a.pieces, part, (long long)(blockIdx.x - groups) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+    return param_grads(a, a.pieces, part, (long long)(blockIdx.x - groups) * (kFoldThreads / 64) + (threadIdx.x >> 6), ggamma,
+                       gbeta, accumulate);
   double s1 = 0.0, s2 = 0.0;
-  group_share(a, a.pieces, part, gamma, blockIdx.x, threadIdx.x, kThreads, s1, s2);
+  group_share(a, a.pieces, part, gamma, blockIdx.x, threadIdx.x, kFoldThreads, s1, s2);
   block_sum2(s1, s2, red);
   if (threadIdx.x == 0) m[blockIdx.x] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
 }
@@ -462,7 +457,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(NormArgs a, u
   constexpr int V = kVec<T>, U = 2;
   __shared__ double red[2 * kThreads / 64];
   if (!SHORT && blockIdx.x >= mine)
-    return param_grads(a, parts, part, (long long)(blockIdx.x - mine) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+    return param_grads(a, parts, part, (long long)(blockIdx.x - mine) * (kThreads / 64) + (threadIdx.x >> 6), ggamma, gbeta,
+                       accumulate);
   const long long row = SHORT ? (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6) : blockIdx.x / a.pieces;
   if (SHORT && row >= (long long)a.B * a.C) return;
   const int c = (int)(row % a.C);
@@ -488,7 +484,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_apply_kernel(NormArgs a, u
     for (int u = 0; u < V; ++u) v[u] = grad_of<ACT>(k, w, v[u], g[u]);
     store_pack<STREAM>(gx + at, repack(v));
   };
-  sweep<V, U>(row * a.P, (row + 1) * a.P, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads, j, a.pieces, INT_MAX,
+  sweep<V, U>(row * a.P, (row + 1) * a.P, SHORT ? threadIdx.x & 63 : threadIdx.x, SHORT ? 64 : kThreads, j, a.pieces,
+              INT_MAX,
               [&](long long at, long long step) {
                 pack<T> px[U], pg[U];
 #pragma unroll
@@ -612,42 +609,42 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
     q[u] = fma(d, d, q[u]);
   };
   sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
-                     [&](long long at, long long step) {
-                       pack<T> k[U];
+                   [&](long long at, long long step) {
+                     pack<T> k[U];
 #pragma unroll
-                       for (int u = 0; u < U; ++u) k[u] = load_any<STREAM>(x + at + u * step);
-                       float d[V], e[V];
+                     for (int u = 0; u < U; ++u) k[u] = load_any<STREAM>(x + at + u * step);
+                     float d[V], e[V];
 #pragma unroll
-                       for (int w = 0; w < V; ++w) d[w] = e[w] = 0.f;
+                     for (int w = 0; w < V; ++w) d[w] = e[w] = 0.f;
 #pragma unroll
-                       for (int u = 0; u < U; ++u) {
-                         float v[V];
-                         unpack(k[u], v);
-#pragma unroll
-                         for (int w = 0; w < V; ++w) {
-                           const float f = v[w] - middle[w];
-                           d[w] += f;
-                           e[w] = fmaf(f, f, e[w]);
-                         }
-                       }
+                     for (int u = 0; u < U; ++u) {
+                       float v[V];
+                       unpack(k[u], v);
 #pragma unroll
                        for (int w = 0; w < V; ++w) {
-                         s[w] += d[w];
-                         q[w] += e[w];
+                         const float f = v[w] - middle[w];
+                         d[w] += f;
+                         e[w] = fmaf(f, f, e[w]);
                        }
-                     },
-                     [&](long long at) {
-                       float v[V];
-                       unpack(load_any<STREAM>(x + at), v);
+                     }
 #pragma unroll
-                       for (int w = 0; w < V; ++w) add1(w, v[w]);
-                     },
-                     [&](long long at, int u) {
-                       const float v = load1(x + at);
+                     for (int w = 0; w < V; ++w) {
+                       s[w] += d[w];
+                       q[w] += e[w];
+                     }
+                   },
+                   [&](long long at) {
+                     float v[V];
+                     unpack(load_any<STREAM>(x + at), v);
 #pragma unroll
-                       for (int w = 0; w < V; ++w)
-                         if (w == u) add1(w, v);
-                     });
+                     for (int w = 0; w < V; ++w) add1(w, v[w]);
+                   },
+                   [&](long long at, int u) {
+                     const float v = load1(x + at);
+#pragma unroll
+                     for (int w = 0; w < V; ++w)
+                       if (w == u) add1(w, v);
+                   });
   if ((int)threadIdx.x < active) {
 #pragma unroll
     for (int u = 0; u < V; ++u) pairs[threadIdx.x * V + u] = make_double2(s[u], q[u]);
@@ -677,7 +674,8 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
 }
 
 // part: the sums of the batch entry's pieces, few enough for every block to add them itself, a group a wave (null: the
-// statistics are in `stat`).
+// statistics are in `stat`).  (Those in LDS and those in memory are read in two ways: one pointer for both would have to be
+// moved out of its LDS array for batch entries after the first.)
 template <class T, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int active, const T* x, const float* gamma,
                                                                const float* beta, const Stat* stat, const double2* part, int parts,
@@ -781,29 +779,29 @@ __global__ __launch_bounds__(1024) void norm_last_grad_sum_kernel(NormArgs a, in
     }
   };
   sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
-                     [&](long long at, long long step) {
-                       pack<T> px[U], pg[U];
+                   [&](long long at, long long step) {
+                     pack<T> px[U], pg[U];
 #pragma unroll
-                       for (int u = 0; u < U; ++u) {
-                         px[u] = load_any<STREAM>(x + at + u * step);
-                         pg[u] = load_any<STREAM>(gy + at + u * step);
-                       }
-                       float t1[V] = {}, t2[V] = {};
+                     for (int u = 0; u < U; ++u) {
+                       px[u] = load_any<STREAM>(x + at + u * step);
+                       pg[u] = load_any<STREAM>(gy + at + u * step);
+                     }
+                     float t1[V] = {}, t2[V] = {};
 #pragma unroll
-                       for (int u = 0; u < U; ++u) add(px[u], pg[u], t1, t2);
-                       flush(t1, t2);
-                     },
-                     [&](long long at) {
-                       float t1[V] = {}, t2[V] = {};
-                       add(load_any<STREAM>(x + at), load_any<STREAM>(gy + at), t1, t2);
-                       flush(t1, t2);
-                     },
-                     [&](long long at, int u) {
-                       const float v = load1(x + at), g = load1(gy + at);
+                     for (int u = 0; u < U; ++u) add(px[u], pg[u], t1, t2);
+                     flush(t1, t2);
+                   },
+                   [&](long long at) {
+                     float t1[V] = {}, t2[V] = {};
+                     add(load_any<STREAM>(x + at), load_any<STREAM>(gy + at), t1, t2);
+                     flush(t1, t2);
+                   },
+                   [&](long long at, int u) {
+                     const float v = load1(x + at), g = load1(gy + at);
 #pragma unroll
-                       for (int w = 0; w < V; ++w)
-                         if (w == u) add1(w, v, g);
-                     });
+                     for (int w = 0; w < V; ++w)
+                       if (w == u) add1(w, v, g);
+                   });
   if ((int)threadIdx.x < active) {
 #pragma unroll
     for (int u = 0; u < V; ++u) pairs[threadIdx.x * V + u] = make_double2(s1[u], s2[u]);
@@ -821,7 +819,8 @@ __global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, 
   constexpr int V = kVec<T>, U = 2;
   extern __shared__ double lds[];
   if (blockIdx.x >= mine)
-    return param_grads(a, parts, part, (long long)(blockIdx.x - mine) * (blockDim.x >> 6) + (threadIdx.x >> 6), ggamma, gbeta, accumulate);
+    return param_grads(a, parts, part, (long long)(blockIdx.x - mine) * (blockDim.x >> 6) + (threadIdx.x >> 6), ggamma, gbeta,
+                       accumulate);
   const int b = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
   float2* const own = reinterpret_cast<float2*>(lds);
   if (m == nullptr) {
@@ -1030,7 +1029,43 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
     small_store<T, LAST>(a, s, b, g, gx, w);
   }
   if (!params) return;
-  const int lane = threadIdx.x & (lanes - 1), P = (int)a.P;
+  // a channel's sums by `lanes` lanes or, where there are fewer channels than waves, by several waves
+  const int nw = (int)blockDim.x >> 6, P = (int)a.P;
+  auto put = [&](int d, double t1, double t2) {
+    const int c = g * a.D + d;
+    if (part != nullptr) {
+      part[(long long)b * a.C + c] = make_double2(t1, t2);
+    } else {
+      if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + t1 : t1);
+      if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + t2 : t2);
+    }
+  };
+  if (2 * a.D <= nw) {
+    const int waves = nw / a.D, d = (int)(threadIdx.x >> 6) / waves, w = (int)(threadIdx.x >> 6) % waves;
+    double t1 = 0.0, t2 = 0.0;
+    if (d < a.D)
+      for (int p = w * 64 + (threadIdx.x & 63); p < P; p += waves * 64) {
+        const float2 q = product[LAST ? p * a.D + d : d * P + p];
+        t1 += q.x;
+        t2 += q.y;
+      }
+    wave_sum2(t1, t2);
+    __syncthreads();                                      // (everybody has read what block_sum2 left in red)
+    if ((threadIdx.x & 63) == 0) {
+      red[2 * (threadIdx.x >> 6)] = t1;
+      red[2 * (threadIdx.x >> 6) + 1] = t2;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x >= a.D) return;
+    t1 = t2 = 0.0;
+    for (int k = 0; k < waves; ++k) {
+      t1 += red[2 * (threadIdx.x * waves + k)];
+      t2 += red[2 * (threadIdx.x * waves + k) + 1];
+    }
+    put(threadIdx.x, t1, t2);
+    return;
+  }
+  const int lane = threadIdx.x & (lanes - 1);
   for (int d0 = 0; d0 < a.D; d0 += blockDim.x / lanes) {  // (the same number of turns for all lanes of a wave)
     const int d = d0 + threadIdx.x / lanes;
     double t1 = 0.0, t2 = 0.0;
@@ -1044,14 +1079,7 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
       t1 += __shfl_xor(t1, off);
       t2 += __shfl_xor(t2, off);
     }
-    if (d >= a.D || lane != 0) continue;
-    const int c = g * a.D + d;
-    if (part != nullptr) {
-      part[(long long)b * a.C + c] = make_double2(t1, t2);
-    } else {
-      if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + t1 : t1);
-      if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + t2 : t2);
-    }
+    if (d < a.D && lane == 0) put(d, t1, t2);
   }
 }
 
@@ -1063,7 +1091,8 @@ constexpr long long kTileBytes = 16384;       // of a whole tile of 256 threads 
 constexpr long long kApplyBlocks = 1 << 22;   // of one that writes: a tile each, but for the very largest fields; channels last,
 constexpr long long kApplyInside = 2048;      // where every block first adds the sums of pieces
 constexpr long long kApplyLast = 8192;        // where a thread first has its channels' factors to work out, so many
-constexpr long long kShortRow = 2048;         // rows below this go wave by wave
+constexpr long long kShortRow = 512;          // rows below this go wave by wave: 4 x 64 rows of 600 take 8.7 us, 7.1 block by
+                                              // block, 32 x 64 of them 9.8 and 10.2
 
 NormArgs norm_args(const NormShape& n) {
   const int D = n.C / n.G;
@@ -1107,11 +1136,15 @@ NormArgs cut_rows(const NormShape& n, int fields, long long blocks) {  // channe
   if (n.P >= kShortRow) deal(a, (long long)n.B * n.C, (n.P + tile - 1) / tile, blocks);
   return a;
 }
-// Channels last: blocks of at least 64 points, whose sums (16 bytes a channel) are then little beside them.
-NormArgs cut_points(const NormShape& n, int fields, long long blocks) {
+// Channels last: blocks of at least 64 points, whose sums (16 bytes a channel) are then little beside them, and of at least
+// three tiles where they only read (sums: every piece is one more to add for one block).
+NormArgs cut_points(const NormShape& n, int fields, long long blocks, int tiles_at_least) {
   NormArgs a = norm_args(n);
   const long long tile = (long long)active_threads(n.C, n.bf16 ? 8 : 4) * (n.bf16 ? 8 : 4) * (fields == 1 ? 4 : 2);
-  const long long tiles = (n.P * n.C + tile - 1) / tile, most = n.B * (n.P / 64 + 1);
+  const long long tiles = (n.P * n.C + tile - 1) / tile;
+  long long most = n.B * (n.P / 64 + 1);
+  if (most > n.B * tiles / tiles_at_least && n.B * tiles > 256) most = n.B * tiles / tiles_at_least;
+  if (most < 256) most = 256;
   deal(a, n.B, tiles, blocks < most ? blocks : most);
   return a;
 }
@@ -1123,8 +1156,8 @@ size_t pair_bytes(const NormShape& n, int active, int threads) {
 
 // scratch: sums of pieces, statistics or means
 size_t norm_part_bytes(const NormShape& n) {
-  const NormArgs f = n.last ? cut_points(n, 1, kSumBlocks / 2) : cut_groups(n);
-  const NormArgs b = n.last ? cut_points(n, 2, kSumBlocks / 2) : cut_rows(n, 2, kSumBlocks);
+  const NormArgs f = n.last ? cut_points(n, 1, kSumBlocks / 2, 3) : cut_groups(n);
+  const NormArgs b = n.last ? cut_points(n, 2, kSumBlocks / 2, 3) : cut_rows(n, 2, kSumBlocks);
   const size_t fwd = (size_t)n.B * n.G * f.pieces, bwd = (size_t)n.B * n.C * b.pieces;
   return ((fwd > bwd ? fwd : bwd) * sizeof(double2) + 255) & ~size_t(255);
 }
@@ -1134,10 +1167,24 @@ unsigned row_blocks(const NormArgs& a, bool short_rows) {
   return (unsigned)(short_rows ? (rows + kThreads / 64 - 1) / (kThreads / 64) : rows * a.pieces);
 }
 
-// Sums of pieces that every block of the next launch adds itself (8 KB from the L2 a block at most), sparing a launch
-constexpr long long kInlineParts = 512;
+// Sums of pieces that every block of the next launch adds itself, sparing a launch: as many as kInlineParts where the field is
+// small (channels first: 4 x 16 x 134400 values, adjoint, 33.6 us and 37.3 with the launch; of a field of 168 MB, where fewer
+// and longer blocks write, 148 and 134), channels last a quarter of that.
+constexpr long long kInlineParts = 2048, kInlineBytes = 64ll << 20;
+bool inline_parts(const NormShape& n, long long parts) {
+  return parts <= (n.last ? kInlineParts / 4 : kInlineParts) && n.P * n.C * n.B * (n.bf16 ? 2 : 4) <= kInlineBytes;
+}
 
-bool small_fits(const NormShape& n, int most) { return n.P > 0 && n.P <= most && n.P * (n.C / n.G) <= most; }
+// Whether one block takes a whole group.  Us, this way and in several launches: channels first, forward, 4 groups of 4096
+// values 5.7 and 7.0, of 16000 7.3 and 7.7, 1024 of 8000 17 and 24.  Channels last, where a group is a narrow column of the
+// field: 4 groups of 4096 7.3 and 8.1, of 16000 13.3 and 8.5, 512 groups of 512 (8 channels) 5.7 and 8.4, 512 of 4000 (2 channels)
+// 25 and 12.
+bool small_fits(const NormShape& n, bool adjoint) {
+  const long long most = n.last ? (adjoint ? 2048 : 8192) : adjoint ? kSmallBwd : kSmallFwd;
+  return n.P > 0 && n.P <= most && n.P * (n.C / n.G) <= most && (!n.last || n.P * n.C * n.B <= 1 << 19);
+}
+// blocks of norm_grad_fold_kernel for the parameters' gradients
+unsigned fold_blocks(const NormShape& n) { return (unsigned)((n.C + kFoldThreads / 64 - 1) / (kFoldThreads / 64)); }
 SmallArgs small_args(const NormShape& n, int V) {
   const int D = n.C / n.G;
   const unsigned by = n.last ? (unsigned)D : (unsigned)n.P;
@@ -1161,7 +1208,7 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
                void* ws, hipStream_t s) {
   double2* part = static_cast<double2*>(ws);
   Stat* stat = reinterpret_cast<Stat*>(static_cast<char*>(ws) + norm_part_bytes(n));
-  if (small_fits(n, kSmallFwd)) {
+  if (small_fits(n, false)) {
     const NormArgs a = norm_args(n);
     const SmallArgs k = small_args(n, kVec<T>);
     with(n.last, [&](auto last) {
@@ -1172,9 +1219,9 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
   }
   const bool hint = streams(n, 1);
   if (n.last) {
-    const NormArgs a = cut_points(n, 1, kSumBlocks / 2), out = cut_points(n, 1, kApplyLast);
+    const NormArgs a = cut_points(n, 1, kSumBlocks / 2, 3), out = cut_points(n, 1, kApplyLast, 1);
     const int active = active_threads(n.C, kVec<T>), threads = (active + 63) / 64 * 64;
-    const bool inside = (long long)n.G * a.pieces <= kInlineParts && n.P > 0;
+    const bool inside = n.P > 0 && inline_parts(n, (long long)n.G * a.pieces);
     const dim3 grid((unsigned)(n.B * a.pieces));
     with(hint, [&](auto stream) {
       constexpr bool S = decltype(stream)::value;
@@ -1188,7 +1235,7 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     return hipGetLastError();
   }
   const NormArgs a = cut_groups(n);
-  const bool short_rows = n.P < kShortRow, inside = !short_rows && a.pieces <= kInlineParts / 2;
+  const bool short_rows = n.P < kShortRow, inside = !short_rows && inline_parts(n, a.pieces);
   const NormArgs rows = cut_rows(n, 1, inside ? kApplyInside : kApplyBlocks);
   with(hint, [&](auto stream) {
     constexpr bool S = decltype(stream)::value;
@@ -1208,7 +1255,7 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   double2* part = static_cast<double2*>(ws);
   float2* m = reinterpret_cast<float2*>(static_cast<char*>(ws) + norm_part_bytes(n));
   const bool params = ggamma != nullptr || gbeta != nullptr;
-  if (small_fits(n, kSmallBwd)) {
+  if (small_fits(n, true)) {
     const NormArgs a = norm_args(n);
     const SmallArgs k = small_args(n, kVec<T>);
     int lanes = 1;
@@ -1220,15 +1267,15 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
                          ggamma, gbeta, accumulate);
     });
     if (later)
-      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3((n.C + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s, a, 0u, part, gamma,
-                         m, ggamma, gbeta, accumulate);
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold_blocks(n)), dim3(kFoldThreads), 0, s, a, 0u, part, gamma, m, ggamma, gbeta,
+                         accumulate);
     return hipGetLastError();
   }
   const bool short_rows = !n.last && n.P < kShortRow, writes = gx != nullptr && n.P > 0;
-  const NormArgs a = n.last ? cut_points(n, 2, kSumBlocks / 2) : cut_rows(n, 2, kSumBlocks);
+  const NormArgs a = n.last ? cut_points(n, 2, kSumBlocks / 2, 3) : cut_rows(n, 2, kSumBlocks);
     const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
-  const bool inside = writes && !short_rows && (long long)(n.last ? n.C : n.C / n.G) * a.pieces <= kInlineParts;
-  const NormArgs out = n.last ? cut_points(n, 2, kApplyLast) : cut_rows(n, 2, inside ? kApplyInside : kApplyBlocks);
+  const bool inside = writes && !short_rows && inline_parts(n, (long long)(n.last ? n.C : n.C / n.G) * a.pieces);
+  const NormArgs out = n.last ? cut_points(n, 2, kApplyLast, 1) : cut_rows(n, 2, inside ? kApplyInside : kApplyBlocks);
   const unsigned channel_blocks = params ? (unsigned)((n.C + threads / 64 - 1) / (threads / 64)) : 0;
   const unsigned groups = (unsigned)(n.B * n.G), blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
   const unsigned own = n.last ? (unsigned)(n.B * out.pieces) : row_blocks(out, short_rows);
@@ -1236,8 +1283,8 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   const float2* means = inside ? nullptr : m;
   auto fold = [&] {
     if (!inside)
-      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? (n.C + kThreads / 64 - 1) / (kThreads / 64) : 0)), dim3(kThreads), 0, s,
-                         a, groups, part, gamma, m, ggamma, gbeta, accumulate);
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? fold_blocks(n) : 0)), dim3(kFoldThreads), 0, s, a, groups, part,
+                         gamma, m, ggamma, gbeta, accumulate);
   };
   with(streams(n, 2), [&](auto stream) {
     constexpr bool S = decltype(stream)::value;

@@ -127,6 +127,13 @@ SIZES = [
     (1, 64, 2, 6000),
     (1, 20, 1, 120001),           # long rows
     (64, 16, 4, 64),              # many short rows
+    (2, 64, 2, 600),              # groups past one block, of short rows
+    (1, 96, 1, 1501),
+    (1, 1000, 4, 211),
+    (3, 1024, 2, 2050),           # rows just long enough for blocks of their own
+    (300, 32, 8, 5),
+    (1, 1023, 3, 100),            # the longest steps of the channels-last kernels
+    (2, 1019, 1, 70),
 ]
 
 
@@ -353,7 +360,8 @@ def test_refusals_without_a_device():
         d = B.make_norm_desc(**{**dict(batch=1, channels=8, groups=2, npoints=100), **change})
         assert lib.fno_group_norm_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == B.FNO_EINVAL, change
         assert B.fno_status_string(B.FNO_EINVAL)
-    for change in (dict(channels=1026), dict(batch=65536), dict(npoints=2 ** 41)):
+    for change in (dict(channels=1026), dict(batch=65536), dict(npoints=2 ** 41), dict(npoints=2 ** 40, channels=32),
+                   dict(batch=60000, channels=256)):
         d = B.make_norm_desc(**{**dict(batch=1, channels=8, groups=2, npoints=100), **change})
         assert lib.fno_group_norm_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == B.FNO_EUNSUPPORTED, change
     p, z, odd = ctypes.c_void_p(4096), ctypes.c_void_p(0), ctypes.c_void_p(4100)
