@@ -146,16 +146,28 @@ __device__ __forceinline__ unsigned shared_exponent(unsigned top, unsigned span)
   const unsigned e = (top + 0xFFFFFu) >> 23;
   return min(max(e, span + 1u), 254u);
 }
-__device__ __forceinline__ unsigned encode_m(float x, unsigned e, unsigned r) {
-  const unsigned bits = __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu, low = (e - kSpanM) << 3, first = ((low + 1u) << 20);
-  unsigned code;
-  if (bits >= first) code = min(((bits + (r << 4)) >> 20) - low, 127u);
-  else code = __builtin_bit_cast(float, first) * ((float)r * (1.0f / 65536.0f)) < fabsf(x) ? 1u : 0u;
+// What the codes of a block have in common, the same in all lanes
+struct Scale8 {
+  unsigned low;        // bits of the smallest power
+  unsigned first;      // bits of what m's code 1 stands for
+  float part;          // that / 65536
+};
+__device__ __forceinline__ Scale8 scale_of(unsigned e, unsigned span) {
+  Scale8 s;
+  s.low = (e - span) << 3;
+  s.first = (s.low + 1u) << 20;
+  s.part = __builtin_bit_cast(float, s.first) * (1.0f / 65536.0f);
+  return s;
+}
+__device__ __forceinline__ unsigned encode_m(float x, const Scale8& s, unsigned r) {
+  const unsigned bits = __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu;
+  const unsigned whole = min(((bits + (r << 4)) >> 20) - s.low, 127u), little = s.part * (float)r < fabsf(x) ? 1u : 0u;
+  const unsigned code = bits >= s.first ? whole : little;
   return x < 0.f ? code + 128u : code;
 }
-__device__ __forceinline__ unsigned encode_v(float x, unsigned e, unsigned r) {
-  const unsigned bits = __builtin_bit_cast(unsigned, x), low = (e - kSpanV) << 3;
-  const int code = (int)((bits + (r << 4)) >> 20) - (int)low;
+__device__ __forceinline__ unsigned encode_v(float x, const Scale8& s, unsigned r) {
+  const unsigned bits = __builtin_bit_cast(unsigned, x);
+  const int code = (int)((bits + (r << 4)) >> 20) - (int)s.low;
   return bits == 0u ? 0u : (unsigned)min(max(code, 1), 255);
 }
 __device__ __forceinline__ float decode_m(unsigned code, unsigned e) {
@@ -170,7 +182,7 @@ __device__ __forceinline__ float decode_v(unsigned code, unsigned e) {
 // the largest of a wave's values, in every lane
 template <int CTRL, int ROWS>
 __device__ __forceinline__ unsigned dpp_max(unsigned v) {
-  return max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROWS, 0xF, false));
+  return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, ROWS == 0xF));
 }
 __device__ __forceinline__ unsigned wave_max(unsigned v) {
   v = dpp_max<0xB1, 0xF>(v);           // lane ^ 1
@@ -187,34 +199,53 @@ struct Group8 {
   v4f p, g;
   unsigned m, v, e;    // codes; exponents, m's in the low byte
 };
-__device__ __forceinline__ void group_step(const AdamwScalars& c, float keep, float scale, unsigned block, int lane, Group8& q) {
-  const unsigned em = q.e & 255u, ev = q.e >> 8;
-  float mi[4], vi[4];
-  unsigned top_m = 0, top_v = 0;
+// N blocks together, so that their chains of dependent steps go side by side.  FINE: square root and quotient to the last
+// bit; otherwise by the instructions that are good to one unit in the last place and take subnormal squares for zero.
+template <int N, bool FINE>
+__device__ __forceinline__ void groups_step(const AdamwScalars& c, float keep, float scale, const unsigned (&block)[N], int lane,
+                                            Group8 (&q)[N]) {
+  float mi[N][4], vi[N][4];
+  unsigned top_m[N], top_v[N];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    mi[u] = decode_m((q.m >> (8 * u)) & 255u, em);
-    vi[u] = decode_v((q.v >> (8 * u)) & 255u, ev);
-    moments(c, q.g[u] * scale, mi[u], vi[u]);
-    q.p[u] = updated(c, keep, q.p[u], mi[u], vi[u]);
-    top_m = max(top_m, __builtin_bit_cast(unsigned, mi[u]) & 0x7FFFFFFFu);
-    top_v = max(top_v, __builtin_bit_cast(unsigned, vi[u]));
-  }
-  const unsigned nm = shared_exponent(wave_max(top_m), kSpanM), nv = shared_exponent(wave_max(top_v), kSpanV);
-  q.m = 0;
-  q.v = 0;
+  for (int k = 0; k < N; ++k) {
+    const unsigned em = q[k].e & 255u, ev = q[k].e >> 8;
+    top_m[k] = top_v[k] = 0;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const unsigned r = mix_bits(block + (unsigned)(4 * lane + u) * 0x9E3779B1u);
-    q.m |= encode_m(mi[u], nm, r & 0xFFFFu) << (8 * u);
-    q.v |= encode_v(vi[u], nv, r >> 16) << (8 * u);
+    for (int u = 0; u < 4; ++u) {
+      float m = decode_m((q[k].m >> (8 * u)) & 255u, em), v = decode_v((q[k].v >> (8 * u)) & 255u, ev);
+      moments(c, q[k].g[u] * scale, m, v);
+      if (FINE) q[k].p[u] = updated(c, keep, q[k].p[u], m, v);
+      else q[k].p[u] = q[k].p[u] * keep - c.lr1 * m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v * c.ic2) + c.eps);
+      top_m[k] = max(top_m[k], __builtin_bit_cast(unsigned, m) & 0x7FFFFFFFu);
+      top_v[k] = max(top_v[k], __builtin_bit_cast(unsigned, v));
+      mi[k][u] = m;
+      vi[k][u] = v;
+    }
   }
-  if (nm == 255u) q.m = 0;             // (uniform)
-  if (nv == 255u) q.v = 0;
-  q.e = nm | nv << 8;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    top_m[k] = wave_max(top_m[k]);
+    top_v[k] = wave_max(top_v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const unsigned nm = shared_exponent(top_m[k], kSpanM), nv = shared_exponent(top_v[k], kSpanV);
+    const Scale8 sm = scale_of(nm, kSpanM), sv = scale_of(nv, kSpanV);
+    unsigned cm = 0, cv = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const unsigned r = mix_bits(block[k] + (unsigned)(4 * lane + u) * 0x9E3779B1u);
+      cm |= encode_m(mi[k][u], sm, r & 0xFFFFu) << (8 * u);
+      cv |= encode_v(vi[k][u], sv, r >> 16) << (8 * u);
+    }
+    q[k].m = nm == 255u ? 0u : cm;
+    q[k].v = nv == 255u ? 0u : cv;
+    q[k].e = nm | nv << 8;
+  }
 }
 
 // A wave takes four blocks of 256 values at a time, all asked for before the first is used.
+template <bool FINE>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScalars c) {
   const int k = tensor_of(l, blockIdx.x);
   const AdamwEntry& t = l.t[k];
@@ -230,6 +261,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
   long long at = begin + wave * (kBlockValues / 4);
   for (; at + 4 * kGroup <= end; at += kBlockValues) {
     Group8 q[4];
+    unsigned block[4];
     const long long b0 = at / kGroup;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -239,11 +271,12 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
       q[u].m = load_codes(m + i);
       q[u].v = load_codes(v + i);
       q[u].e = e[b0 + u];
+      block[u] = random_of(b0 + u);
     }
+    groups_step<4, FINE>(c, t.keep, scale, block, lane, q);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const long long i = at + u * kGroup + 4 * lane;
-      group_step(c, t.keep, scale, random_of(b0 + u), lane, q[u]);
       store4(t.p + i, q[u].p);
       store_codes(m + i, q[u].m);
       store_codes(v + i, q[u].v);
@@ -253,7 +286,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
   // the tensor's last blocks, the very last one cut: values past the end are zeros that nobody stores
   const long long stop = at + kBlockValues / 4 < end ? at + kBlockValues / 4 : end;
   for (; at < stop; at += kGroup) {
-    Group8 q{};
+    Group8 one[1] = {};
+    Group8& q = one[0];
     const long long i = at + 4 * lane;
     q.e = e[at / kGroup];
 #pragma unroll
@@ -264,7 +298,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
       q.m |= (unsigned)m[i + u] << (8 * u);
       q.v |= (unsigned)v[i + u] << (8 * u);
     }
-    group_step(c, t.keep, scale, random_of(at / kGroup), lane, q);
+    const unsigned block[1] = {random_of(at / kGroup)};
+    groups_step<1, FINE>(c, t.keep, scale, block, lane, one);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (i + u >= end) continue;
@@ -404,7 +439,9 @@ hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwStep& st, hi
                        (float)(st.lr / c1), (float)(1.0 / c2), (float)st.max_norm,
                        mix_bits(mix_bits(st.seed) ^ (unsigned)st.step), st.norm};
   return over_tensors(t, count, st.lr, piece_of(t, count, kStepBlocks), [&](const AdamwList& l, long long pieces) {
-    if (st.bits == 8) hipLaunchKernelGGL(adamw8_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
+    // the root of a subnormal square is below 1.1e-19, less than half a unit in the last place of eps from 2e-12 on
+    if (st.bits == 8 && st.eps >= 2e-12) hipLaunchKernelGGL(adamw8_kernel<false>, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
+    else if (st.bits == 8) hipLaunchKernelGGL(adamw8_kernel<true>, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
     else hipLaunchKernelGGL(adamw32_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
   });
 }

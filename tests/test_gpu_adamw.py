@@ -116,6 +116,28 @@ def test_a_step_matches_the_oracle(sizes, bits, skip):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 1e-15, 1e-12, 3e-12, 1e-3])
+def test_eps_of_any_size(bits, eps):
+    """Down to zero, with gradients whose squares are tiny (of 1e-15) or subnormal (of 3e-19, where v has few bits left and
+    the parameters are only asked to be finite): the quotient is then m over the root of v alone."""
+    for tiny in (1.0, 1e-15, 3e-19):
+        t = Tensors([700, 5000], bits)
+        for k, n in enumerate(t.sizes):
+            g = (tiny * np.sign(t.p[k]) * (0.5 + np.abs(t.p[k]) % 1.0)).astype(np.float32)       # 0.5 to 1.5 times `tiny`
+            t.g[k] = g
+            t.dg[k].copy_(torch.from_numpy(g))
+            for s in (t.m[k], t.v[k]) + (() if bits == 32 else (t.exps[k],)):
+                s[:] = 0
+            for s in (t.dm[k], t.dv[k]) + (() if bits == 32 else (t.de[k],)):
+                s.zero_()
+        B.fno_adamw_step(t.list, HYPER["lr"], HYPER["beta1"], HYPER["beta2"], eps, 1, seed=2)
+        if tiny > 1e-18:
+            t.check_params(1, hyper=dict(HYPER, eps=eps))
+        assert all(torch.isfinite(p).all() for p in t.dp) or (eps == 0.0 and tiny < 1e-18)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("max_norm", [0.5, 1e9])
 def test_clipping_by_the_norm_of_all_gradients(bits, max_norm):
     t = Tensors([5000, 3, 70000, 1], bits)
