@@ -2,6 +2,8 @@
 // moments stand for.
 #include "fno_device.h"
 
+#include <type_traits>
+
 namespace fno {
 
 namespace {
@@ -45,17 +47,30 @@ __device__ __forceinline__ int tensor_of(const AdamwList& l, unsigned piece) {
   return lo;
 }
 
-// Four floats, four codes or 8 bytes at an address that is 4-byte aligned; every value is touched once a step.
+// Four floats, four codes or four bf16 values at an address that is 4-byte aligned.  STREAM: with the nontemporal hint, for lists
+// that the memory-side cache does not hold.
+template <bool STREAM>
 __device__ __forceinline__ v4f load4(const float* p) {
   typedef v4f loose __attribute__((aligned(4)));
-  return __builtin_nontemporal_load(reinterpret_cast<const loose*>(p));
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const loose*>(p));
+  else return *reinterpret_cast<const loose*>(p);
 }
+template <bool STREAM>
 __device__ __forceinline__ void store4(float* p, v4f v) {
   typedef v4f loose __attribute__((aligned(4)));
-  __builtin_nontemporal_store(v, reinterpret_cast<loose*>(p));
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<loose*>(p));
+  else *reinterpret_cast<loose*>(p) = v;
 }
-__device__ __forceinline__ unsigned load_codes(const u8* p) { return __builtin_nontemporal_load(reinterpret_cast<const unsigned*>(p)); }
-__device__ __forceinline__ void store_codes(u8* p, unsigned v) { __builtin_nontemporal_store(v, reinterpret_cast<unsigned*>(p)); }
+template <bool STREAM>
+__device__ __forceinline__ void store_halves(u16* p, v2u v) {
+  typedef v2u loose __attribute__((aligned(4)));
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<loose*>(p));
+  else *reinterpret_cast<loose*>(p) = v;
+}
+template <bool STREAM>
+__device__ __forceinline__ unsigned load_codes(const u8* p) { return ld_once<STREAM>(reinterpret_cast<const unsigned*>(p)); }
+template <bool STREAM>
+__device__ __forceinline__ void store_codes(u8* p, unsigned v) { st_once<STREAM>(reinterpret_cast<unsigned*>(p), v); }
 
 __host__ __device__ __forceinline__ unsigned mix_bits(unsigned x) {
   x ^= x >> 16;
@@ -90,6 +105,7 @@ __device__ __forceinline__ float updated(const AdamwScalars& c, float keep, floa
 }
 
 // A thread takes 16 values at a time, four from each of four quarters of the block's, all asked for before the first is used.
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw32_kernel(AdamwList l, AdamwScalars c) {
   const AdamwEntry& t = l.t[tensor_of(l, blockIdx.x)];
   float scale;
@@ -104,10 +120,10 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(AdamwList l, AdamwSca
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const long long i = at + u * (kBlockValues / 4) + 4 * threadIdx.x;
-      gq[u] = load4(g + i);
-      mq[u] = load4(m + i);
-      vq[u] = load4(v + i);
-      pq[u] = load4(p + i);
+      gq[u] = load4<STREAM>(g + i);
+      mq[u] = load4<STREAM>(m + i);
+      vq[u] = load4<STREAM>(v + i);
+      pq[u] = load4<STREAM>(p + i);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -120,9 +136,9 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(AdamwList l, AdamwSca
         vq[u][w] = vi;
         pq[u][w] = updated(c, t.keep, pq[u][w], mi, vi);
       }
-      store4(m + i, mq[u]);
-      store4(v + i, vq[u]);
-      store4(p + i, pq[u]);
+      store4<STREAM>(m + i, mq[u]);
+      store4<STREAM>(v + i, vq[u]);
+      store4<STREAM>(p + i, pq[u]);
     }
   }
   for (long long i = at + threadIdx.x; i < end; i += kThreads) {
@@ -245,7 +261,7 @@ __device__ __forceinline__ void groups_step(const AdamwScalars& c, float keep, f
 }
 
 // A wave takes four blocks of 256 values at a time, all asked for before the first is used.
-template <bool FINE>
+template <bool FINE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScalars c) {
   const int k = tensor_of(l, blockIdx.x);
   const AdamwEntry& t = l.t[k];
@@ -266,10 +282,10 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const long long i = at + u * kGroup + 4 * lane;
-      q[u].p = load4(t.p + i);
-      q[u].g = load4(t.g + i);
-      q[u].m = load_codes(m + i);
-      q[u].v = load_codes(v + i);
+      q[u].p = load4<STREAM>(t.p + i);
+      q[u].g = load4<STREAM>(t.g + i);
+      q[u].m = load_codes<STREAM>(m + i);
+      q[u].v = load_codes<STREAM>(v + i);
       q[u].e = e[b0 + u];
       block[u] = random_of(b0 + u);
     }
@@ -277,9 +293,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const long long i = at + u * kGroup + 4 * lane;
-      store4(t.p + i, q[u].p);
-      store_codes(m + i, q[u].m);
-      store_codes(v + i, q[u].v);
+      store4<STREAM>(t.p + i, q[u].p);
+      store_codes<STREAM>(m + i, q[u].m);
+      store_codes<STREAM>(v + i, q[u].v);
       if (lane == 0) e[b0 + u] = (u16)q[u].e;
     }
   }
@@ -312,6 +328,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
 }
 
 // p and g of an entry hold the outputs here
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw_read_kernel(AdamwList l) {
   const AdamwEntry& t = l.t[tensor_of(l, blockIdx.x)];
   const long long begin = (long long)(blockIdx.x - t.first) * l.piece;
@@ -319,7 +336,6 @@ __global__ __launch_bounds__(kThreads) void adamw_read_kernel(AdamwList l) {
   const u8 *const m = static_cast<const u8*>(t.m), *const v = static_cast<const u8*>(t.v);
   const u16* const e = reinterpret_cast<const u16*>(t.e);
   u16 *const mo = reinterpret_cast<u16*>(t.p), *const vo = reinterpret_cast<u16*>(const_cast<float*>(t.g));
-  typedef v2u loose __attribute__((aligned(4)));
   auto put = [&](long long at, unsigned cm, unsigned cv, unsigned ex) {
     unsigned a[4], b[4];
 #pragma unroll
@@ -329,8 +345,8 @@ __global__ __launch_bounds__(kThreads) void adamw_read_kernel(AdamwList l) {
     }
     const v2u x = {a[0] >> 16 | (a[1] & 0xFFFF0000u), a[2] >> 16 | (a[3] & 0xFFFF0000u)};
     const v2u y = {b[0] >> 16 | (b[1] & 0xFFFF0000u), b[2] >> 16 | (b[3] & 0xFFFF0000u)};
-    __builtin_nontemporal_store(x, reinterpret_cast<loose*>(mo + at));
-    __builtin_nontemporal_store(y, reinterpret_cast<loose*>(vo + at));
+    store_halves<STREAM>(mo + at, x);
+    store_halves<STREAM>(vo + at, y);
   };
   long long at = begin + 4 * threadIdx.x;
   constexpr int U = kBlockValues / (4 * kThreads);
@@ -338,14 +354,14 @@ __global__ __launch_bounds__(kThreads) void adamw_read_kernel(AdamwList l) {
     unsigned cm[U], cv[U], ex[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      cm[u] = load_codes(m + at + u * 4 * kThreads);
-      cv[u] = load_codes(v + at + u * 4 * kThreads);
+      cm[u] = load_codes<STREAM>(m + at + u * 4 * kThreads);
+      cv[u] = load_codes<STREAM>(v + at + u * 4 * kThreads);
       ex[u] = e[(at + u * 4 * kThreads) / kGroup];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) put(at + u * 4 * kThreads, cm[u], cv[u], ex[u]);
   }
-  for (; at + 4 <= end; at += 4 * kThreads) put(at, load_codes(m + at), load_codes(v + at), e[at / kGroup]);
+  for (; at + 4 <= end; at += 4 * kThreads) put(at, load_codes<STREAM>(m + at), load_codes<STREAM>(v + at), e[at / kGroup]);
   for (int u = 0; u < 4; ++u) {
     if (at + u >= end) break;
     const unsigned ex = e[at / kGroup];
@@ -365,6 +381,7 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 }
 
 // A square of a float is exact in double, and so squares of the largest and the smallest floats are neither infinite nor zero.
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void grad_norm_partial_kernel(AdamwList l, double* part) {
   __shared__ double red[kThreads / 64];
   const AdamwEntry& t = l.t[tensor_of(l, blockIdx.x)];
@@ -376,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void grad_norm_partial_kernel(AdamwList l
   for (; at + kBlockValues <= end; at += kBlockValues) {
     v4f q[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) q[u] = load4(g + at + u * (kBlockValues / 4) + 4 * threadIdx.x);
+    for (int u = 0; u < 4; ++u) q[u] = load4<STREAM>(g + at + u * (kBlockValues / 4) + 4 * threadIdx.x);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -392,6 +409,18 @@ __global__ __launch_bounds__(1024) void grad_norm_final_kernel(const double* par
   for (long long i = threadIdx.x; i < count; i += 1024) s += part[i];
   s = block_sum(s, red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+// Whether a list with this many bytes a value is more than the memory-side cache holds.
+bool streams(const AdamwTensor* t, int count, int bytes) {
+  long long n = 0;
+  for (int k = 0; k < count; ++k) n += t[k].n;
+  return n > kStreamBytes / bytes;
+}
+template <class F>
+void with(bool b, F&& f) {
+  if (b) f(std::true_type());
+  else f(std::false_type());
 }
 
 // Values that a block takes: so many that all tensors together make about `blocks` blocks, and at least kBlockValues.
@@ -439,10 +468,14 @@ hipError_t launch_adamw(const AdamwTensor* t, int count, const AdamwStep& st, hi
                        (float)(st.lr / c1), (float)(1.0 / c2), (float)st.max_norm,
                        mix_bits(mix_bits(st.seed) ^ (unsigned)st.step), st.norm};
   return over_tensors(t, count, st.lr, piece_of(t, count, kStepBlocks), [&](const AdamwList& l, long long pieces) {
-    // the root of a subnormal square is below 1.1e-19, less than half a unit in the last place of eps from 2e-12 on
-    if (st.bits == 8 && st.eps >= 2e-12) hipLaunchKernelGGL(adamw8_kernel<false>, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
-    else if (st.bits == 8) hipLaunchKernelGGL(adamw8_kernel<true>, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
-    else hipLaunchKernelGGL(adamw32_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, c);
+    const dim3 grid((unsigned)pieces);
+    with(streams(t, count, st.bits == 8 ? 10 : 16), [&](auto stream) {
+      constexpr bool S = decltype(stream)::value;
+      // the root of a subnormal square is below 1.1e-19, less than half a unit in the last place of eps from 2e-12 on
+      if (st.bits == 8 && st.eps >= 2e-12) hipLaunchKernelGGL((adamw8_kernel<false, S>), grid, dim3(kThreads), 0, s, l, c);
+      else if (st.bits == 8) hipLaunchKernelGGL((adamw8_kernel<true, S>), grid, dim3(kThreads), 0, s, l, c);
+      else hipLaunchKernelGGL(adamw32_kernel<S>, grid, dim3(kThreads), 0, s, l, c);
+    });
   });
 }
 
@@ -457,7 +490,9 @@ hipError_t launch_grad_norm(const AdamwTensor* t, int count, float* norm, void* 
   double* part = static_cast<double*>(ws);
   long long done = 0;
   const hipError_t e = over_tensors(t, count, 0.0, piece_of(t, count, kNormBlocks), [&](const AdamwList& l, long long pieces) {
-    hipLaunchKernelGGL(grad_norm_partial_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, part + done);
+    with(streams(t, count, 4), [&](auto stream) {
+      hipLaunchKernelGGL(grad_norm_partial_kernel<decltype(stream)::value>, dim3((unsigned)pieces), dim3(kThreads), 0, s, l, part + done);
+    });
     done += pieces;
   });
   if (e != hipSuccess) return e;
@@ -475,7 +510,9 @@ hipError_t launch_adamw_state_read(const AdamwTensor* t, int count, void* const*
       o[j].g = static_cast<const float*>(v_out[k + j]);
     }
     const hipError_t e = over_tensors(o, here, 0.0, piece_of(o, here, kStepBlocks), [&](const AdamwList& l, long long pieces) {
-      hipLaunchKernelGGL(adamw_read_kernel, dim3((unsigned)pieces), dim3(kThreads), 0, s, l);
+      with(streams(o, here, 6), [&](auto stream) {
+        hipLaunchKernelGGL(adamw_read_kernel<decltype(stream)::value>, dim3((unsigned)pieces), dim3(kThreads), 0, s, l);
+      });
     });
     if (e != hipSuccess) return e;
   }
