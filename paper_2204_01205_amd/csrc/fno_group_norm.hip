@@ -388,23 +388,30 @@ __global__ __launch_bounds__(kThreads) void norm_grad_sum_kernel(NormArgs a, con
   }
 }
 
-// A channel's parameter gradients, by a wave: sums over batch entries and pieces.  part[(b, c)][piece].
-__device__ __forceinline__ void param_grads(const NormArgs& a, int pieces, const double2* part, long long c, float* ggamma,
-                                            float* gbeta, int accumulate) {
-  if (c >= a.C) return;
-  double s1 = 0.0, s2 = 0.0;
+// A thread's share of a channel's parameter gradients: sums over batch entries and pieces.  part[(b, c)][piece].
+__device__ __forceinline__ void channel_share(const NormArgs& a, int pieces, const double2* part, long long c, int tid, int threads,
+                                              double& s1, double& s2) {
   const int count = a.B * pieces;
 #pragma unroll 8
-  for (int q = threadIdx.x & 63; q < count; q += 64) {
+  for (int q = tid; q < count; q += threads) {
     const int b = q / pieces;
     const double2 p = part[((long long)b * a.C + c) * pieces + (q - b * pieces)];
     s1 += p.x;
     s2 += p.y;
   }
-  wave_sum2(s1, s2);
-  if ((threadIdx.x & 63) != 0) return;
+}
+__device__ __forceinline__ void put_params(long long c, double s1, double s2, float* ggamma, float* gbeta, int accumulate) {
   if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + s1 : s1);
   if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + s2 : s2);
+}
+// The whole of it, by a wave
+__device__ __forceinline__ void param_grads(const NormArgs& a, int pieces, const double2* part, long long c, float* ggamma,
+                                            float* gbeta, int accumulate) {
+  if (c >= a.C) return;
+  double s1 = 0.0, s2 = 0.0;
+  channel_share(a, pieces, part, c, threadIdx.x & 63, 64, s1, s2);
+  wave_sum2(s1, s2);
+  if ((threadIdx.x & 63) == 0) put_params(c, s1, s2, ggamma, gbeta, accumulate);
 }
 // A thread's share of the sums of gamma gz and gamma gz xh over a group: thread `tid` of `threads`
 __device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const double2* part, const float* gamma, long long bg,
@@ -433,16 +440,23 @@ __device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const
 }
 
 constexpr int kFoldThreads = 1024;     // one block has a group's tens of thousands of sums to add
-// Blocks 0 .. groups - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the
-// parameters' gradients.
+__host__ __device__ __forceinline__ int fold_channels(int B, int pieces) { return B * pieces <= 512 ? kFoldThreads / 64 : 1; }
+// Blocks 0 .. groups - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the parameter
+// gradients of one channel, or, where the sums of a channel are few, of 16, a wave each.
 __global__ __launch_bounds__(kFoldThreads) void norm_grad_fold_kernel(NormArgs a, unsigned groups, const double2* part,
-                                                                  const float* gamma, float2* m, float* ggamma, float* gbeta,
-                                                                  int accumulate) {
+                                                                      const float* gamma, float2* m, float* ggamma, float* gbeta,
+                                                                      int accumulate) {
   __shared__ double red[2 * kFoldThreads / 64];
-  if (blockIdx.x >= groups)
+  double s1 = 0.0, s2 = 0.0;
+  if (blockIdx.x >= groups && fold_channels(a.B, a.pieces) > 1)
     return param_grads(a, a.pieces, part, (long long)(blockIdx.x - groups) * (kFoldThreads / 64) + (threadIdx.x >> 6), ggamma,
                        gbeta, accumulate);
-  double s1 = 0.0, s2 = 0.0;
+  if (blockIdx.x >= groups) {
+    channel_share(a, a.pieces, part, blockIdx.x - groups, threadIdx.x, kFoldThreads, s1, s2);
+    block_sum2(s1, s2, red);
+    if (threadIdx.x == 0) put_params(blockIdx.x - groups, s1, s2, ggamma, gbeta, accumulate);
+    return;
+  }
   group_share(a, a.pieces, part, gamma, blockIdx.x, threadIdx.x, kFoldThreads, s1, s2);
   block_sum2(s1, s2, red);
   if (threadIdx.x == 0) m[blockIdx.x] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
@@ -1033,12 +1047,8 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
   const int nw = (int)blockDim.x >> 6, P = (int)a.P;
   auto put = [&](int d, double t1, double t2) {
     const int c = g * a.D + d;
-    if (part != nullptr) {
-      part[(long long)b * a.C + c] = make_double2(t1, t2);
-    } else {
-      if (gbeta != nullptr) gbeta[c] = (float)(accumulate ? (double)gbeta[c] + t1 : t1);
-      if (ggamma != nullptr) ggamma[c] = (float)(accumulate ? (double)ggamma[c] + t2 : t2);
-    }
+    if (part != nullptr) part[(long long)b * a.C + c] = make_double2(t1, t2);
+    else put_params(c, t1, t2, ggamma, gbeta, accumulate);
   };
   if (2 * a.D <= nw) {
     const int waves = nw / a.D, d = (int)(threadIdx.x >> 6) / waves, w = (int)(threadIdx.x >> 6) % waves;
@@ -1184,7 +1194,10 @@ bool small_fits(const NormShape& n, bool adjoint) {
   return n.P > 0 && n.P <= most && n.P * (n.C / n.G) <= most && (!n.last || n.P * n.C * n.B <= 1 << 19);
 }
 // blocks of norm_grad_fold_kernel for the parameters' gradients
-unsigned fold_blocks(const NormShape& n) { return (unsigned)((n.C + kFoldThreads / 64 - 1) / (kFoldThreads / 64)); }
+unsigned fold_blocks(const NormShape& n, const NormArgs& a) {
+  const int channels = fold_channels(n.B, a.pieces);
+  return (unsigned)((n.C + channels - 1) / channels);
+}
 SmallArgs small_args(const NormShape& n, int V) {
   const int D = n.C / n.G;
   const unsigned by = n.last ? (unsigned)D : (unsigned)n.P;
@@ -1267,7 +1280,7 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
                          ggamma, gbeta, accumulate);
     });
     if (later)
-      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold_blocks(n)), dim3(kFoldThreads), 0, s, a, 0u, part, gamma, m, ggamma, gbeta,
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold_blocks(n, a)), dim3(kFoldThreads), 0, s, a, 0u, part, gamma, m, ggamma, gbeta,
                          accumulate);
     return hipGetLastError();
   }
@@ -1283,7 +1296,7 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   const float2* means = inside ? nullptr : m;
   auto fold = [&] {
     if (!inside)
-      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? fold_blocks(n) : 0)), dim3(kFoldThreads), 0, s, a, groups, part,
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? fold_blocks(n, a) : 0)), dim3(kFoldThreads), 0, s, a, groups, part,
                          gamma, m, ggamma, gbeta, accumulate);
   };
   with(streams(n, 2), [&](auto stream) {
