@@ -215,52 +215,41 @@ struct Group8 {
   v4f p, g;
   unsigned m, v, e;    // codes; exponents, m's in the low byte
 };
-// N blocks together, so that their chains of dependent steps go side by side.  FINE: square root and quotient to the last
-// bit; otherwise by the instructions that are good to one unit in the last place and take subnormal squares for zero.
-template <int N, bool FINE>
-__device__ __forceinline__ void groups_step(const AdamwScalars& c, float keep, float scale, const unsigned (&block)[N], int lane,
-                                            Group8 (&q)[N]) {
-  float mi[N][4], vi[N][4];
-  unsigned top_m[N], top_v[N];
+// FINE: square root and quotient to the last bit; otherwise by the instructions that are good to one unit in the last place and
+// take subnormal squares for zero.
+template <bool FINE>
+__device__ __forceinline__ void group_step(const AdamwScalars& c, float keep, float scale, unsigned block, int lane, Group8& q) {
+  const unsigned em = q.e & 255u, ev = q.e >> 8;
+  float mi[4], vi[4];
+  unsigned top_m = 0, top_v = 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const unsigned em = q[k].e & 255u, ev = q[k].e >> 8;
-    top_m[k] = top_v[k] = 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float m = decode_m((q[k].m >> (8 * u)) & 255u, em), v = decode_v((q[k].v >> (8 * u)) & 255u, ev);
-      moments(c, q[k].g[u] * scale, m, v);
-      if (FINE) q[k].p[u] = updated(c, keep, q[k].p[u], m, v);
-      else q[k].p[u] = q[k].p[u] * keep - c.lr1 * m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v * c.ic2) + c.eps);
-      top_m[k] = max(top_m[k], __builtin_bit_cast(unsigned, m) & 0x7FFFFFFFu);
-      top_v[k] = max(top_v[k], __builtin_bit_cast(unsigned, v));
-      mi[k][u] = m;
-      vi[k][u] = v;
-    }
+  for (int u = 0; u < 4; ++u) {
+    float m = decode_m((q.m >> (8 * u)) & 255u, em), v = decode_v((q.v >> (8 * u)) & 255u, ev);
+    moments(c, q.g[u] * scale, m, v);
+    if (FINE) q.p[u] = updated(c, keep, q.p[u], m, v);
+    else q.p[u] = q.p[u] * keep - c.lr1 * m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v * c.ic2) + c.eps);
+    top_m = max(top_m, __builtin_bit_cast(unsigned, m) & 0x7FFFFFFFu);
+    top_v = max(top_v, __builtin_bit_cast(unsigned, v));
+    mi[u] = m;
+    vi[u] = v;
   }
+  const unsigned nm = shared_exponent(wave_max(top_m), kSpanM), nv = shared_exponent(wave_max(top_v), kSpanV);
+  const Scale8 sm = scale_of(nm, kSpanM), sv = scale_of(nv, kSpanV);
+  q.m = 0;
+  q.v = 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    top_m[k] = wave_max(top_m[k]);
-    top_v[k] = wave_max(top_v[k]);
+  for (int u = 0; u < 4; ++u) {
+    const unsigned r = mix_bits(block + (unsigned)(4 * lane + u) * 0x9E3779B1u);
+    q.m |= encode_m(mi[u], sm, r & 0xFFFFu) << (8 * u);
+    q.v |= encode_v(vi[u], sv, r >> 16) << (8 * u);
   }
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const unsigned nm = shared_exponent(top_m[k], kSpanM), nv = shared_exponent(top_v[k], kSpanV);
-    const Scale8 sm = scale_of(nm, kSpanM), sv = scale_of(nv, kSpanV);
-    unsigned cm = 0, cv = 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const unsigned r = mix_bits(block[k] + (unsigned)(4 * lane + u) * 0x9E3779B1u);
-      cm |= encode_m(mi[k][u], sm, r & 0xFFFFu) << (8 * u);
-      cv |= encode_v(vi[k][u], sv, r >> 16) << (8 * u);
-    }
-    q[k].m = nm == 255u ? 0u : cm;
-    q[k].v = nv == 255u ? 0u : cv;
-    q[k].e = nm | nv << 8;
-  }
+  if (nm == 255u) q.m = 0;             // (the same in all lanes)
+  if (nv == 255u) q.v = 0;
+  q.e = nm | nv << 8;
 }
 
-// A wave takes four blocks of 256 values at a time, all asked for before the first is used.
+// A wave takes four blocks of 256 values at a time, all asked for before the first is used, each stored when it is done (354 M
+// values, with norm and read: 1.52 ms; all four worked side by side and stored together 1.55).
 template <bool FINE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScalars c) {
   const int k = tensor_of(l, blockIdx.x);
@@ -277,7 +266,6 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
   long long at = begin + wave * (kBlockValues / 4);
   for (; at + 4 * kGroup <= end; at += kBlockValues) {
     Group8 q[4];
-    unsigned block[4];
     const long long b0 = at / kGroup;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -287,12 +275,11 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
       q[u].m = load_codes<STREAM>(m + i);
       q[u].v = load_codes<STREAM>(v + i);
       q[u].e = e[b0 + u];
-      block[u] = random_of(b0 + u);
     }
-    groups_step<4, FINE>(c, t.keep, scale, block, lane, q);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const long long i = at + u * kGroup + 4 * lane;
+      group_step<FINE>(c, t.keep, scale, random_of(b0 + u), lane, q[u]);
       store4<STREAM>(t.p + i, q[u].p);
       store_codes<STREAM>(m + i, q[u].m);
       store_codes<STREAM>(v + i, q[u].v);
@@ -302,8 +289,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
   // the tensor's last blocks, the very last one cut: values past the end are zeros that nobody stores
   const long long stop = at + kBlockValues / 4 < end ? at + kBlockValues / 4 : end;
   for (; at < stop; at += kGroup) {
-    Group8 one[1] = {};
-    Group8& q = one[0];
+    Group8 q{};
     const long long i = at + 4 * lane;
     q.e = e[at / kGroup];
 #pragma unroll
@@ -314,8 +300,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(AdamwList l, AdamwScal
       q.m |= (unsigned)m[i + u] << (8 * u);
       q.v |= (unsigned)v[i + u] << (8 * u);
     }
-    const unsigned block[1] = {random_of(at / kGroup)};
-    groups_step<1, FINE>(c, t.keep, scale, block, lane, one);
+    group_step<FINE>(c, t.keep, scale, random_of(at / kGroup), lane, q);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (i + u >= end) continue;
