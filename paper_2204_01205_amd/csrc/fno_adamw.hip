@@ -1,5 +1,16 @@
 // One AdamW step over the tensors of a list with moments in 32 or 8 bits, the norm of their gradients, and what 8-bit
 // moments stand for.
+//
+// All three are bound by memory: a step reads 16 and writes 12 bytes a value, with 8-bit moments 10 and 6.  The addresses of
+// up to 64 tensors go with a launch's arguments, so that a list of small tensors is one launch and no table has to be kept in
+// step with the gradients' addresses; a block takes 4096 values of one tensor in memory order.  354 million parameters (four
+// blocks of 20 channels at 24 x 24 x 24 x 8 modes): 32 bits 1.71 ms (5.8 TB/s), 8 bits 0.97 (5.8), norm 0.21 (6.6), read of the
+// 8-bit moments 0.34 (6.2); longer stretches a block 1.87 to 1.95 (32 bits), plain instead of nontemporal accesses 1.84.
+//
+// 8-bit moments: 256 consecutive values, four to a lane of one wave, share a power of two for each moment; a code is a small
+// float relative to it.  v spans 31 powers below the largest of its block and m 15 (v is a square), both in steps of an
+// eighth.  An average of decay 0.999 moves by a hundredth of such a step at a time, so that rounding to nearest would leave it
+// where it is; with the bits of a float, rounding at random is one addition before the cut.
 #include "fno_device.h"
 
 #include <type_traits>

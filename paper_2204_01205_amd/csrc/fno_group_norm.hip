@@ -7,6 +7,11 @@
 // sweep that writes.  The statistics come from d = x - k, mean = k + E d, var = E d^2 - (E d)^2, k the middle one of three of
 // the group's values, so that values far from zero lose nothing, one that is far from the others does no harm as k, and a
 // constant group has the variance zero.  Four or eight terms are added in float, everything else in double.
+//
+// Measured, with the bytes that the launches move (x twice; adjoint x and gy twice) at a copy's 6.2 TB/s in brackets: 60 x 60 x
+// 64 x 30 points, 20 channels, forward 262 us (268); 64 x 64 x 64 x 20, 32 channels last, 324 (325); 128 x 128 x 64 x 32, 20
+// channels, adjoint 2.09 ms (2.16).  bf16, adjoint of 2 x 64 x 64 x 64 x 16, 20 channels last: 340 us (270), the vector unit has
+// 26 instructions a value, two of them transcendental.  Fields of a few MB: launches of 3 to 10 us each.
 #include "fno_device.h"
 
 #include <climits>
