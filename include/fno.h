@@ -279,9 +279,9 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
  * a block share, m's and v's.  With E the exponent, a code's lower three bits f and the bits e above them stand for
  * (1 + f / 8) 2^(e + E - 127 - K), code 0 for zero: v has no sign, five bits e and K = 31; m has its sign in bit 7, four bits
  * e and K = 15.  All bytes zero are moments of zero.  E = 255 (its codes are 0): a value of the block was not finite, and every
- * one of it is NaN from then on.  The update uses the new moments before they are rounded.  They are rounded up or down at random with the
- * odds that keep the mean (a decay of 0.1 % a step would never move a code otherwise), by a hash of seed, step, the tensor's
- * place in the list and the value's place in it: the same bits on every run.  A v that is not zero is at least the smallest
+ * one of it is NaN from then on.  The update uses the new moments before they are rounded.  They are rounded up or down at
+ * random with the odds that keep the mean (a decay of 0.1 % a step would never move a code otherwise), by a hash of seed, step,
+ * the tensor's place in the list and the value's place in it: the same bits on every run.  A v that is not zero is at least the smallest
  * code, so that no step is divided by a vanished v.
  *
  * tensors: host array, read during the call only; every pointer in it is a device pointer, param, grad, m and v 4-byte
@@ -306,7 +306,8 @@ int fno_grad_norm_workspace_bytes(int32_t count, const fno_adamw_tensor* tensors
 int fno_grad_norm(int32_t count, const fno_adamw_tensor* tensors, float* norm, void* ws, size_t ws_bytes, void* stream);
 
 /* The values that moments in 8 bits stand for, as bf16, which every code is exactly: m_out[k], v_out[k] (host arrays of
- * `count` device pointers) receive n bf16 values of tensor k.  param and grad are not used. */
+ * `count` device pointers, 4-byte aligned, null only where n = 0) receive n bf16 values of tensor k.  param and grad are not
+ * used. */
 int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* const* m_out, void* const* v_out,
                          void* stream);
 
