@@ -989,7 +989,8 @@ __global__ __launch_bounds__(1024) void norm_small_kernel(NormArgs a, SmallArgs 
   const int b = blockIdx.x / a.G, g = blockIdx.x % a.G;
   float v[kSmallValues];
   small_load<T, LAST>(a, s, b, g, x, v);
-  const float first = load1(x + small_at<LAST>(a, s, b, g, 0));
+  // k is the group's first value, whatever it is: differences and their squares are formed in double
+  const double first = load1(x + small_at<LAST>(a, s, b, g, 0));
   double sum = 0.0, square = 0.0;
   small_values<T>(s, [&](int k, int) {
     const double d = v[k] - first;
