@@ -4,9 +4,14 @@
 // What the operator moves bounds it: x in and y out (adjoint: x and gy in, gx out), 20 to 40 operations a value.  The
 // statistics (adjoint: the sums) of a group need all of it before its first output, so a group that does not fit one
 // block's registers is read twice: sums of pieces, a small launch that adds the pieces' sums in a fixed order, and the
-// sweep that writes.  The statistics come from d = x - k, mean = k + E d, var = E d^2 - (E d)^2, k the middle one of three of
-// the group's values, so that values far from zero lose nothing, one that is far from the others does no harm as k, and a
-// constant group has the variance zero.  Four or eight terms are added in float, everything else in double.
+// sweep that writes.
+//
+// Statistics: a block takes mean and variance of its piece from d = x - k, mean = k + E d, var = E d^2 - (E d)^2, k the piece's
+// first value (of the group), and the pieces are put together by var = E (var_j + (mean_j - mean)^2), about the mean of the first
+// one.  k is one of the N values it is subtracted from, so that (E d)^2 <= N var: what the subtraction of the squares can lose is a
+// factor N of a piece, which double has to spare, whatever k is and wherever the group lies (with the squares in float, a
+// constant field with zeros at its corners had rstd off by 1e-2).  Differences and squares are formed in double too: no float
+// is too large or too small for them.  Adjoint: four or eight terms are added in float, everything else in double.
 //
 // Measured, with the bytes that the launches move (x twice; adjoint x and gy twice) at a copy's 6.2 TB/s in brackets: 60 x 60 x
 // 64 x 30 points, 20 channels, forward 262 us (268); 64 x 64 x 64 x 20, 32 channels last, 324 (325); 128 x 128 x 64 x 32, 20
@@ -99,17 +104,34 @@ struct NormArgs {
   int pieces;           // blocks of a range
   int run;              // tiles of a stretch
 };
+// How ranges were cut into pieces for the statistics.  A range: channels first the values of a group, channels last all of a
+// batch entry; begin: where it starts, counted from an aligned base.
+struct Cut {
+  long long range, stretch;      // values of a range, and of a piece
+  double inv;                    // 1 / range
+  int pieces;
+  int align;                     // pieces start at multiples of this; what lies before and behind belongs to the first one
+};
+__device__ __forceinline__ long long piece_values(const Cut& c, long long begin, int j) {
+  long long head = -begin & (c.align - 1);
+  if (head > c.range) head = c.range;
+  const long long whole = (c.range - head) & -(long long)c.align;
+  long long v = whole - j * c.stretch;
+  v = v < 0 ? 0 : v > c.stretch ? c.stretch : v;
+  return j == 0 ? v + (c.range - whole) : v;
+}
 
 // What a group's values go through: xh = (x - mean) rstd with the mean in two floats, so that x - hi is exact near it.
 struct Stat {
   float hi, lo, rstd, pad;
 };
-__device__ __forceinline__ Stat stat_of(double k, double sum, double square, const NormArgs& a, float* mean, float* rstd,
-                                        long long at) {
-  const double off = sum * a.inv_n, mu = k + off;
-  double var = square * a.inv_n - off * off;
-  if (var < 0.0) var = 0.0;                              // (a NaN stays one)
-  const double rs = 1.0 / sqrt(var + a.eps);
+// mean and variance of values of which d = x - k has the mean `off` and d^2 the mean `square`
+__device__ __forceinline__ double2 moments_of(double k, double off, double square) {
+  const double var = square - off * off;
+  return make_double2(k + off, var < 0.0 ? 0.0 : var);   // (a NaN stays one)
+}
+__device__ __forceinline__ Stat stat_of(double2 moments, double eps, float* mean, float* rstd, long long at) {
+  const double mu = moments.x, rs = 1.0 / sqrt(moments.y + eps);
   if (mean != nullptr) mean[at] = (float)mu;
   if (rstd != nullptr) rstd[at] = (float)rs;
   Stat s;
@@ -175,77 +197,70 @@ __device__ __forceinline__ void sweep(long long begin, long long end, int tid, i
 // piece of one row (one channel), or whole short rows wave by wave, where gamma and beta come in.
 // ------------------------------------------------------------------------------------------
 
-// The value k of group g of batch entry b
-template <class T, bool LAST>
-__device__ __forceinline__ float middle_of(const NormArgs& a, const T* x, long long b, int g) {
-  if (a.P == 0) return 0.f;
-  const long long c0 = g * a.D, c1 = c0 + a.D / 2, c2 = c0 + a.D - 1, p1 = a.P / 2, p2 = a.P - 1;
-  const float u = load1(LAST ? x + b * a.P * a.C + c0 : x + (b * a.C + c0) * a.P);
-  const float v = load1(LAST ? x + (b * a.P + p1) * a.C + c1 : x + (b * a.C + c1) * a.P + p1);
-  const float w = load1(LAST ? x + (b * a.P + p2) * a.C + c2 : x + (b * a.C + c2) * a.P + p2);
-  return __builtin_amdgcn_fmed3f(u, v, w);
-}
-
-// part[(bg, piece)] = (sum d, sum d^2); stat[bg].hi = k, for the launches that follow, which may write over x
+// part[(bg, piece)] = mean and variance of the piece's values
 template <class T, bool STREAM>
-__global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs a, const T* x, double2* part, Stat* stat) {
+__global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs a, Cut cut, const T* x, double2* part) {
   constexpr int V = kVec<T>, U = 4;
   __shared__ double red[2 * kThreads / 64];
-  const long long bg = blockIdx.x / a.pieces, j = blockIdx.x % a.pieces, n = a.P * a.D;
-  const float middle = middle_of<T, false>(a, x, bg / a.G, (int)(bg % a.G));
+  const long long bg = blockIdx.x / a.pieces, begin = bg * cut.range;
+  const int j = blockIdx.x % a.pieces;
+  const long long count = piece_values(cut, begin, j);
+  const double k = count > 0 ? load1(x + (j == 0 ? begin : (begin + V - 1) / V * V + j * cut.stretch)) : 0.f;
   double s = 0.0, q = 0.0;
-  auto add = [&](pack<T> k) {
-    float v[V], d = 0.f, e = 0.f;
-    unpack(k, v);
-#pragma unroll
-    for (int u = 0; u < V; ++u) {
-      const float w = v[u] - middle;
-      d += w;
-      e = fmaf(w, w, e);
-    }
+  auto add1 = [&](float v) {
+    const double d = v - k;
     s += d;
-    q += e;
+    q = fma(d, d, q);
   };
-  sweep<V, U>(bg * n, (bg + 1) * n, threadIdx.x, kThreads, j * a.run, 1, a.run,
+  auto add = [&](pack<T> p) {
+    float v[V];
+    unpack(p, v);
+#pragma unroll
+    for (int u = 0; u < V; ++u) add1(v[u]);
+  };
+  sweep<V, U>(begin, begin + cut.range, threadIdx.x, kThreads, (long long)j * a.run, 1, a.run,
               [&](long long at, long long step) {
-                pack<T> k[U];
+                pack<T> p[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) k[u] = load_pack<STREAM>(x + at + u * step);
+                for (int u = 0; u < U; ++u) p[u] = load_pack<STREAM>(x + at + u * step);
 #pragma unroll
-                for (int u = 0; u < U; ++u) add(k[u]);
+                for (int u = 0; u < U; ++u) add(p[u]);
               },
               [&](long long at) { add(load_pack<STREAM>(x + at)); },
-              [&](long long at) {
-                const double d = load1(x + at) - middle;
-                s += d;
-                q = fma(d, d, q);
-              });
+              [&](long long at) { add1(load1(x + at)); });
   block_sum2(s, q, red);
-  if (threadIdx.x != 0) return;
-  part[bg * a.pieces + j] = make_double2(s, q);
-  if (j == 0) stat[bg].hi = middle;
+  const double inv = count > 0 ? 1.0 / (double)count : 0.0;
+  if (threadIdx.x == 0) part[bg * a.pieces + j] = moments_of(k, s * inv, q * inv);
 }
 
-// The statistics of group bg from its pieces' sums, in every thread of a block; red: as for block_sum2.
-__device__ __forceinline__ Stat block_stat(const NormArgs& a, int pieces, const Stat* stat, const double2* part, long long bg,
+// A thread's share of the sums that give a range's moments about the mean of its first piece; part: the range's pieces.
+__device__ __forceinline__ void piece_share(const Cut& c, long long begin, const double2* part, int tid, int threads, double& s,
+                                            double& q) {
+  const double k = part[0].x;
+  for (int j = tid; j < c.pieces; j += threads) {
+    const double2 p = part[j];
+    const double w = (double)piece_values(c, begin, j), d = p.x - k;
+    s = fma(w, d, s);
+    q = fma(w, fma(d, d, p.y), q);
+  }
+}
+// The statistics of group bg from its pieces, in every thread of a block; red: as for block_sum2.
+__device__ __forceinline__ Stat block_stat(const NormArgs& a, const Cut& c, long long begin, const double2* part, long long bg,
                                            float* mean, float* rstd, double* red) {
   double s = 0.0, q = 0.0;
-  for (int j = threadIdx.x; j < pieces; j += kThreads) {
-    const double2 p = part[bg * pieces + j];
-    s += p.x;
-    q += p.y;
-  }
+  part += bg * c.pieces;
+  piece_share(c, begin, part, threadIdx.x, kThreads, s, q);
   block_sum2(s, q, red);
-  return stat_of(stat[bg].hi, s, q, a, mean, rstd, bg);
+  return stat_of(moments_of(part[0].x, s * c.inv, q * c.inv), a.eps, mean, rstd, bg);
 }
 
-// Adds the pieces of every (b, g), a group a block.
-__global__ __launch_bounds__(kThreads) void norm_stat_kernel(NormArgs a, const double2* part, Stat* stat, float* mean, float* rstd) {
+// Puts the pieces of every (b, g) together, a group a block.
+__global__ __launch_bounds__(kThreads) void norm_stat_kernel(NormArgs a, Cut cut, const double2* part, Stat* stat, float* mean,
+                                                             float* rstd) {
   __shared__ double red[2 * kThreads / 64];
   const bool tells = threadIdx.x == 0;
   const long long bg = blockIdx.x;
-  const Stat s = block_stat(a, a.pieces, stat, part, bg, tells ? mean : nullptr, tells ? rstd : nullptr, red);
-  __syncthreads();
+  const Stat s = block_stat(a, cut, bg * cut.range, part, bg, tells ? mean : nullptr, tells ? rstd : nullptr, red);
   if (tells) stat[bg] = s;
 }
 
@@ -286,11 +301,11 @@ __device__ __forceinline__ void apply_range(const Affine& f, const T* x, T* y, l
               [&](long long at) { store1(y + at, normed<ACT>(f, load1(x + at))); });
 }
 
-// A piece of a row per block; short: a row per wave.  part: the sums of the group's `parts` pieces, few enough for every
-// block to add them itself (null: the statistics are in `stat`).
+// A piece of a row per block; short: a row per wave.  part: the moments of the groups' pieces, few enough for every block to put
+// its group's together itself (null: the statistics are in `stat`).
 template <class T, int ACT, bool SHORT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, const T* x, const float* gamma, const float* beta,
-                                                              const Stat* stat, const double2* part, int parts, float* mean,
+                                                              const Stat* stat, const double2* part, Cut cut, float* mean,
                                                               float* rstd, T* y) {
   __shared__ double red[2 * kThreads / 64];
   const long long row = SHORT ? (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6) : blockIdx.x / a.pieces;
@@ -300,7 +315,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, const 
   Stat st;
   if (!SHORT && part != nullptr) {
     const bool tells = j == 0 && c % a.D == 0 && threadIdx.x == 0;
-    st = block_stat(a, parts, stat, part, row / a.D, tells ? mean : nullptr, tells ? rstd : nullptr, red);
+    st = block_stat(a, cut, row / a.D * cut.range, part, row / a.D, tells ? mean : nullptr, tells ? rstd : nullptr, red);
   } else {
     st = stat[row / a.D];
   }
@@ -602,62 +617,43 @@ __device__ __forceinline__ double2* channel_sums(double2* lds, int rows, int C) 
   return sums;
 }
 
-// part[(b, g)][piece] = (sum d, sum d^2); stat[(b, g)].hi = k
+// part[(b, g)][piece] = mean and variance of the group's values in the piece
 template <class T, bool STREAM>
-__global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int active, const T* x, double2* part, Stat* stat) {
+__global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, Cut cut, int active, const T* x, double2* part) {
   constexpr int V = kVec<T>, U = 4;
   extern __shared__ double2 pairs[];
-  __shared__ float middles[kMaxNormChannels];
+  __shared__ float firsts[kMaxNormChannels];
   const int b = (int)blockIdx.x / a.pieces, j = blockIdx.x % a.pieces;
-  const long long base = (long long)b * a.P * a.C;
-  double s[V], q[V];
-  float middle[V];
-  for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
-    middles[g] = middle_of<T, true>(a, x, b, g);
-    if (j == 0) stat[(long long)b * a.G + g].hi = middles[g];
-  }
+  const long long base = (long long)b * cut.range;
+  const double count = (double)(piece_values(cut, 0, j) / a.G);        // of every group
+  double s[V], q[V], k[V];
+  for (int g = threadIdx.x; g < a.G; g += blockDim.x) firsts[g] = count > 0.0 ? load1(x + base + j * cut.stretch + g * a.D) : 0.f;
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < V; ++u) {
     s[u] = q[u] = 0.0;
-    middle[u] = middles[((int)threadIdx.x * V + u) % a.C / a.D];
+    k[u] = firsts[((int)threadIdx.x * V + u) % a.C / a.D];
   }
   auto add1 = [&](int u, float v) {
-    const double d = v - middle[u];
+    const double d = v - k[u];
     s[u] += d;
     q[u] = fma(d, d, q[u]);
   };
-  sweep_last<V, U>(base, base + a.P * a.C, active, (long long)j * a.run, 1, a.run,
+  auto add = [&](pack<T> p) {
+    float v[V];
+    unpack(p, v);
+#pragma unroll
+    for (int u = 0; u < V; ++u) add1(u, v[u]);
+  };
+  sweep_last<V, U>(base, base + cut.range, active, (long long)j * a.run, 1, a.run,
                    [&](long long at, long long step) {
-                     pack<T> k[U];
+                     pack<T> p[U];
 #pragma unroll
-                     for (int u = 0; u < U; ++u) k[u] = load_any<STREAM>(x + at + u * step);
-                     float d[V], e[V];
+                     for (int u = 0; u < U; ++u) p[u] = load_any<STREAM>(x + at + u * step);
 #pragma unroll
-                     for (int w = 0; w < V; ++w) d[w] = e[w] = 0.f;
-#pragma unroll
-                     for (int u = 0; u < U; ++u) {
-                       float v[V];
-                       unpack(k[u], v);
-#pragma unroll
-                       for (int w = 0; w < V; ++w) {
-                         const float f = v[w] - middle[w];
-                         d[w] += f;
-                         e[w] = fmaf(f, f, e[w]);
-                       }
-                     }
-#pragma unroll
-                     for (int w = 0; w < V; ++w) {
-                       s[w] += d[w];
-                       q[w] += e[w];
-                     }
+                     for (int u = 0; u < U; ++u) add(p[u]);
                    },
-                   [&](long long at) {
-                     float v[V];
-                     unpack(load_any<STREAM>(x + at), v);
-#pragma unroll
-                     for (int w = 0; w < V; ++w) add1(w, v[w]);
-                   },
+                   [&](long long at) { add(load_any<STREAM>(x + at)); },
                    [&](long long at, int u) {
                      const float v = load1(x + at);
 #pragma unroll
@@ -670,6 +666,8 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
   }
   const double2* const sums = channel_sums(pairs, active * V / a.C, a.C);
   double2* const to = part + (long long)b * a.G * a.pieces + j;
+  const double inv = count > 0.0 ? 1.0 / count : 0.0;
+  auto put = [&](int g, double2 m) { to[(long long)g * a.pieces] = moments_of(firsts[g], m.x * inv, m.y * inv); };
   if (a.D <= 32) {
     for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
       double2 m = sums[g * a.D];
@@ -677,7 +675,7 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
         m.x += sums[g * a.D + d].x;
         m.y += sums[g * a.D + d].y;
       }
-      to[(long long)g * a.pieces] = m;
+      put(g, m);
     }
   } else {
     for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
@@ -687,17 +685,17 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, int act
         m.y += sums[g * a.D + d].y;
       }
       wave_sum2(m.x, m.y);
-      if ((threadIdx.x & 63) == 0) to[(long long)g * a.pieces] = m;
+      if ((threadIdx.x & 63) == 0) put(g, m);
     }
   }
 }
 
-// part: the sums of the batch entry's pieces, few enough for every block to add them itself, a group a wave (null: the
+// part: the moments of the pieces, few enough for every block to put its batch entry's together itself, a group a wave (null: the
 // statistics are in `stat`).  (Those in LDS and those in memory are read in two ways: one pointer for both would have to be
 // moved out of its LDS array for batch entries after the first.)
 template <class T, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int active, const T* x, const float* gamma,
-                                                               const float* beta, const Stat* stat, const double2* part, int parts,
+                                                               const float* beta, const Stat* stat, const double2* part, Cut cut,
                                                                float* mean, float* rstd, T* y) {
   constexpr int V = kVec<T>, U = 4;
   extern __shared__ double lds[];
@@ -707,14 +705,12 @@ __global__ __launch_bounds__(1024) void norm_last_apply_kernel(NormArgs a, int a
     const bool tells = j == 0 && (threadIdx.x & 63) == 0;
     for (int g = threadIdx.x >> 6; g < a.G; g += blockDim.x >> 6) {
       const long long bg = (long long)b * a.G + g;
+      const double2* const mine_of = part + bg * cut.pieces;
       double s = 0.0, q = 0.0;
-      for (int k = threadIdx.x & 63; k < parts; k += 64) {
-        const double2 p = part[bg * parts + k];
-        s += p.x;
-        q += p.y;
-      }
+      piece_share(cut, 0, mine_of, threadIdx.x & 63, 64, s, q);
       wave_sum2(s, q);
-      const Stat st = stat_of(stat[bg].hi, s, q, a, tells ? mean : nullptr, tells ? rstd : nullptr, bg);
+      const Stat st = stat_of(moments_of(mine_of[0].x, s * cut.inv, q * cut.inv), a.eps, tells ? mean : nullptr,
+                              tells ? rstd : nullptr, bg);
       if ((threadIdx.x & 63) == 0) mine[g] = st;
     }
     __syncthreads();
@@ -999,7 +995,8 @@ __global__ __launch_bounds__(1024) void norm_small_kernel(NormArgs a, SmallArgs 
   });
   block_sum2(sum, square, red);
   const bool tells = threadIdx.x == 0;
-  const Stat st = stat_of(first, sum, square, a, tells ? mean : nullptr, tells ? rstd : nullptr, blockIdx.x);
+  const Stat st = stat_of(moments_of(first, sum * a.inv_n, square * a.inv_n), a.eps, tells ? mean : nullptr, tells ? rstd : nullptr,
+                          blockIdx.x);
   for (int d = threadIdx.x; d < a.D; d += blockDim.x) {
     const Affine f = affine_of(st, gamma ? gamma[g * a.D + d] : 1.f, beta ? beta[g * a.D + d] : 0.f);
     affine[d] = make_float2(f.scale, f.shift);
@@ -1165,6 +1162,14 @@ NormArgs cut_points(const NormShape& n, int fields, long long blocks, int tiles_
   return a;
 }
 
+// The cuts of cut_groups() and, channels last, of cut_points(): piece j starts behind j stretches of whole tiles.
+Cut cut_of(const NormShape& n, const NormArgs& a) {
+  const long long range = n.last ? n.P * n.C : n.P * a.D;
+  const int V = n.bf16 ? 8 : 4;
+  const long long tile = n.last ? (long long)active_threads(n.C, V) * V * 4 : tile_values(n, 1);
+  return Cut{range, a.run * tile, range > 0 ? 1.0 / (double)range : 0.0, a.pieces, n.last ? 1 : V};
+}
+
 // LDS of the channels-last sums: a pair for every value of the active threads, one more for every thread or channel
 size_t pair_bytes(const NormShape& n, int active, int threads) {
   return ((size_t)active * (n.bf16 ? 8 : 4) + (threads > n.C ? threads : n.C)) * sizeof(double2);
@@ -1241,28 +1246,31 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     const NormArgs a = cut_points(n, 1, kSumBlocks / 2, 3), out = cut_points(n, 1, kApplyLast, 1);
     const int active = active_threads(n.C, kVec<T>), threads = (active + 63) / 64 * 64;
     const bool inside = n.P > 0 && inline_parts(n, (long long)n.G * a.pieces);
+    const Cut cut = cut_of(n, a);
     const dim3 grid((unsigned)(n.B * a.pieces));
     with(hint, [&](auto stream) {
       constexpr bool S = decltype(stream)::value;
-      hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), pair_bytes(n, active, threads), s, a, active, x, part, stat);
-      if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
+      hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), pair_bytes(n, active, threads), s, a, cut, active, x,
+                         part);
+      if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, cut, part, stat, mean, rstd);
       if (n.P > 0)
         hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT, S>), dim3((unsigned)(n.B * out.pieces)), dim3(threads),
-                           inside ? n.G * sizeof(Stat) : 0, s, out, active, x, gamma, beta, stat, inside ? part : nullptr, a.pieces, mean,
+                           inside ? n.G * sizeof(Stat) : 0, s, out, active, x, gamma, beta, stat, inside ? part : nullptr, cut, mean,
                            rstd, y);
     });
     return hipGetLastError();
   }
   const NormArgs a = cut_groups(n);
+  const Cut cut = cut_of(n, a);
   const bool short_rows = n.P < kShortRow, inside = !short_rows && inline_parts(n, a.pieces);
   const NormArgs rows = cut_rows(n, 1, inside ? kApplyInside : kApplyBlocks);
   with(hint, [&](auto stream) {
     constexpr bool S = decltype(stream)::value;
-    hipLaunchKernelGGL((norm_sum_kernel<T, S>), dim3((unsigned)(n.B * n.G * a.pieces)), dim3(kThreads), 0, s, a, x, part, stat);
-    if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, part, stat, mean, rstd);
+    hipLaunchKernelGGL((norm_sum_kernel<T, S>), dim3((unsigned)(n.B * n.G * a.pieces)), dim3(kThreads), 0, s, a, cut, x, part);
+    if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, cut, part, stat, mean, rstd);
     with(short_rows, [&](auto short_) {
       hipLaunchKernelGGL((norm_apply_kernel<T, ACT, decltype(short_)::value, S>), dim3(row_blocks(rows, short_rows)), dim3(kThreads), 0, s,
-                         rows, x, gamma, beta, stat, inside ? part : nullptr, a.pieces, mean, rstd, y);
+                         rows, x, gamma, beta, stat, inside ? part : nullptr, cut, mean, rstd, y);
     });
   });
   return hipGetLastError();

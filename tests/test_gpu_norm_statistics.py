@@ -25,3 +25,75 @@ def test_one_value_far_from_all_others(c, groups, p, far, rest, where, dtype, la
     y, mean, rstd = n.forward()
     n.check_forward(y, mean, rstd)
     n.check_backward(mean, rstd, *n.backward(mean, rstd))
+
+
+SHAPES = [(1, 1, 1, 1 << 20), (1, 4, 2, 1 << 18), (2, 6, 2, 70001), (1, 3, 1, 5000011), (3, 20, 5, 9999), (1, 512, 4, 300)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rest,spread,corner", [(1000.1, 0.0, 0.0), (1000.1, 0.1, 0.0), (300.0, 1.0, 0.0), (1000.0, 4.0, 0.3), (-7e4, 0.0, 1.0)])
+@pytest.mark.parametrize("b,c,groups,p", SHAPES)
+def test_corners_unlike_the_rest(b, c, groups, p, rest, spread, corner, dtype, layout):
+    """Padding, boundary layers, inactive cells: the first and the last point, then the middle one too, far from all others,
+    which are (nearly) constant."""
+    n = Norm(b, c, groups, p, layout, dtype, "identity")
+    rng = np.random.default_rng(4)
+    n.x = rounded(rest + spread * rng.standard_normal((b, c, p)))
+    n.x[:, :, [0, -1]] = rounded(corner)
+    for _ in range(2):
+        y, mean, rstd = n.forward()
+        n.check_forward(y, mean, rstd)
+        n.x[:, :, p // 2] = rounded(corner)
+    y, mean, rstd = n.forward()
+    n.check_backward(mean, rstd, *n.backward(mean, rstd))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("p", [1000, 300007])
+def test_a_field_that_jumps(layout, p):
+    """Halves at 0 and at 1000, each with a small spread, and a ramp: pieces whose means are far apart."""
+    rng = np.random.default_rng(6)
+    for base in (np.where(np.arange(p) < p // 2, 0.0, 1000.0), np.linspace(-2000, 5000, p)):
+        n = Norm(2, 4, 2, p, layout, act="identity")
+        n.x = (base + 0.01 * rng.standard_normal((2, 4, p))).astype(np.float32)
+        n.check_forward(*n.forward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("power", [-100, -83, -40, 40, 83, 100])
+@pytest.mark.parametrize("b,c,groups,p", [(2, 6, 3, 1000), (2, 6, 3, 50001), (1, 20, 2, 40000)])
+def test_forward_of_large_and_small_fields(b, c, groups, p, power, dtype, layout):
+    """With eps = 0 a power of two in x changes nothing in y, bit for bit, and is the statistics' own."""
+    n = Norm(b, c, groups, p, layout, dtype, eps=0.0)
+    y, mean, rstd = n.forward()
+    n.check_forward(y, mean, rstd)
+    n.x = np.ldexp(n.x, power).astype(np.float32)
+    y2, mean2, rstd2 = n.forward()
+    assert np.array_equal(np.ldexp(mean, power), mean2) and np.array_equal(np.ldexp(rstd, -power), rstd2) and np.array_equal(y, y2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("p", [1000, 50001])
+def test_large_fields_with_the_usual_eps(p):
+    """1e25, where eps is nothing: rstd is a float like any other on both sides of the one-launch limit."""
+    n = Norm(1, 4, 2, p, act="gelu")
+    n.x *= np.float32(1e25)
+    n.check_forward(*n.forward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("seed", range(10))
+def test_constants_with_all_their_bits_between_zeros(seed, layout):
+    """24 bits each, so that no square and no sum of them fits a float."""
+    n = Norm(1, 4, 4, 40000 if seed % 2 else 1 << 18, layout, "f32", "identity")
+    n.x[:] = (10.0 ** np.random.default_rng(seed).uniform(-6, 6, 4)).astype(np.float32)[:, None]
+    n.x[:, :, [0, -1]] = 0.0
+    y, mean, rstd = n.forward()
+    n.check_forward(y, mean, rstd)
+    n.check_backward(mean, rstd, *n.backward(mean, rstd))
