@@ -460,21 +460,32 @@ __device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const
 }
 
 constexpr int kFoldThreads = 1024;     // one block has a group's tens of thousands of sums to add
-__host__ __device__ __forceinline__ int fold_channels(int B, int pieces) { return B * pieces <= 512 ? kFoldThreads / 64 : 1; }
-// Blocks 0 .. groups - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the parameter
-// gradients of one channel, or, where the sums of a channel are few, of 16, a wave each.
-__global__ __launch_bounds__(kFoldThreads) void norm_grad_fold_kernel(NormArgs a, unsigned groups, const double2* part,
+// Groups, or channels, of a block that have this many sums each: one, or, where they are few, a wave each.  (Groups are many only
+// where their sums are few: with 2^22 groups there are 2 a group, and a block for each would be more threads than a launch has.)
+__host__ __device__ __forceinline__ int fold_each(int sums) { return sums <= 512 ? kFoldThreads / 64 : 1; }
+// Blocks 0 .. blocks - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the parameter
+// gradients.
+__global__ __launch_bounds__(kFoldThreads) void norm_grad_fold_kernel(NormArgs a, unsigned blocks, const double2* part,
                                                                       const float* gamma, float2* m, float* ggamma, float* gbeta,
                                                                       int accumulate) {
   __shared__ double red[2 * kFoldThreads / 64];
   double s1 = 0.0, s2 = 0.0;
-  if (blockIdx.x >= groups && fold_channels(a.B, a.pieces) > 1)
-    return param_grads(a, a.pieces, part, (long long)(blockIdx.x - groups) * (kFoldThreads / 64) + (threadIdx.x >> 6), ggamma,
-                       gbeta, accumulate);
-  if (blockIdx.x >= groups) {
-    channel_share(a, a.pieces, part, blockIdx.x - groups, threadIdx.x, kFoldThreads, s1, s2);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (blockIdx.x >= blocks) {
+    const unsigned at = blockIdx.x - blocks;
+    if (fold_each(a.B * a.pieces) > 1)
+      return param_grads(a, a.pieces, part, (long long)at * (kFoldThreads / 64) + wave, ggamma, gbeta, accumulate);
+    channel_share(a, a.pieces, part, at, threadIdx.x, kFoldThreads, s1, s2);
     block_sum2(s1, s2, red);
-    if (threadIdx.x == 0) put_params(blockIdx.x - groups, s1, s2, ggamma, gbeta, accumulate);
+    if (threadIdx.x == 0) put_params(at, s1, s2, ggamma, gbeta, accumulate);
+    return;
+  }
+  if (fold_each(a.D * a.pieces) > 1) {
+    const long long bg = (long long)blockIdx.x * (kFoldThreads / 64) + wave;
+    if (bg >= (long long)a.B * a.G) return;
+    group_share(a, a.pieces, part, gamma, bg, lane, 64, s1, s2);
+    wave_sum2(s1, s2);
+    if (lane == 0) m[bg] = make_float2((float)(s1 * a.inv_n), (float)(s2 * a.inv_n));
     return;
   }
   group_share(a, a.pieces, part, gamma, blockIdx.x, threadIdx.x, kFoldThreads, s1, s2);
@@ -1204,10 +1215,10 @@ bool small_fits(const NormShape& n, bool adjoint) {
   const long long most = n.last ? (adjoint ? 2048 : 8192) : adjoint ? kSmallBwd : kSmallFwd;
   return n.P > 0 && n.P <= most && n.P * (n.C / n.G) <= most && (!n.last || n.P * n.C * n.B <= 1 << 19);
 }
-// blocks of norm_grad_fold_kernel for the parameters' gradients
-unsigned fold_blocks(const NormShape& n, const NormArgs& a) {
-  const int channels = fold_channels(n.B, a.pieces);
-  return (unsigned)((n.C + channels - 1) / channels);
+// blocks of norm_grad_fold_kernel for `count` groups or channels of `sums` sums each
+unsigned fold_blocks(long long count, int sums) {
+  const int each = fold_each(sums);
+  return (unsigned)((count + each - 1) / each);
 }
 SmallArgs small_args(const NormShape& n, int V) {
   const int D = n.C / n.G;
@@ -1294,8 +1305,8 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
                          ggamma, gbeta, accumulate);
     });
     if (later)
-      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold_blocks(n, a)), dim3(kFoldThreads), 0, s, a, 0u, part, gamma, m, ggamma, gbeta,
-                         accumulate);
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold_blocks(n.C, n.B * a.pieces)), dim3(kFoldThreads), 0, s, a, 0u, part, gamma, m,
+                         ggamma, gbeta, accumulate);
     return hipGetLastError();
   }
   const bool short_rows = !n.last && n.P < kShortRow, writes = gx != nullptr && n.P > 0;
@@ -1304,14 +1315,14 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   const bool inside = writes && !short_rows && inline_parts(n, (long long)(n.last ? n.C : n.C / n.G) * a.pieces);
   const NormArgs out = n.last ? cut_points(n, 2, kApplyLast, 1) : cut_rows(n, 2, inside ? kApplyInside : kApplyBlocks);
   const unsigned channel_blocks = params ? (unsigned)((n.C + threads / 64 - 1) / (threads / 64)) : 0;
-  const unsigned groups = (unsigned)(n.B * n.G), blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
+  const unsigned groups = fold_blocks((long long)n.B * n.G, a.D * a.pieces), blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
   const unsigned own = n.last ? (unsigned)(n.B * out.pieces) : row_blocks(out, short_rows);
   const dim3 grid(own + (inside ? channel_blocks : 0));
   const float2* means = inside ? nullptr : m;
   auto fold = [&] {
     if (!inside)
-      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? fold_blocks(n, a) : 0)), dim3(kFoldThreads), 0, s, a, groups, part,
-                         gamma, m, ggamma, gbeta, accumulate);
+      hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? fold_blocks(n.C, n.B * a.pieces) : 0)), dim3(kFoldThreads), 0, s,
+                         a, groups, part, gamma, m, ggamma, gbeta, accumulate);
   };
   with(streams(n, 2), [&](auto stream) {
     constexpr bool S = decltype(stream)::value;

@@ -97,3 +97,14 @@ def test_constants_with_all_their_bits_between_zeros(seed, layout):
     y, mean, rstd = n.forward()
     n.check_forward(y, mean, rstd)
     n.check_backward(mean, rstd, *n.backward(mean, rstd))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("b,c,groups,p", [(4096, 1024, 1024, 1), (4096, 1024, 1024, 2), (65535, 128, 64, 1), (16384, 512, 512, 1), (3000, 1000, 500, 2)])
+def test_millions_of_groups(b, c, groups, p, layout):
+    """As many groups as a descriptor may have, in fields of a few MB."""
+    n = Norm(b, c, groups, p, layout)
+    y, mean, rstd = n.forward()
+    n.check_forward(y, mean, rstd)
+    n.check_backward(mean, rstd, *n.backward(mean, rstd))
