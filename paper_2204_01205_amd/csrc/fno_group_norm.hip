@@ -901,7 +901,8 @@ __global__ __launch_bounds__(1024) void norm_last_grad_apply_kernel(NormArgs a, 
 // ------------------------------------------------------------------------------------------
 // Groups that one block holds in its registers: one launch, x (and gy) read once.  A thread has 16 values of the group,
 // those of whole 16-byte runs where the runs stay within a point's channels of the group (channels first: always), else
-// every `threads`-th.  The adjoint's sums over a channel go through LDS.
+// every `threads`-th.  The adjoint's sums over a channel go through LDS.  Groups by batch entries in two dimensions of the grid: 2^23
+// groups of 512 threads are more than one dimension holds.
 // ------------------------------------------------------------------------------------------
 constexpr int kSmallValues = 16;                          // of a thread
 constexpr int kSmallFwd = 1024 * kSmallValues, kSmallBwd = 8192;
@@ -993,7 +994,7 @@ __global__ __launch_bounds__(1024) void norm_small_kernel(NormArgs a, SmallArgs 
                                                           T* y, float* mean, float* rstd) {
   __shared__ double red[2 * 1024 / 64];
   __shared__ float2 affine[kMaxNormChannels];
-  const int b = blockIdx.x / a.G, g = blockIdx.x % a.G;
+  const int b = blockIdx.y, g = blockIdx.x;
   float v[kSmallValues];
   small_load<T, LAST>(a, s, b, g, x, v);
   // k is the group's first value, whatever it is: differences and their squares are formed in double
@@ -1007,7 +1008,7 @@ __global__ __launch_bounds__(1024) void norm_small_kernel(NormArgs a, SmallArgs 
   block_sum2(sum, square, red);
   const bool tells = threadIdx.x == 0;
   const Stat st = stat_of(moments_of(first, sum * a.inv_n, square * a.inv_n), a.eps, tells ? mean : nullptr, tells ? rstd : nullptr,
-                          blockIdx.x);
+                          (long long)b * a.G + g);
   for (int d = threadIdx.x; d < a.D; d += blockDim.x) {
     const Affine f = affine_of(st, gamma ? gamma[g * a.D + d] : 1.f, beta ? beta[g * a.D + d] : 0.f);
     affine[d] = make_float2(f.scale, f.shift);
@@ -1029,14 +1030,15 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
   __shared__ double red[2 * 1024 / 64];
   __shared__ float2 affine[kMaxNormChannels];
   extern __shared__ double lds[];
-  const int b = blockIdx.x / a.G, g = blockIdx.x % a.G;
+  const int b = blockIdx.y, g = blockIdx.x;
   const bool params = part != nullptr || ggamma != nullptr || gbeta != nullptr;
   float v[kSmallValues], w[kSmallValues];
   small_load<T, LAST>(a, s, b, g, x, v);
   small_load<T, LAST>(a, s, b, g, gy, w);
   for (int d = threadIdx.x; d < a.D; d += blockDim.x)
     affine[d] = make_float2(gamma ? gamma[g * a.D + d] : 1.f, beta ? beta[g * a.D + d] : 0.f);
-  const float mu = mean[blockIdx.x], rs = rstd[blockIdx.x];
+  const long long bg = (long long)b * a.G + g;
+  const float mu = mean[bg], rs = rstd[bg];
   float2* const product = reinterpret_cast<float2*>(lds);      // gz and gz xh of every value
   __syncthreads();
   double s1 = 0.0, s2 = 0.0;
@@ -1247,7 +1249,7 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     const NormArgs a = norm_args(n);
     const SmallArgs k = small_args(n, kVec<T>);
     with(n.last, [&](auto last) {
-      hipLaunchKernelGGL((norm_small_kernel<T, ACT, decltype(last)::value>), dim3(n.B * n.G), dim3(small_threads(k.n)), 0, s, a, k, x,
+      hipLaunchKernelGGL((norm_small_kernel<T, ACT, decltype(last)::value>), dim3(n.G, n.B), dim3(small_threads(k.n)), 0, s, a, k, x,
                          gamma, beta, y, mean, rstd);
     });
     return hipGetLastError();
@@ -1300,7 +1302,7 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
     while (lanes < 64 && lanes < n.P) lanes *= 2;
     const bool later = params && n.B > 1;
     with(n.last, [&](auto last) {
-      hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.B * n.G), dim3(small_threads(k.n)),
+      hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.G, n.B), dim3(small_threads(k.n)),
                          params ? k.n * sizeof(float2) : 0, s, a, k, lanes, x, gy, gamma, beta, mean, rstd, gx, later ? part : nullptr,
                          ggamma, gbeta, accumulate);
     });

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2204_01205_amd import binding as B
 from test_gpu_norm import Norm
 
 
@@ -108,3 +109,36 @@ def test_millions_of_groups(b, c, groups, p, layout):
     y, mean, rstd = n.forward()
     n.check_forward(y, mean, rstd)
     n.check_backward(mean, rstd, *n.backward(mean, rstd))
+
+
+@pytest.mark.gpu
+def test_the_most_groups_of_one_launch_at_their_longest():
+    """2^23 groups of 7200 bf16 values (121 GB, in place): more threads than one dimension of a grid holds."""
+    b, c, p = 8192, 1024, 7200
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 1.35e11:
+        pytest.skip("needs 135 GB")
+    one = Norm(1, 4, 4, p, dtype="bf16", act="identity")
+    one.gamma[:], one.beta[:] = 1, 0                     # the big field's are null
+    y, mean, rstd = one.forward()
+    one.check_forward(y, mean, rstd)
+    one.gy = one.x
+    gx = one.backward(mean, rstd)[0]
+    desc = B.make_norm_desc(b, c, c, p, dtype=B.FNO_DTYPE_BF16, activation=B.FNO_ACT_IDENTITY)
+    x = torch.empty(b, c // 4, 4, p, dtype=torch.bfloat16, device="cuda")
+    ws = B.alloc_norm_workspace(desc)
+    m, r = torch.empty(b, c, device="cuda"), torch.empty(b, c, device="cuda")
+    places = [(0, 0), (0, c // 4 - 1), (b // 2, 7), (4095, c // 4 - 1), (4096, 0), (b - 1, c // 4 - 1)]
+
+    def check(want):
+        assert all(torch.equal(x[i, j].float().cpu(), torch.from_numpy(want[0])) for i, j in places)
+        assert torch.equal(m, torch.from_numpy(mean).cuda().expand(b, 4).repeat(1, c // 4)) and torch.equal(r[b - 1, -4:].cpu(), torch.from_numpy(rstd[0]))
+
+    x.copy_(one.dev(one.x).expand(b, c // 4, 4, p))
+    B.fno_group_norm_fwd(desc, x, None, None, x, m, r, ws)
+    check(y)
+    x.copy_(one.dev(one.x).expand(b, c // 4, 4, p))
+    B.fno_group_norm_bwd(desc, x, None, None, m, r, x, x, None, None, ws)
+    check(gx)
+    del x
+    torch.cuda.empty_cache()
