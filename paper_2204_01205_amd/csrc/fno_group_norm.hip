@@ -1240,6 +1240,17 @@ void with(bool b, F&& f) {
   else f(std::false_type());
 }
 
+// One launch after the other, none after one that was refused: the next one would read what that one had to leave.
+struct Launches {
+  hipError_t status = hipSuccess;
+  template <class F>
+  void operator()(F&& launch) {
+    if (status != hipSuccess) return;
+    launch();
+    status = hipGetLastError();
+  }
+};
+
 template <class T, int ACT>
 hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* beta, T* y, float* mean, float* rstd,
                void* ws, hipStream_t s) {
@@ -1255,6 +1266,7 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     return hipGetLastError();
   }
   const bool hint = streams(n, 1);
+  Launches then;
   if (n.last) {
     const NormArgs a = cut_points(n, 1, kSumBlocks / 2, 3), out = cut_points(n, 1, kApplyLast, 1);
     const int active = active_threads(n.C, kVec<T>), threads = (active + 63) / 64 * 64;
@@ -1263,15 +1275,19 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
     const dim3 grid((unsigned)(n.B * a.pieces));
     with(hint, [&](auto stream) {
       constexpr bool S = decltype(stream)::value;
-      hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), pair_bytes(n, active, threads), s, a, cut, active, x,
-                         part);
-      if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, cut, part, stat, mean, rstd);
-      if (n.P > 0)
+      then([&] {
+        hipLaunchKernelGGL((norm_last_sum_kernel<T, S>), grid, dim3(threads), pair_bytes(n, active, threads), s, a, cut, active, x, part);
+      });
+      if (!inside) then([&] {
+        hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, cut, part, stat, mean, rstd);
+      });
+      if (n.P > 0) then([&] {
         hipLaunchKernelGGL((norm_last_apply_kernel<T, ACT, S>), dim3((unsigned)(n.B * out.pieces)), dim3(threads),
                            inside ? n.G * sizeof(Stat) : 0, s, out, active, x, gamma, beta, stat, inside ? part : nullptr, cut, mean,
                            rstd, y);
+      });
     });
-    return hipGetLastError();
+    return then.status;
   }
   const NormArgs a = cut_groups(n);
   const Cut cut = cut_of(n, a);
@@ -1279,14 +1295,20 @@ hipError_t fwd(const NormShape& n, const T* x, const float* gamma, const float* 
   const NormArgs rows = cut_rows(n, 1, inside ? kApplyInside : kApplyBlocks);
   with(hint, [&](auto stream) {
     constexpr bool S = decltype(stream)::value;
-    hipLaunchKernelGGL((norm_sum_kernel<T, S>), dim3((unsigned)(n.B * n.G * a.pieces)), dim3(kThreads), 0, s, a, cut, x, part);
-    if (!inside) hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, cut, part, stat, mean, rstd);
+    then([&] {
+      hipLaunchKernelGGL((norm_sum_kernel<T, S>), dim3((unsigned)(n.B * n.G * a.pieces)), dim3(kThreads), 0, s, a, cut, x, part);
+    });
+    if (!inside) then([&] {
+      hipLaunchKernelGGL(norm_stat_kernel, dim3(n.B * n.G), dim3(kThreads), 0, s, a, cut, part, stat, mean, rstd);
+    });
     with(short_rows, [&](auto short_) {
-      hipLaunchKernelGGL((norm_apply_kernel<T, ACT, decltype(short_)::value, S>), dim3(row_blocks(rows, short_rows)), dim3(kThreads), 0, s,
-                         rows, x, gamma, beta, stat, inside ? part : nullptr, cut, mean, rstd, y);
+      then([&] {
+        hipLaunchKernelGGL((norm_apply_kernel<T, ACT, decltype(short_)::value, S>), dim3(row_blocks(rows, short_rows)), dim3(kThreads), 0,
+                           s, rows, x, gamma, beta, stat, inside ? part : nullptr, cut, mean, rstd, y);
+      });
     });
   });
-  return hipGetLastError();
+  return then.status;
 }
 
 template <class T, int ACT>
@@ -1295,6 +1317,7 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
   double2* part = static_cast<double2*>(ws);
   float2* m = reinterpret_cast<float2*>(static_cast<char*>(ws) + norm_part_bytes(n));
   const bool params = ggamma != nullptr || gbeta != nullptr;
+  Launches then;
   if (small_fits(n, true)) {
     const NormArgs a = norm_args(n);
     const SmallArgs k = small_args(n, kVec<T>);
@@ -1302,51 +1325,63 @@ hipError_t bwd(const NormShape& n, const T* x, const float* gamma, const float* 
     while (lanes < 64 && lanes < n.P) lanes *= 2;
     const bool later = params && n.B > 1;
     with(n.last, [&](auto last) {
-      hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.G, n.B), dim3(small_threads(k.n)),
-                         params ? k.n * sizeof(float2) : 0, s, a, k, lanes, x, gy, gamma, beta, mean, rstd, gx, later ? part : nullptr,
-                         ggamma, gbeta, accumulate);
+      then([&] {
+        hipLaunchKernelGGL((norm_small_grad_kernel<T, ACT, decltype(last)::value>), dim3(n.G, n.B), dim3(small_threads(k.n)),
+                           params ? k.n * sizeof(float2) : 0, s, a, k, lanes, x, gy, gamma, beta, mean, rstd, gx, later ? part : nullptr,
+                           ggamma, gbeta, accumulate);
+      });
     });
-    if (later)
+    if (later) then([&] {
       hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(fold_blocks(n.C, n.B * a.pieces)), dim3(kFoldThreads), 0, s, a, 0u, part, gamma, m,
                          ggamma, gbeta, accumulate);
-    return hipGetLastError();
+    });
+    return then.status;
   }
   const bool short_rows = !n.last && n.P < kShortRow, writes = gx != nullptr && n.P > 0;
   const NormArgs a = n.last ? cut_points(n, 2, kSumBlocks / 2, 3) : cut_rows(n, 2, kSumBlocks);
-    const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
+  const int active = active_threads(n.C, kVec<T>), threads = n.last ? (active + 63) / 64 * 64 : kThreads;
   const bool inside = writes && !short_rows && inline_parts(n, (long long)(n.last ? n.C : n.C / n.G) * a.pieces);
   const NormArgs out = n.last ? cut_points(n, 2, kApplyLast, 1) : cut_rows(n, 2, inside ? kApplyInside : kApplyBlocks);
   const unsigned channel_blocks = params ? (unsigned)((n.C + threads / 64 - 1) / (threads / 64)) : 0;
-  const unsigned groups = fold_blocks((long long)n.B * n.G, a.D * a.pieces), blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
+  const unsigned groups = fold_blocks((long long)n.B * n.G, a.D * a.pieces);
+  const unsigned blocks = n.last ? (unsigned)(n.B * a.pieces) : row_blocks(a, short_rows);
   const unsigned own = n.last ? (unsigned)(n.B * out.pieces) : row_blocks(out, short_rows);
   const dim3 grid(own + (inside ? channel_blocks : 0));
   const float2* means = inside ? nullptr : m;
   auto fold = [&] {
-    if (!inside)
+    if (!inside) then([&] {
       hipLaunchKernelGGL(norm_grad_fold_kernel, dim3(groups + (params ? fold_blocks(n.C, n.B * a.pieces) : 0)), dim3(kFoldThreads), 0, s,
                          a, groups, part, gamma, m, ggamma, gbeta, accumulate);
+    });
   };
   with(streams(n, 2), [&](auto stream) {
     constexpr bool S = decltype(stream)::value;
     if (n.last) {
-      hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT, S>), dim3(blocks), dim3(threads), pair_bytes(n, active, threads), s, a,
-                         active, x, gy, gamma, beta, mean, rstd, part);
+      then([&] {
+        hipLaunchKernelGGL((norm_last_grad_sum_kernel<T, ACT, S>), dim3(blocks), dim3(threads), pair_bytes(n, active, threads), s, a,
+                           active, x, gy, gamma, beta, mean, rstd, part);
+      });
       fold();
-      if (writes)
+      if (writes) then([&] {
         hipLaunchKernelGGL((norm_last_grad_apply_kernel<T, ACT, S>), grid, dim3(threads), inside ? n.G * sizeof(float2) : 0, s, out, own,
                            active, x, gy, gamma, beta, mean, rstd, means, part, a.pieces, ggamma, gbeta, accumulate, gx);
+      });
       return;
     }
     with(short_rows, [&](auto short_) {
       constexpr bool R = decltype(short_)::value;
-      hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, R, S>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd, part);
+      then([&] {
+        hipLaunchKernelGGL((norm_grad_sum_kernel<T, ACT, R, S>), dim3(blocks), dim3(kThreads), 0, s, a, x, gy, gamma, beta, mean, rstd,
+                           part);
+      });
       fold();
-      if (writes)
+      if (writes) then([&] {
         hipLaunchKernelGGL((norm_grad_apply_kernel<T, ACT, R, S>), grid, dim3(kThreads), 0, s, out, own, x, gy, gamma, beta, mean, rstd,
                            means, part, a.pieces, ggamma, gbeta, accumulate, gx);
+      });
     });
   });
-  return hipGetLastError();
+  return then.status;
 }
 
 // f(type, activation) for the type and activation of a descriptor
