@@ -337,18 +337,19 @@ __device__ __forceinline__ void terms(const Slope& k, float x, float gy, float& 
   d = x - k.mean;
   gz = ACT == 0 ? gy : gy * slope_f<ACT>(fmaf(d, k.scale, k.shift));
 }
-// and gx = gz rstd gamma - rstd m1 - d rstd^2 m2, m1 and m2 the group's means of gamma gz and gamma gz xh
+// and gx = gz rstd gamma - rstd m1 - xh rstd m2, m1 and m2 the group's means of gamma gz and gamma gz xh.  (xh = d rstd costs a
+// product a value; rstd^2 m2 in its place, for d, would leave the floats where rstd is past 1e18 or below 1e-18.)
 struct Weights {
-  float gz, d, one;
+  float rstd, gz, xh, one;
 };
 __device__ __forceinline__ Weights weights_of(float rstd, float gamma, float2 m) {
-  return Weights{rstd * gamma, -rstd * rstd * m.y, -rstd * m.x};
+  return Weights{rstd, rstd * gamma, -rstd * m.y, -rstd * m.x};
 }
 template <int ACT>
 __device__ __forceinline__ float grad_of(const Slope& k, const Weights& w, float x, float gy) {
   float d, gz;
   terms<ACT>(k, x, gy, d, gz);
-  return fmaf(gz, w.gz, fmaf(d, w.d, w.one));
+  return fmaf(gz, w.gz, fmaf(d * w.rstd, w.xh, w.one));
 }
 
 // part[(row, piece)] = (sum gz, sum gz xh)

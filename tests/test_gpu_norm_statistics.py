@@ -142,3 +142,25 @@ def test_the_most_groups_of_one_launch_at_their_longest():
     check(gx)
     del x
     torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("power", [-100, -83, -60, -40, 40, 60, 83, 100])
+@pytest.mark.parametrize("b,c,groups,p", [(2, 6, 3, 300), (2, 6, 3, 1000), (2, 6, 3, 50001), (1, 20, 2, 40000), (3, 40, 1, 400)])
+def test_adjoint_of_large_and_small_fields(b, c, groups, p, power, dtype, layout):
+    """With eps = 0 a power of two in x is its inverse in gx and nothing in the parameters' gradients: bit for bit where no
+    product of a cotangent and a difference leaves the normal floats, else to 2^-33 of the sums, a last bit of the means."""
+    n = Norm(b, c, groups, p, layout, dtype, eps=0.0)
+    y, mean, rstd = n.forward()
+    gx, gg, gb = n.backward(mean, rstd)
+    n.check_backward(mean, rstd, gx, gg, gb)
+    n.x = np.ldexp(n.x, power).astype(np.float32)
+    gx2, gg2, gb2 = n.backward(np.ldexp(mean, power), np.ldexp(rstd, -power))
+    gx2 = np.ldexp(gx2.astype(np.float64), power)
+    if abs(power) <= 60:
+        assert np.array_equal(gx2, gx) and np.array_equal(gg2, gg) and np.array_equal(gb2, gb)
+    tol = 1e-6 * np.abs(gx).max() + (2.0 ** -8 if dtype == "bf16" else 0) * np.abs(gx)
+    assert np.all(np.abs(gx2 - gx) <= tol)
+    assert np.all(np.abs(gg2 - gg) <= 1e-6 * np.abs(gg).max()) and np.array_equal(gb2, gb)
