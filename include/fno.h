@@ -254,8 +254,8 @@ int fno_group_norm_workspace_bytes(const fno_norm_desc* desc, size_t* bytes);
 
 /* Forward.  gamma, beta nullable (1 and 0); mean, rstd out float [B][groups], nullable: what the backward call needs.
  * y may be x itself; no other overlap.  x and y 16-byte aligned, ws 256-byte aligned.  npoints = 0 gives mean 0 and
- * rstd 1 / sqrt(eps).  An infinity or a NaN in a group makes the whole group NaN.  Fixed summation order: the same bits
- * on every run. */
+ * rstd 1 / sqrt(eps); x and y (below x and gy) may then be null.  An infinity or a NaN in a group makes the whole group NaN.
+ * Fixed summation order: the same bits on every run. */
 int fno_group_norm_fwd(const fno_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
                        float* mean, float* rstd, void* ws, size_t ws_bytes, void* stream);
 

@@ -647,7 +647,7 @@ int fno_group_norm_fwd(const fno_norm_desc* desc, const void* x, const float* ga
   fno::NormShape n;
   int rc = norm_shape(desc, &n);
   if (rc != FNO_OK) return rc;
-  if (x == nullptr || y == nullptr) { set_detail("x and y are required"); return FNO_EINVAL; }
+  if (n.P > 0 && (x == nullptr || y == nullptr)) { set_detail("x and y are required"); return FNO_EINVAL; }
   if (misaligned16(x, y)) return FNO_EINVAL;
   rc = check_norm_ws(n, ws, ws_bytes);
   if (rc != FNO_OK) return rc;
@@ -661,7 +661,7 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
   fno::NormShape n;
   int rc = norm_shape(desc, &n);
   if (rc != FNO_OK) return rc;
-  if (x == nullptr || mean == nullptr || rstd == nullptr || gy == nullptr) { set_detail("x, mean, rstd and gy are required"); return FNO_EINVAL; }
+  if (mean == nullptr || rstd == nullptr || (n.P > 0 && (x == nullptr || gy == nullptr))) { set_detail("x, mean, rstd and gy are required"); return FNO_EINVAL; }
   if (misaligned16(x, gy, gx)) return FNO_EINVAL;
   rc = check_norm_ws(n, ws, ws_bytes);
   if (rc != FNO_OK) return rc;

@@ -164,3 +164,14 @@ def test_adjoint_of_large_and_small_fields(b, c, groups, p, power, dtype, layout
     tol = 1e-6 * np.abs(gx).max() + (2.0 ** -8 if dtype == "bf16" else 0) * np.abs(gx)
     assert np.all(np.abs(gx2 - gx) <= tol)
     assert np.all(np.abs(gg2 - gg) <= 1e-6 * np.abs(gg).max()) and np.array_equal(gb2, gb)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["first", "last"])
+def test_no_points_through_tensors(layout):
+    """An empty tensor has no address."""
+    n = Norm(2, 4, 2, 0, layout, eps=0.25)
+    y, mean, rstd = n.forward()
+    assert y.size == 0 and (mean == 0).all() and (rstd == 2).all()
+    gx, gg, gb = n.backward(mean, rstd)
+    assert gx.size == 0 and (gg == 0).all() and (gb == 0).all()
