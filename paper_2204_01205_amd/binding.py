@@ -423,9 +423,17 @@ def make_adamw_tensors(params, grads, m, v, exps=None, weight_decay=0.0) -> Adam
                         (list(params), list(grads), list(m), list(v), None if exps is None else list(exps)))
 
 
+def _list_stream(tensors: AdamwTensors) -> int:
+    """The current stream, for a list whose tensors live on the current GPU: the call goes to that stream alone."""
+    current = torch.cuda.current_device()
+    if tensors.device is not None and tensors.device.index != current:
+        raise ValueError(f"the tensors of the list live on {tensors.device}, the current device is cuda:{current}")
+    return torch._C._cuda_getCurrentRawStream(current)
+
+
 def fno_adamw_step(tensors: AdamwTensors, lr, beta1, beta2, eps, step, grad_norm=None, max_norm=1.0, seed=0) -> None:
     status = lib().fno_adamw_step(tensors.count, tensors.array, tensors.bits, lr, beta1, beta2, eps, step,
-                                  _address(grad_norm, torch.float32, 1, "grad_norm"), max_norm, seed, _raw_stream())
+                                  _address(grad_norm, torch.float32, 1, "grad_norm"), max_norm, seed, _list_stream(tensors))
     if status:
         _check(status)
 
@@ -442,7 +450,7 @@ def alloc_grad_norm_workspace(tensors: AdamwTensors, device="cuda") -> torch.Ten
 
 def fno_grad_norm(tensors: AdamwTensors, norm, ws) -> None:
     status = lib().fno_grad_norm(tensors.count, tensors.array, _address(norm, torch.float32, 1, "norm"),
-                                 _address(ws, torch.uint8, ws.numel(), "ws"), ws.numel(), _raw_stream())
+                                 _address(ws, torch.uint8, ws.numel(), "ws"), ws.numel(), _list_stream(tensors))
     if status:
         _check(status)
 
@@ -456,7 +464,7 @@ def fno_adamw_state_read(tensors: AdamwTensors, m_out, v_out) -> None:
         raise ValueError("m_out and v_out must have one entry a tensor")
     outs = [(ctypes.c_void_p * max(count, 1))(*[_address(t, bf16, n, name) for t, n in zip(out, tensors.sizes)])
             for name, out in (("m_out", m_out), ("v_out", v_out))]
-    status = lib().fno_adamw_state_read(count, tensors.array, outs[0], outs[1], _raw_stream())
+    status = lib().fno_adamw_state_read(count, tensors.array, outs[0], outs[1], _list_stream(tensors))
     if status:
         _check(status)
 
