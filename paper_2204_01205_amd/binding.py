@@ -159,9 +159,12 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _raw_stream() -> int:
-    """The current stream's handle, without the stream object that _stream() makes (0.3 us instead of 3)."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _raw_stream(device: Optional[int] = None) -> int:
+    """The current stream's handle, without the stream object that _stream() makes (0.3 us instead of 3), where torch has the
+    call that its own generated code uses for that; it is not among the documented ones."""
+    device = torch.cuda.current_device() if device is None else device
+    handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return handle(device) if handle is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _address(t: Optional[torch.Tensor], dtype, numel: int, name: str):
@@ -383,7 +386,9 @@ def fno_group_norm_bwd(desc, x, gamma, beta, mean, rstd, gy, gx, ggamma, gbeta, 
 
 class AdamwTensors:
     """The host array of tensors that fno_adamw_step, fno_grad_norm and fno_adamw_state_read take, and the tensors
-    themselves, which have to live as long as the array is used.  Built by make_adamw_tensors()."""
+    themselves, which have to live as long as the array is used.  Built by make_adamw_tensors().  The array holds addresses: a
+    program that puts another tensor in the place of one of these (a new gradient every step, as after grad = None) has to
+    build the list again, or the calls go on with the old one."""
 
     def __init__(self, array, count, sizes, bits, device, keep):
         self.array, self.count, self.sizes, self.bits, self.device, self.keep = array, count, sizes, bits, device, keep
@@ -428,7 +433,7 @@ def _list_stream(tensors: AdamwTensors) -> int:
     current = torch.cuda.current_device()
     if tensors.device is not None and tensors.device.index != current:
         raise ValueError(f"the tensors of the list live on {tensors.device}, the current device is cuda:{current}")
-    return torch._C._cuda_getCurrentRawStream(current)
+    return _raw_stream(current)
 
 
 def fno_adamw_step(tensors: AdamwTensors, lr, beta1, beta2, eps, step, grad_norm=None, max_norm=1.0, seed=0) -> None:

@@ -1,4 +1,4 @@
-"""Which stream the calls on a list of tensors go to, without a device."""
+"""Which stream the calls on a list of tensors go to."""
 import pytest
 import torch
 
@@ -16,3 +16,21 @@ def test_a_list_on_another_device_is_refused(monkeypatch, call):
     there = B.AdamwTensors(here.array, 0, [], 8, torch.device("cuda", 1), here.keep)
     with pytest.raises(ValueError, match="cuda:1"):
         call(there)
+
+
+def test_the_stream_without_the_undocumented_call(monkeypatch):
+    class Stream:
+        cuda_stream = 77
+
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: Stream)
+    assert B._raw_stream(0) == 77
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert B._raw_stream() == 77
+
+
+@pytest.mark.gpu
+def test_the_current_streams_handle():
+    assert B._raw_stream() == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(torch.cuda.Stream()):
+        assert B._raw_stream() == torch.cuda.current_stream().cuda_stream != torch.cuda.default_stream().cuda_stream
