@@ -463,6 +463,8 @@ __device__ __forceinline__ void group_share(const NormArgs& a, int pieces, const
 constexpr int kFoldThreads = 1024;     // one block has a group's tens of thousands of sums to add
 // Groups, or channels, of a block that have this many sums each: one, or, where they are few, a wave each.  (Groups are many only
 // where their sums are few: with 2^22 groups there are 2 a group, and a block for each would be more threads than a launch has.)
+// Adjoint, us, now, a block each, a wave each: 64 x 64 groups of 9000 values 124, 147, 124; one group of 1024 rows of 20000 81.6,
+// 85.7, 99.0; channels last, 64 x 128 groups of 3000 95.6, 139.7, 100.5.
 __host__ __device__ __forceinline__ int fold_each(int sums) { return sums <= 512 ? kFoldThreads / 64 : 1; }
 // Blocks 0 .. blocks - 1 (maybe none): m[bg] = the group's means of gamma gz and gamma gz xh.  The blocks behind: the parameter
 // gradients.
@@ -680,6 +682,8 @@ __global__ __launch_bounds__(1024) void norm_last_sum_kernel(NormArgs a, Cut cut
   double2* const to = part + (long long)b * a.G * a.pieces + j;
   const double inv = count > 0.0 ? 1.0 / count : 0.0;
   auto put = [&](int g, double2 m) { to[(long long)g * a.pieces] = moments_of(firsts[g], m.x * inv, m.y * inv); };
+  // a group a thread, or a wave (forward, us: 64 groups of one channel 12.2 and 18.7, 8 of 8 12.1 and 12.6, 4 of 32 12.2 and 12.0, one
+  // of 1024 27.7 and 17.5)
   if (a.D <= 32) {
     for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
       double2 m = sums[g * a.D];
@@ -1115,9 +1119,12 @@ __global__ __launch_bounds__(1024) void norm_small_grad_kernel(NormArgs a, Small
 // ------------------------------------------------------------------------------------------
 constexpr long long kSumBlocks = 4096;        // blocks of a launch that only reads: 16 a CU; channels last, half as many
 constexpr long long kTileBytes = 16384;       // of a whole tile of 256 threads that read one field
-constexpr long long kApplyBlocks = 1 << 22;   // of one that writes: a tile each, but for the very largest fields; channels last,
-constexpr long long kApplyInside = 2048;      // where every block first adds the sums of pieces
-constexpr long long kApplyLast = 8192;        // where a thread first has its channels' factors to work out, so many
+constexpr long long kApplyBlocks = 1 << 22;   // of one that writes: a tile each, but for the very largest fields
+// Where every block first adds the sums of pieces, fewer (adjoint of 24 rows of 357210: 512 blocks 35.0 us, 2048 33.6, a tile a block
+// 35.0; of 20 rows of 700000 57.6, 56.0, 57.9), and channels last, where a thread first has its channels' factors to work out
+// (5242880 points of 32 channels: 1024 blocks 340, 8192 327, a tile a block 332; bf16 adjoint, 2 x 4194304 points of 20: 341, 344, 488).
+constexpr long long kApplyInside = 2048;
+constexpr long long kApplyLast = 8192;
 constexpr long long kShortRow = 512;          // rows below this go wave by wave: 4 x 64 rows of 600 take 8.7 us, 7.1 block by
                                               // block, 32 x 64 of them 9.8 and 10.2
 
@@ -1164,7 +1171,9 @@ NormArgs cut_rows(const NormShape& n, int fields, long long blocks) {  // channe
   return a;
 }
 // Channels last: blocks of at least 64 points, whose sums (16 bytes a channel) are then little beside them, and of at least
-// three tiles where they only read (sums: every piece is one more to add for one block).
+// three tiles where they only read (every piece is one more to add: 400000 points of 20 channels, forward with one tile 26.4 us, two
+// 23.8, three 23.6, six 23.6; adjoint 40.6, 40.5, 38.3, 38.0), but no fewer than 256 in all (bf16, 4 x 13440 points of 27: 64 blocks
+// 13.0, 128 12.5, 256 and more 12.3; adjoint of 20000 points of 256: 256 29.6, 1024 34.0).
 NormArgs cut_points(const NormShape& n, int fields, long long blocks, int tiles_at_least) {
   NormArgs a = norm_args(n);
   const long long tile = (long long)active_threads(n.C, n.bf16 ? 8 : 4) * (n.bf16 ? 8 : 4) * (fields == 1 ? 4 : 2);
@@ -1202,9 +1211,11 @@ unsigned row_blocks(const NormArgs& a, bool short_rows) {
   return (unsigned)(short_rows ? (rows + kThreads / 64 - 1) / (kThreads / 64) : rows * a.pieces);
 }
 
-// Sums of pieces that every block of the next launch adds itself, sparing a launch: as many as kInlineParts where the field is
-// small (channels first: 4 x 16 x 134400 values, adjoint, 33.6 us and 37.3 with the launch; of a field of 168 MB, where fewer
-// and longer blocks write, 148 and 134), channels last a quarter of that.
+// Sums of pieces that every block of the next launch adds itself, sparing a launch: few of them, in small fields.  Us, this way
+// and with the launch.  Channels first: adjoint of 20 x 80000 values, 800 sums, 12.7 and 13.4, of 20 x 200000, 1960 sums, 20.5 and
+// 20.0, of 20 x 400000, 3920 sums, 36.0 and 33.9; fields of 32 MB 20.9 and 22.6, of 64 MB 38.7 and 41.2, of 128 MB 78.9 and 79.2,
+// of 320 MB 172.8 and 160.7, as fewer and longer blocks write.  Channels last, where a block adds those of all its groups: 20
+// channels in 4 groups, 400 sums 8.8 and 9.8, 800 sums 9.8 and 10.0; 64 in 16, 500 sums 10.4 and 9.7; 20 in 20, 1000 sums 11.1 and 9.7.
 constexpr long long kInlineParts = 2048, kInlineBytes = 64ll << 20;
 bool inline_parts(const NormShape& n, long long parts) {
   return parts <= (n.last ? kInlineParts / 4 : kInlineParts) && n.P * n.C * n.B * (n.bf16 ? 2 : 4) <= kInlineBytes;
