@@ -233,7 +233,9 @@ int fno_adam_step(int64_t n, float* param, const float* grad, float* m, float* v
  * dtype is that of x, y, gy and gx: float, or bf16 (16 bits, each the upper half of a float).  Everything else is float.
  * Statistics are formed in double; the adjoint's sums in double, over a few values in float, whatever the dtype; bf16 results are
  * rounded once, to nearest even.  Range: x to 1e36 in size and sqrt(var + eps) from 1e-36 to 1e36, any mean beside any spread; in
- * the adjoint gy, and gy (x - mean) where it counts in the sums, from 1e-30 to 1e36.  activation: FNO_ACT_IDENTITY, FNO_ACT_GELU or FNO_ACT_SILU (z / (1 + exp(-z))). */
+ * the adjoint gy, and gy (x - mean) where it counts in the sums, from 1e-30 to 1e36.  (The adjoint starts from the saved mean, a
+ * float: its xh is off by up to 2^-24 |mean| rstd, the forward call's is not.)
+ * activation: FNO_ACT_IDENTITY, FNO_ACT_GELU or FNO_ACT_SILU (z / (1 + exp(-z))). */
 enum { FNO_ACT_SILU = 2 };       /* fno_group_norm_fwd and fno_group_norm_bwd only */
 enum { FNO_LAYOUT_CHANNELS_FIRST = 0, FNO_LAYOUT_CHANNELS_LAST = 1 };
 enum { FNO_DTYPE_F32 = 0, FNO_DTYPE_BF16 = 1 };
