@@ -14,9 +14,10 @@
 // is too large or too small for them.  Adjoint: four or eight terms are added in float, everything else in double.
 //
 // Measured, with the bytes that the launches move (x twice; adjoint x and gy twice) at a copy's 6.2 TB/s in brackets: 60 x 60 x
-// 64 x 30 points, 20 channels, forward 262 us (268); 64 x 64 x 64 x 20, 32 channels last, 324 (325); 128 x 128 x 64 x 32, 20
-// channels, adjoint 2.09 ms (2.16).  bf16, adjoint of 2 x 64 x 64 x 64 x 16, 20 channels last: 340 us (270), the vector unit has
-// 26 instructions a value, two of them transcendental.  Fields of a few MB: launches of 3 to 10 us each.
+// 64 x 30 points, 20 channels, forward 270 us (268); 64 x 64 x 64 x 20, 32 channels last, 330 (325); 128 x 128 x 64 x 32, 20
+// channels, adjoint 2.12 ms (2.16).  bf16, adjoint of 2 x 64 x 64 x 64 x 16, 20 channels last: 340 us (270), the vector unit has
+// 27 and 28 instructions a value, two of them transcendental, and is busy for 125 of 171 us and 128 of 208.  Fields of a few MB:
+// launches of 4 to 13 us each.
 #include "fno_device.h"
 
 #include <climits>
