@@ -43,16 +43,24 @@ lib, p, size = B.lib(), ctypes.c_void_p(1 << 20), ctypes.c_size_t(1 << 60)
 seen, count, fails = (((ctypes.c_ulonglong * 7) * 256).in_dll(takes, "launches"), ctypes.c_int.in_dll(takes, "launched"),
                       ctypes.c_int.in_dll(takes, "fails_at"))
 
-def call(op, desc, fail=0):
+def call(op, kw, fail=0):
     count.value, fails.value = 0, fail
-    d = ctypes.byref(desc)
+    if "sizes" in kw:
+        n, bits = len(kw["sizes"]), kw["bits"]
+        tensors = (B.FnoAdamwTensor * max(n, 1))(*[B.FnoAdamwTensor(1 << 20, 1 << 20, 1 << 20, 1 << 20, 1 << 20, s, 0.0) for s in kw["sizes"]])
+        outs = (ctypes.c_void_p * max(n, 1))(*[1 << 20] * n)
+        rc = lib.fno_adamw_step(n, tensors, bits, 1e-3, 0.9, 0.999, 1e-8, 1, None, 1.0, 0, None) if op == "step" else \
+             lib.fno_grad_norm(n, tensors, p, p, size, None) if op == "norm" else \
+             lib.fno_adamw_state_read(n, tensors, outs, outs, None)
+        return rc, [list(seen[k]) for k in range(min(count.value, 256))]
+    d = ctypes.byref(B.make_norm_desc(**kw))
     rc = lib.fno_group_norm_fwd(d, p, p, p, p, p, p, p, size, None) if op == "fwd" else \
          lib.fno_group_norm_bwd(d, p, p, p, p, p, p, p, p, p, p, size, None)
     return rc, [list(seen[k]) for k in range(count.value)]
 
 out = []
 for op, kw, fail in json.loads(sys.stdin.read()):
-    out.append(call(op, B.make_norm_desc(**kw), fail))
+    out.append(call(op, kw, fail))
 print(json.dumps(out))
 """
 
@@ -107,3 +115,21 @@ def test_nothing_is_launched_after_a_launch_that_failed(launches, op):
     assert max(k for _, _, k in calls) >= 3
     for (_, kw, k), (status, made) in zip(calls, launches(calls)):
         assert status == -4 and len(made) == k, (kw, k, status, made)
+
+
+LISTS = [[1], [0, 5, 0], [4096, 4097, 1], [7] * 200, [0] * 70 + [3], [2 ** 22] * 65, [2 ** 32 + 777, 12], [2 ** 40, 2 ** 40, 1, 2 ** 39], [2 ** 34] * 130]
+
+
+@pytest.mark.parametrize("op,bits", [("step", 32), ("step", 8), ("norm", 32), ("read", 8)])
+def test_lists_of_tensors(launches, op, bits):
+    whole = launches([(op, dict(sizes=s, bits=bits), 0) for s in LISTS])
+    calls = []
+    for sizes, (status, made) in zip(LISTS, whole):
+        assert status == 0 and made, sizes
+        for gx, gy, gz, bx, by, bz, lds in made:
+            assert 0 < gx * bx < 2 ** 32 and gy == gz == by == bz == 1 and bx <= 1024 and lds == 0, (sizes, made)
+        # up to 64 tensors a launch
+        assert len(made) <= -(-len(sizes) // 64) + (op == "norm") + sum(n > 2 ** 32 for n in sizes)
+        calls += [(op, dict(sizes=sizes, bits=bits), k) for k in range(1, len(made) + 1)]
+    for (_, kw, k), (status, made) in zip(calls, launches(calls)):
+        assert status == -4 and len(made) == k, (kw["sizes"][:5], k)
