@@ -270,6 +270,41 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
                        const float* mean, const float* rstd, const void* gy, void* gx, float* ggamma, float* gbeta,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* Layer norm with an activation: the statistics of every (batch entry, point) over its C channels,
+ *   mean = sum_c x / C, var = sum_c (x - mean)^2 / C;  rstd = 1 / sqrt(var + eps);  xh = (x - mean) rstd;
+ *   y = act(gamma xh + beta), gamma and beta [C], one value a channel.
+ * Layouts, dtypes and activations as for the group norm above (rows of any other model are FNO_LAYOUT_CHANNELS_LAST).
+ * Statistics and sums over channels are in float, about a mean of their own, so that a point's values may lie anywhere beside
+ * their spread; bf16 results are rounded once, to nearest even.  Range: x to 1e18 in size; squares of deviations below
+ * 1e-38 are lost, which shows where eps is as small.  A NaN or an infinity makes all channels of its point NaN, and no other
+ * point.  One channel gives xh = 0. */
+typedef struct {
+  int64_t npoints;     /* P >= 0                                                      */
+  double eps;          /* >= 0, finite; with 0 a point of equal channels gives NaN    */
+  int32_t batch;       /* B, 1 .. 65535                                               */
+  int32_t channels;    /* C, 1 .. 1024 channels first, 1 .. 16384 channels last       */
+  int32_t layout;      /* FNO_LAYOUT_*                                                */
+  int32_t dtype;       /* FNO_DTYPE_*, of x, y, gy and gx                             */
+  int32_t activation;  /* FNO_ACT_*                                                   */
+  int32_t flags;       /* FNO_FLAG_ACCUMULATE_GRADS (of the backward call) or 0       */
+} fno_layer_norm_desc;
+
+/* Forward.  gamma, beta nullable (1 and 0).  y may be x itself; no other overlap.  x and y 16-byte aligned; they may be null
+ * where npoints is 0.  Needs no workspace, and saves nothing: the adjoint has x's statistics at hand when it has x. */
+int fno_layer_norm_fwd(const fno_layer_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
+                       void* stream);
+
+/* Adjoint for the cotangent gy of y, with gz = gy act'(gamma xh + beta) and h = gamma gz:
+ *   gbeta[c] = sum gz,  ggamma[c] = sum gz xh  (over batch entries and points, Sec. 2.1),
+ *   gx = rstd (h - sum_c h / C - xh sum_c h xh / C).
+ * gx, ggamma, gbeta nullable; gx is overwritten and may be gy or x itself (no other overlap); ggamma and gbeta are
+ * overwritten, or added to with FNO_FLAG_ACCUMULATE_GRADS; npoints = 0 gives gradients of zero.  Sums over points: floats in a fixed
+ * order within a block, then double; the same bits on every run.  ws: device scratch of fno_layer_norm_workspace_bytes() bytes
+ * (host-only call), 256-byte aligned. */
+int fno_layer_norm_workspace_bytes(const fno_layer_norm_desc* desc, size_t* bytes);
+int fno_layer_norm_bwd(const fno_layer_norm_desc* desc, const void* x, const float* gamma, const float* beta, const void* gy,
+                       void* gx, float* ggamma, float* gbeta, void* ws, size_t ws_bytes, void* stream);
+
 /* One AdamW step over many tensors (Loshchilov & Hutter, Algorithm 2: Adam, Sec. 4, with the decay apart from the
  * gradient), in place, in as few launches as the tensors' addresses fit (64 tensors each).  For every value
  *   g' = s g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
@@ -313,6 +348,46 @@ int fno_grad_norm(int32_t count, const fno_adamw_tensor* tensors, float* norm, v
  * used. */
 int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* const* m_out, void* const* v_out,
                          void* stream);
+
+/* One Muon step over many tensors of matrices, in place: the momentum of every matrix, made orthogonal by Newton-Schulz
+ * products (Higham, Functions of Matrices, ch. 8), is what moves it.  For every matrix on its own
+ *   g' = s g;  m = momentum m + g';  u = g' + momentum m where nesterov is set, else m;  X = u / (||u||_F + eps);
+ *   `iterations` times:  X = a X + (b A + c A A) X,  A = X X^H;
+ *   param = param (1 - lr weight_decay) - lr scale X,
+ * s from grad_norm and max_norm as in fno_adamw_step: where *grad_norm is not finite nothing is written at all.  A matrix of
+ * zeros stays one (X = 0), one that holds a NaN or an infinity becomes NaN, and no other matrix of the list does.
+ *
+ * kind FNO_MUON_MATRICES: float [batch][rows][cols], a stack of real matrices (batch 1: one).
+ * kind FNO_MUON_MODES: complex [rows][cols][batch], the layout of the spectral weights R [Cin][Cout][modes]: one complex matrix
+ * for every kept mode, the map that the mode mix applies there.  rows, cols <= 32 (FNO_EUNSUPPORTED beyond).
+ *
+ * Products: single precision, or sums of products of 16-bit parts that carry 22 bits of the largest value of a matrix (real
+ * matrices with more than 32 on their shorter side).
+ *
+ * tensors, options: host memory, read during the call only; pointers in tensors are device pointers, param, grad and momentum
+ * 4-byte aligned (8-byte: complex ones).  Tensors must not overlap.  Empty tensors (batch, rows or cols 0) and count = 0 are
+ * allowed.  ws: device scratch of fno_muon_workspace_bytes() bytes (host-only call), 256-byte aligned; null where that is 0. */
+enum { FNO_MUON_MATRICES = 0, FNO_MUON_MODES = 1 };
+typedef struct {
+  float* param;
+  const float* grad;
+  float* momentum;
+  int64_t batch;         /* matrices, 0 .. 2^31 - 1                                   */
+  int32_t rows, cols;    /* 0 .. 32768                                                */
+  int32_t kind;          /* FNO_MUON_*                                                */
+  double scale;          /* of the step; finite                                       */
+  double weight_decay;   /* finite                                                    */
+} fno_muon_tensor;
+typedef struct {
+  double lr, momentum;   /* finite; 0 <= momentum < 1                                 */
+  double eps;            /* >= 0                                                      */
+  double a, b, c;        /* finite                                                    */
+  int32_t iterations;    /* 0 .. 64                                                   */
+  int32_t nesterov;      /* 0 or 1                                                    */
+} fno_muon_options;
+int fno_muon_workspace_bytes(int32_t count, const fno_muon_tensor* tensors, size_t* bytes);
+int fno_muon_step(int32_t count, const fno_muon_tensor* tensors, const fno_muon_options* options, const float* grad_norm,
+                  double max_norm, void* ws, size_t ws_bytes, void* stream);
 
 /* Projection to the output channels (end of Sec. 2.4) through one hidden layer, fused per point:
  *   y = W2 gelu(W1 x + b1) + b2,  W1 [hidden][c_in], W2 [c_out][hidden].  The hidden tensor is

@@ -527,6 +527,62 @@ def group_norm_bwd(x, gamma, beta, mean, rstd, groups, gy, act="gelu"):
     return {"gx": (rs * (gh - s1 - xh * s2)).reshape(x.shape), "ggamma": (gz * xh).sum((0, 2)), "gbeta": gz.sum((0, 2))}
 
 
+def layer_norm_fwd(x, gamma, beta, eps, act="gelu"):
+    """Layer norm with an activation of x (B, C, ...): statistics of every point over its channels.  gamma, beta None = 1, 0."""
+    x = np.asarray(x, np.float64)
+    side = (1, -1) + (1,) * (x.ndim - 2)
+    d = x - x.mean(1, keepdims=True)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        z = d / np.sqrt((d ** 2).mean(1, keepdims=True) + eps)
+    z = z * (1.0 if gamma is None else np.asarray(gamma, np.float64).reshape(side))
+    return _ACTS[act][0](z + (0.0 if beta is None else np.asarray(beta, np.float64).reshape(side)))
+
+
+def layer_norm_bwd(x, gamma, beta, eps, gy, act="gelu"):
+    """Adjoint of layer_norm_fwd for a cotangent gy: the chain rule through act, the affine map, and xh = d rstd, whose mean and
+    rstd depend on every channel of the point."""
+    x, gy = np.asarray(x, np.float64), np.asarray(gy, np.float64)
+    side, over = (1, -1) + (1,) * (x.ndim - 2), (0,) + tuple(range(2, x.ndim))
+    ga = np.ones(x.shape[1]) if gamma is None else np.asarray(gamma, np.float64)
+    be = np.zeros(x.shape[1]) if beta is None else np.asarray(beta, np.float64)
+    d = x - x.mean(1, keepdims=True)
+    rstd = 1.0 / np.sqrt((d ** 2).mean(1, keepdims=True) + eps)
+    xh = d * rstd
+    gz = gy * _ACTS[act][1](xh * ga.reshape(side) + be.reshape(side))
+    h = gz * ga.reshape(side)
+    gx = rstd * (h - h.mean(1, keepdims=True) - xh * (h * xh).mean(1, keepdims=True))
+    return {"gx": gx, "ggamma": (gz * xh).sum(over), "gbeta": gz.sum(over)}
+
+
+def newton_schulz(u, iterations=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    """X = u / (|u|_F + eps), then `iterations` times X = a X + (b A + c A A) X with A = X X^H, for matrices (..., rows, cols), real or
+    complex.  A matrix of zeros stays one."""
+    x = np.asarray(u, np.complex128 if np.iscomplexobj(u) else np.float64)
+    size = np.sqrt((np.abs(x) ** 2).sum((-2, -1), keepdims=True))
+    x = x / np.where(size == 0, 1.0, size + eps)
+    a, b, c = coefficients
+    for _ in range(iterations):
+        A = x @ np.conj(np.swapaxes(x, -1, -2))
+        x = a * x + (b * A + c * (A @ A)) @ x
+    return x
+
+
+def muon_step(param, grad, momentum, lr, mu, scale=1.0, weight_decay=0.0, nesterov=True, grad_scale=1.0, **kw):
+    """One Muon step of a tensor: real (..., rows, cols), or complex (rows, cols, modes...) with one matrix a mode.  Returns
+    (param, momentum)."""
+    kind = np.complex128 if np.iscomplexobj(param) else np.float64
+    param, grad, momentum = (np.asarray(t, kind) for t in (param, grad, momentum))
+    g = grad * grad_scale
+    m = mu * momentum + g
+    u = g + mu * m if nesterov else m
+    if kind is np.complex128:
+        x = newton_schulz(np.moveaxis(u.reshape(u.shape[:2] + (-1,)), 2, 0), **kw)
+        x = np.moveaxis(x, 0, 2).reshape(u.shape)
+    else:
+        x = newton_schulz(u, **kw)
+    return param * (1.0 - lr * weight_decay) - lr * scale * x, m
+
+
 def adamw_step(param, grad, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, scale=1.0):
     """One update of AdamW: Adam of the scaled gradient, and the parameter's own decay apart from it.  Returns
     (param, m, v)."""

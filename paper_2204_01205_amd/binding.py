@@ -21,6 +21,7 @@ FNO_ACT_IDENTITY, FNO_ACT_GELU = 0, 1
 FNO_ACT_SILU = 2                 # group norm only
 FNO_LAYOUT_CHANNELS_FIRST, FNO_LAYOUT_CHANNELS_LAST = 0, 1
 FNO_DTYPE_F32, FNO_DTYPE_BF16 = 0, 1
+FNO_MUON_MATRICES, FNO_MUON_MODES = 0, 1
 FNO_OP_SPECTRAL_CONV_FWD, FNO_OP_SPECTRAL_CONV_BWD, FNO_OP_BLOCK_FWD, FNO_OP_BLOCK_BWD = 0, 1, 2, 3
 FNO_FLAG_MSE_TARGET = 1
 FNO_FLAG_ACCUMULATE_GRADS = 2
@@ -35,6 +36,7 @@ EXPORTS = [
     "fno_time_lift_bwd_workspace_bytes", "fno_time_lift_bwd",
     "fno_spectral_conv_fwd_static",
     "fno_group_norm_workspace_bytes", "fno_group_norm_fwd", "fno_group_norm_bwd",
+    "fno_layer_norm_workspace_bytes", "fno_layer_norm_fwd", "fno_layer_norm_bwd", "fno_muon_workspace_bytes", "fno_muon_step",
     "fno_adamw_step", "fno_grad_norm_workspace_bytes", "fno_grad_norm", "fno_adamw_state_read",
     "fno_status_string", "fno_timing_enable", "fno_timing_read",
 ]
@@ -53,6 +55,23 @@ class FnoNormDesc(ctypes.Structure):
     _fields_ = [("npoints", ctypes.c_int64), ("eps", ctypes.c_double), ("batch", ctypes.c_int32),
                 ("channels", ctypes.c_int32), ("groups", ctypes.c_int32), ("layout", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class FnoLayerNormDesc(ctypes.Structure):
+    _fields_ = [("npoints", ctypes.c_int64), ("eps", ctypes.c_double), ("batch", ctypes.c_int32),
+                ("channels", ctypes.c_int32), ("layout", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class FnoMuonTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p), ("batch", ctypes.c_int64),
+                ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("kind", ctypes.c_int32), ("scale", ctypes.c_double),
+                ("weight_decay", ctypes.c_double)]
+
+
+class FnoMuonOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("eps", ctypes.c_double), ("a", ctypes.c_double),
+                ("b", ctypes.c_double), ("c", ctypes.c_double), ("iterations", ctypes.c_int32), ("nesterov", ctypes.c_int32)]
 
 
 class FnoAdamwTensor(ctypes.Structure):
@@ -86,6 +105,9 @@ def lib() -> ctypes.CDLL:
         p, i32, f64, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_double, ctypes.c_size_t
         l.fno_group_norm_fwd.argtypes = [p] * 8 + [size, p]
         l.fno_group_norm_bwd.argtypes = [p] * 11 + [size, p]
+        l.fno_layer_norm_fwd.argtypes = [p] * 6
+        l.fno_layer_norm_bwd.argtypes = [p] * 9 + [size, p]
+        l.fno_muon_step.argtypes = [i32, p, p, p, f64, p, size, p]
         l.fno_adamw_step.argtypes = [i32, p, i32, f64, f64, f64, f64, i32, p, f64, ctypes.c_uint32, p]
         l.fno_grad_norm.argtypes = [i32, p, p, p, size, p]
         l.fno_adamw_state_read.argtypes = [i32, p, p, p, p]
@@ -384,6 +406,132 @@ def fno_group_norm_bwd(desc, x, gamma, beta, mean, rstd, gy, gx, ggamma, gbeta, 
         _check(status)
 
 
+def make_layer_norm_desc(batch: int, channels: int, npoints: int, layout: int = FNO_LAYOUT_CHANNELS_FIRST,
+                         dtype: int = FNO_DTYPE_F32, activation: int = FNO_ACT_GELU, eps: float = 1e-5,
+                         flags: int = 0) -> FnoLayerNormDesc:
+    return FnoLayerNormDesc(npoints, eps, batch, channels, layout, dtype, activation, flags)
+
+
+def fno_layer_norm_workspace_bytes(desc: FnoLayerNormDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fno_layer_norm_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_layer_norm_workspace(desc: FnoLayerNormDesc, device="cuda") -> torch.Tensor:
+    """Scratch of the backward call (the forward call needs none)."""
+    return torch.empty(max(fno_layer_norm_workspace_bytes(desc), 256), dtype=torch.uint8, device=device)
+
+
+def _layer_norm_stream(desc, device) -> tuple:
+    """Type and number of a field's values, and the current stream of the GPU that the field lives on, which has to be the
+    current one."""
+    current = torch.cuda.current_device()
+    if device.index != current:
+        raise ValueError(f"the tensors live on {device}, the current device is cuda:{current}")
+    dtype = torch.bfloat16 if desc.dtype == FNO_DTYPE_BF16 else torch.float32
+    return dtype, desc.batch * desc.channels * desc.npoints, _raw_stream(current)
+
+
+def _one_device(device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} lives on {t.device}, not on {device}")
+
+
+def fno_layer_norm_fwd(desc, x, gamma, beta, y) -> None:
+    _one_device(x.device, gamma=gamma, beta=beta, y=y)
+    if not x.is_cuda:
+        raise ValueError("x must live on the GPU")
+    dtype, field, stream = _layer_norm_stream(desc, x.device)
+    channels, f32 = desc.channels, torch.float32
+    status = lib().fno_layer_norm_fwd(
+        ctypes.byref(desc), _address(x, dtype, field, "x"), _address(gamma, f32, channels, "gamma"),
+        _address(beta, f32, channels, "beta"), _address(y, dtype, field, "y"), stream)
+    if status:
+        _check(status)
+
+
+def fno_layer_norm_bwd(desc, x, gamma, beta, gy, gx, ggamma, gbeta, ws) -> None:
+    _one_device(x.device, gamma=gamma, beta=beta, gy=gy, gx=gx, ggamma=ggamma, gbeta=gbeta, ws=ws)
+    if not x.is_cuda:
+        raise ValueError("x must live on the GPU")
+    dtype, field, stream = _layer_norm_stream(desc, x.device)
+    channels, f32 = desc.channels, torch.float32
+    status = lib().fno_layer_norm_bwd(
+        ctypes.byref(desc), _address(x, dtype, field, "x"), _address(gamma, f32, channels, "gamma"),
+        _address(beta, f32, channels, "beta"), _address(gy, dtype, field, "gy"), _address(gx, dtype, field, "gx"),
+        _address(ggamma, f32, channels, "ggamma"), _address(gbeta, f32, channels, "gbeta"),
+        _address(ws, torch.uint8, ws.numel(), "ws"), ws.numel(), stream)
+    if status:
+        _check(status)
+
+
+class MuonTensors:
+    """The host array of matrices that fno_muon_step takes, and the tensors themselves, which have to live as long as the
+    array is used.  Built by make_muon_tensors().  The array holds addresses: a program that puts another tensor in the place of
+    one of these has to build the list again, or the calls go on with the old one."""
+
+    def __init__(self, array, count, device, keep):
+        self.array, self.count, self.device, self.keep = array, count, device, keep
+
+
+def make_muon_tensors(params, grads, momentum, scale=1.0, weight_decay=0.0) -> MuonTensors:
+    """Lists of tensors on one GPU, parameter, gradient and momentum of a kind and shape each.  float32 [rows][cols] or
+    [batch][rows][cols]: real matrices; complex64 [rows][cols] or [rows][cols][modes...]: one complex matrix a mode, as the
+    spectral weights R [c_in][c_out][kx][ky][kz][kt] are.  scale, weight_decay: one number, or one a tensor."""
+    count = len(params)
+    each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * count
+    scale, decay = each(scale), each(weight_decay)
+    if not (len(grads) == len(momentum) == len(scale) == len(decay) == count):
+        raise ValueError("params, grads, momentum, scale and weight_decay must have one entry a tensor")
+    array, devices = (FnoMuonTensor * max(count, 1))(), set()
+    for k in range(count):
+        p, is_complex = params[k], params[k].is_complex()
+        if p.dim() < 2 or (not is_complex and p.dim() > 3):
+            raise ValueError(f"params[{k}] has {p.dim()} axes: matrices have two, a stack of real ones three")
+        rows, cols = p.shape[:2] if is_complex else p.shape[-2:]
+        batch = 1
+        for n in p.shape[2:] if is_complex else p.shape[:-2]:
+            batch *= int(n)
+        dtype = torch.complex64 if is_complex else torch.float32
+        for name, t in (("params", p), ("grads", grads[k]), ("momentum", momentum[k])):
+            if t.shape != p.shape or t.dtype != dtype:
+                raise ValueError(f"{name}[{k}] is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(p.shape)}")
+            if t.is_conj():
+                raise ValueError(f"{name}[{k}] is a conjugate view")
+        array[k] = FnoMuonTensor(_ptr(p, name=f"params[{k}]"), _ptr(grads[k], name=f"grads[{k}]"),
+                                 _ptr(momentum[k], name=f"momentum[{k}]"), batch, rows, cols,
+                                 FNO_MUON_MODES if is_complex else FNO_MUON_MATRICES, scale[k], decay[k])
+        devices |= {t.device for t in (p, grads[k], momentum[k])}
+    if len(devices) > 1:
+        raise ValueError("all tensors of a list must live on one GPU")
+    return MuonTensors(array, count, devices.pop() if devices else None, (list(params), list(grads), list(momentum)))
+
+
+def fno_muon_workspace_bytes(tensors: MuonTensors) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().fno_muon_workspace_bytes(ctypes.c_int32(tensors.count), tensors.array, ctypes.byref(n)))
+    return int(n.value)
+
+
+def alloc_muon_workspace(tensors: MuonTensors, device="cuda") -> torch.Tensor:
+    return torch.empty(max(fno_muon_workspace_bytes(tensors), 256), dtype=torch.uint8, device=device)
+
+
+def fno_muon_step(tensors: MuonTensors, lr, momentum, ws, iterations=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7,
+                  nesterov=True, grad_norm=None, max_norm=1.0) -> None:
+    stream = _list_stream(tensors)
+    if tensors.device is not None:
+        _one_device(tensors.device, ws=ws, grad_norm=grad_norm)
+    options = FnoMuonOptions(lr, momentum, eps, *coefficients, iterations, 1 if nesterov else 0)
+    status = lib().fno_muon_step(tensors.count, tensors.array, ctypes.addressof(options),
+                                 _address(grad_norm, torch.float32, 1, "grad_norm"), max_norm,
+                                 _address(ws, torch.uint8, ws.numel(), "ws"), ws.numel(), stream)
+    if status:
+        _check(status)
+
+
 class AdamwTensors:
     """The host array of tensors that fno_adamw_step, fno_grad_norm and fno_adamw_state_read take, and the tensors
     themselves, which have to live as long as the array is used.  Built by make_adamw_tensors().  The array holds addresses: a
@@ -426,6 +574,19 @@ def make_adamw_tensors(params, grads, m, v, exps=None, weight_decay=0.0) -> Adam
         raise ValueError("all tensors of a list must live on one GPU")
     return AdamwTensors(array, count, sizes, 32 if exps is None else 8, devices.pop() if devices else None,
                         (list(params), list(grads), list(m), list(v), None if exps is None else list(exps)))
+
+
+def make_grad_tensors(grads) -> AdamwTensors:
+    """A list of gradients alone (float32 or complex64, on one GPU), for fno_grad_norm: of parameters that different
+    optimizers move."""
+    array, sizes, devices = (FnoAdamwTensor * max(len(grads), 1))(), [], set()
+    for k, g in enumerate(grads):
+        sizes.append(g.numel() * (2 if g.is_complex() else 1))
+        array[k] = FnoAdamwTensor(None, _ptr(g, name=f"grads[{k}]"), None, None, None, sizes[k], 0.0)
+        devices.add(g.device)
+    if len(devices) > 1:
+        raise ValueError("all tensors of a list must live on one GPU")
+    return AdamwTensors(array, len(grads), sizes, 32, devices.pop() if devices else None, (list(grads),))
 
 
 def _list_stream(tensors: AdamwTensors) -> int:

@@ -372,6 +372,50 @@ int check_norm_ws(const fno::NormShape& n, void* ws, size_t ws_bytes) {
   return FNO_OK;
 }
 
+// Validates a layer norm's descriptor.
+int layer_shape(const fno_layer_norm_desc* d, fno::LayerShape* n) {
+  if (d == nullptr) { set_detail("descriptor is null"); return FNO_EINVAL; }
+  if (d->batch < 1 || d->channels < 1 || d->npoints < 0) { set_detail("batch and channels must be >= 1, npoints >= 0"); return FNO_EINVAL; }
+  if (d->layout != FNO_LAYOUT_CHANNELS_FIRST && d->layout != FNO_LAYOUT_CHANNELS_LAST) { set_detail("unknown layout"); return FNO_EINVAL; }
+  if (d->dtype != FNO_DTYPE_F32 && d->dtype != FNO_DTYPE_BF16) { set_detail("unknown dtype"); return FNO_EINVAL; }
+  if (d->activation != FNO_ACT_IDENTITY && d->activation != FNO_ACT_GELU && d->activation != FNO_ACT_SILU) { set_detail("unknown activation"); return FNO_EINVAL; }
+  if (d->flags & ~FNO_FLAG_ACCUMULATE_GRADS) { set_detail("unknown flag bits"); return FNO_EINVAL; }
+  if (!(d->eps >= 0.0) || !std::isfinite(d->eps)) { set_detail("eps must be finite and at least 0"); return FNO_EINVAL; }
+  const bool last = d->layout == FNO_LAYOUT_CHANNELS_LAST;
+  if (d->channels > (last ? fno::kMaxLayerChannelsLast : fno::kMaxLayerChannelsFirst) || d->batch > 65535 ||
+      d->npoints > ((int64_t)1 << 40) || (double)d->batch * d->channels * (double)d->npoints > 17592186044416.0) {
+    set_detail("layer_norm covers channels <= %d (first) or %d (last), batch <= 65535, 2^44 values", fno::kMaxLayerChannelsFirst, fno::kMaxLayerChannelsLast);
+    return FNO_EUNSUPPORTED;
+  }
+  *n = fno::LayerShape{d->batch, d->channels, d->npoints, last, d->dtype == FNO_DTYPE_BF16, d->activation, d->eps};
+  return FNO_OK;
+}
+
+// Validates a list of matrices; `pointers`: whether the call uses them.
+int muon_list(int32_t count, const fno_muon_tensor* t, bool pointers, std::vector<fno::MuonTensor>* out) {
+  if (count < 0 || (count > 0 && t == nullptr)) { set_detail("count must be non-negative, tensors not null"); return FNO_EINVAL; }
+  out->reserve((size_t)count);
+  double values = 0.0;
+  for (int k = 0; k < count; ++k) {
+    if (t[k].kind != FNO_MUON_MATRICES && t[k].kind != FNO_MUON_MODES) { set_detail("unknown kind of tensor %d", k); return FNO_EINVAL; }
+    if (t[k].batch < 0 || t[k].rows < 0 || t[k].cols < 0) { set_detail("sizes of tensor %d must be non-negative", k); return FNO_EINVAL; }
+    if (!std::isfinite(t[k].scale) || !std::isfinite(t[k].weight_decay)) { set_detail("scale and weight_decay of tensor %d must be finite", k); return FNO_EINVAL; }
+    const bool modes = t[k].kind == FNO_MUON_MODES;
+    const int side = modes ? fno::kMaxMuonModes : fno::kMaxMuonSide;
+    if (t[k].rows > side || t[k].cols > side || t[k].batch > INT32_MAX) { set_detail("tensor %d: muon_step covers rows and cols <= %d (matrices) or %d (modes), batch < 2^31", k, fno::kMaxMuonSide, fno::kMaxMuonModes); return FNO_EUNSUPPORTED; }
+    if (t[k].batch == 0 || t[k].rows == 0 || t[k].cols == 0) continue;
+    values += (double)t[k].batch * t[k].rows * t[k].cols;
+    if (values > 1099511627776.0) { set_detail("muon_step covers lists of up to 2^40 values"); return FNO_EUNSUPPORTED; }
+    if (pointers) {
+      if (t[k].param == nullptr || t[k].grad == nullptr || t[k].momentum == nullptr) { set_detail("a pointer of tensor %d is null", k); return FNO_EINVAL; }
+      const uintptr_t bits = reinterpret_cast<uintptr_t>(t[k].param) | reinterpret_cast<uintptr_t>(t[k].grad) | reinterpret_cast<uintptr_t>(t[k].momentum);
+      if (bits & (modes ? 7 : 3)) { set_detail("pointers of tensor %d must be %d-byte aligned", k, modes ? 8 : 4); return FNO_EINVAL; }
+    }
+    out->push_back(fno::MuonTensor{t[k].param, t[k].grad, t[k].momentum, t[k].batch, t[k].rows, t[k].cols, modes, t[k].scale, t[k].weight_decay});
+  }
+  return FNO_OK;
+}
+
 // Validates a list of tensors; `need`: which of their pointers the call uses.
 enum { kAdamwParam = 1, kAdamwGrad = 2, kAdamwState = 4, kAdamwCodes = 8 };
 int adamw_list(int32_t count, const fno_adamw_tensor* t, int need, std::vector<fno::AdamwTensor>* out) {
@@ -670,6 +714,80 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
                                      (desc->flags & FNO_FLAG_ACCUMULATE_GRADS) ? 1 : 0, ws,
                                      static_cast<hipStream_t>(stream)));
   return FNO_OK;
+}
+
+int fno_layer_norm_workspace_bytes(const fno_layer_norm_desc* desc, size_t* bytes) {
+  fno::LayerShape n;
+  const int rc = layer_shape(desc, &n);
+  if (rc != FNO_OK) return rc;
+  if (bytes == nullptr) { set_detail("bytes is required"); return FNO_EINVAL; }
+  *bytes = fno::layer_norm_workspace_bytes(n);
+  return FNO_OK;
+}
+
+int fno_layer_norm_fwd(const fno_layer_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
+                       void* stream) {
+  fno::LayerShape n;
+  const int rc = layer_shape(desc, &n);
+  if (rc != FNO_OK) return rc;
+  if (n.P == 0) return FNO_OK;
+  if (x == nullptr || y == nullptr) { set_detail("x and y are required"); return FNO_EINVAL; }
+  if (misaligned16(x, y)) return FNO_EINVAL;
+  FNO_HIP(fno::launch_layer_norm_fwd(n, x, gamma, beta, y, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+}
+
+int fno_layer_norm_bwd(const fno_layer_norm_desc* desc, const void* x, const float* gamma, const float* beta, const void* gy,
+                       void* gx, float* ggamma, float* gbeta, void* ws, size_t ws_bytes, void* stream) {
+  fno::LayerShape n;
+  const int rc = layer_shape(desc, &n);
+  if (rc != FNO_OK) return rc;
+  if (n.P > 0 && (x == nullptr || gy == nullptr)) { set_detail("x and gy are required"); return FNO_EINVAL; }
+  if (misaligned16(x, gy, gx)) return FNO_EINVAL;
+  if (ws == nullptr) { set_detail("workspace is null"); return FNO_EINVAL; }
+  if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) { set_detail("workspace must be 256-byte aligned"); return FNO_ENOSPC; }
+  const size_t need = fno::layer_norm_workspace_bytes(n);
+  if (ws_bytes < need) { set_detail("workspace too small: need %lld bytes", (long long)need); return FNO_ENOSPC; }
+  if (gx == nullptr && ggamma == nullptr && gbeta == nullptr) return FNO_OK;
+  FNO_HIP(fno::launch_layer_norm_bwd(n, x, gamma, beta, gy, gx, ggamma, gbeta,
+                                     (desc->flags & FNO_FLAG_ACCUMULATE_GRADS) ? 1 : 0, ws, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+}
+
+int fno_muon_workspace_bytes(int32_t count, const fno_muon_tensor* tensors, size_t* bytes) try {
+  if (bytes == nullptr) { set_detail("bytes is required"); return FNO_EINVAL; }
+  std::vector<fno::MuonTensor> list;
+  const int rc = muon_list(count, tensors, false, &list);
+  if (rc != FNO_OK) return rc;
+  *bytes = fno::muon_workspace_bytes(list.data(), (int)list.size());
+  return FNO_OK;
+} catch (const std::bad_alloc&) {
+  set_detail("out of host memory");
+  return FNO_EHIP;
+}
+
+int fno_muon_step(int32_t count, const fno_muon_tensor* tensors, const fno_muon_options* o, const float* grad_norm,
+                  double max_norm, void* ws, size_t ws_bytes, void* stream) try {
+  if (o == nullptr) { set_detail("options are null"); return FNO_EINVAL; }
+  if (!std::isfinite(o->lr) || !(o->momentum >= 0.0 && o->momentum < 1.0)) { set_detail("lr must be finite, momentum in [0, 1)"); return FNO_EINVAL; }
+  if (!(o->eps >= 0.0) || !std::isfinite(o->eps)) { set_detail("eps must be finite and at least 0"); return FNO_EINVAL; }
+  if (!std::isfinite(o->a) || !std::isfinite(o->b) || !std::isfinite(o->c)) { set_detail("a, b and c must be finite"); return FNO_EINVAL; }
+  if (o->iterations < 0 || o->iterations > 64) { set_detail("iterations must lie in 0 .. 64"); return FNO_EINVAL; }
+  if (o->nesterov != 0 && o->nesterov != 1) { set_detail("nesterov must be 0 or 1"); return FNO_EINVAL; }
+  if (grad_norm != nullptr && !(max_norm > 0.0)) { set_detail("max_norm must be positive"); return FNO_EINVAL; }
+  std::vector<fno::MuonTensor> list;
+  const int rc = muon_list(count, tensors, true, &list);
+  if (rc != FNO_OK) return rc;
+  const size_t need = fno::muon_workspace_bytes(list.data(), (int)list.size());
+  if (need > 0 && ws == nullptr) { set_detail("workspace is null"); return FNO_EINVAL; }
+  if ((reinterpret_cast<uintptr_t>(ws) & 255) != 0) { set_detail("workspace must be 256-byte aligned"); return FNO_ENOSPC; }
+  if (ws_bytes < need) { set_detail("workspace too small: need %lld bytes", (long long)need); return FNO_ENOSPC; }
+  const fno::MuonStep st{o->lr, o->momentum, o->eps, o->a, o->b, o->c, o->iterations, o->nesterov != 0, grad_norm, max_norm};
+  FNO_HIP(fno::launch_muon(list.data(), (int)list.size(), st, ws, static_cast<hipStream_t>(stream)));
+  return FNO_OK;
+} catch (const std::bad_alloc&) {
+  set_detail("out of host memory");
+  return FNO_EHIP;
 }
 
 int fno_adamw_step(int32_t count, const fno_adamw_tensor* tensors, int32_t state_bits, double lr, double beta1,

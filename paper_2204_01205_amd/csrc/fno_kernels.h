@@ -147,6 +147,42 @@ hipError_t launch_group_norm_bwd(const NormShape& n, const void* x, const float*
                                  const float* mean, const float* rstd, const void* gy, void* gx, float* ggamma,
                                  float* gbeta, int accumulate, void* ws, hipStream_t s);
 
+// Layer norm with an activation (fno_layer_norm.hip).  x, y, gy, gx as for the group norm.  Outputs of the adjoint nullable.
+// ws: layer_norm_workspace_bytes() of scratch (adjoint only).
+struct LayerShape {
+  int B, C;
+  int64_t P;
+  bool last, bf16;
+  int act;             // 0 identity, 1 GELU, 2 SiLU
+  double eps;
+};
+constexpr int kMaxLayerChannelsFirst = 1024, kMaxLayerChannelsLast = 16384;
+size_t layer_norm_workspace_bytes(const LayerShape& n);
+hipError_t launch_layer_norm_fwd(const LayerShape& n, const void* x, const float* gamma, const float* beta, void* y, hipStream_t s);
+hipError_t launch_layer_norm_bwd(const LayerShape& n, const void* x, const float* gamma, const float* beta, const void* gy,
+                                 void* gx, float* ggamma, float* gbeta, int accumulate, void* ws, hipStream_t s);
+
+// Muon step over the tensors of a list (fno_muon.hip).  ws: muon_workspace_bytes() of scratch.
+struct MuonTensor {
+  float* p;
+  const float* g;
+  float* m;
+  int64_t batch;
+  int rows, cols;
+  bool modes;          // complex [rows][cols][batch], else float [batch][rows][cols]
+  double scale, decay;
+};
+struct MuonStep {
+  double lr, momentum, eps, a, b, c;
+  int iterations;
+  bool nesterov;
+  const float* norm;   // device scalar, nullable
+  double max_norm;
+};
+constexpr int kMaxMuonModes = 32, kMaxMuonSide = 32768;
+size_t muon_workspace_bytes(const MuonTensor* t, int count);
+hipError_t launch_muon(const MuonTensor* t, int count, const MuonStep& st, void* ws, hipStream_t s);
+
 // AdamW over the tensors of a list, the norm of their gradients, and what 8-bit moments stand for (fno_adamw.hip).
 struct AdamwTensor {
   float* p;
