@@ -1,0 +1,39 @@
+// What the Muon step's kernels share.
+#pragma once
+#include "fno_device.h"
+
+namespace fno {
+
+// Numbers of a step that all matrices have in common
+struct MuonScalars {
+  float mu, a, b, c, max_norm;
+  int nesterov, iterations;
+  double eps;
+  const float* norm;      // device scalar, nullable
+};
+
+// Steps of the spectral weights (fno_muon_modes.hip)
+hipError_t launch_muon_modes(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);
+
+namespace {
+
+// What the gradient is multiplied by; false where the norm is not finite.
+__device__ __forceinline__ bool muon_scale(const MuonScalars& c, float& scale) {
+  scale = 1.0f;
+  if (c.norm == nullptr) return true;
+  const float norm = *c.norm;
+  if (!(norm <= 3.402823466e38f)) return false;
+  if (norm > c.max_norm) scale = c.max_norm / norm;
+  return true;
+}
+// New momentum, and what is made orthogonal
+__device__ __forceinline__ float muon_momentum(const MuonScalars& c, float g, float& m) {
+  m = fmaf(c.mu, m, g);
+  return c.nesterov ? fmaf(c.mu, m, g) : m;
+}
+// 1 / (|u|_F + eps); a matrix of zeros stays one.  Squares are in double, which holds those of all floats.
+__device__ __forceinline__ double muon_inverse(double squares, double eps) { return squares == 0.0 ? 0.0 : 1.0 / (sqrt(squares) + eps); }
+
+}  // namespace
+
+}  // namespace fno

@@ -2,7 +2,7 @@
 //
 // Plain kernel: a block has a matrix, keeps X, its Gram matrix and the polynomial of it in scratch, and a thread an entry of
 // each product at a time.
-#include "fno_device.h"
+#include "fno_muon.h"
 
 namespace fno {
 
@@ -121,7 +121,12 @@ size_t muon_workspace_bytes(const MuonTensor* t, int count) {
 }
 
 hipError_t launch_muon(const MuonTensor* t, int count, const MuonStep& st, void* ws, hipStream_t s) {
+  const MuonScalars c{(float)st.momentum, (float)st.a, (float)st.b, (float)st.c, (float)st.max_norm, st.nesterov ? 1 : 0,
+                      st.iterations, st.eps, st.norm};
+  const hipError_t e = launch_muon_modes(t, count, c, st.lr, s);
+  if (e != hipSuccess) return e;
   for (int k = 0; k < count; ++k) {
+    if (t[k].modes) continue;
     const bool tall = t[k].rows > t[k].cols;
     const long long row = t[k].modes ? t[k].cols * t[k].batch : t[k].cols, col = t[k].modes ? t[k].batch : 1;
     const MuonArgs a{t[k].p, t[k].m, t[k].g, st.norm, (long long)t[k].batch, tall ? col : row, tall ? row : col,
