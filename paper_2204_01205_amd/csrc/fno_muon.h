@@ -15,6 +15,10 @@ struct MuonScalars {
 // Steps of the spectral weights (fno_muon_modes.hip)
 hipError_t launch_muon_modes(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);
 
+// Steps of the small real matrices of a list (fno_muon_small.hip)
+bool muon_is_small(const MuonTensor& t);
+hipError_t launch_muon_small(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);
+
 namespace {
 
 // What the gradient is multiplied by; false where the norm is not finite.

@@ -116,17 +116,20 @@ size_t scratch_of(const MuonTensor& t) {
 
 size_t muon_workspace_bytes(const MuonTensor* t, int count) {
   size_t most = 0;
-  for (int k = 0; k < count; ++k) most = scratch_of(t[k]) > most ? scratch_of(t[k]) : most;
+  for (int k = 0; k < count; ++k)
+    if (!t[k].modes && !muon_is_small(t[k])) most = scratch_of(t[k]) > most ? scratch_of(t[k]) : most;
   return most;
 }
 
 hipError_t launch_muon(const MuonTensor* t, int count, const MuonStep& st, void* ws, hipStream_t s) {
   const MuonScalars c{(float)st.momentum, (float)st.a, (float)st.b, (float)st.c, (float)st.max_norm, st.nesterov ? 1 : 0,
                       st.iterations, st.eps, st.norm};
-  const hipError_t e = launch_muon_modes(t, count, c, st.lr, s);
+  hipError_t e = launch_muon_modes(t, count, c, st.lr, s);
+  if (e != hipSuccess) return e;
+  e = launch_muon_small(t, count, c, st.lr, s);
   if (e != hipSuccess) return e;
   for (int k = 0; k < count; ++k) {
-    if (t[k].modes) continue;
+    if (t[k].modes || muon_is_small(t[k])) continue;
     const bool tall = t[k].rows > t[k].cols;
     const long long row = t[k].modes ? t[k].cols * t[k].batch : t[k].cols, col = t[k].modes ? t[k].batch : 1;
     const MuonArgs a{t[k].p, t[k].m, t[k].g, st.norm, (long long)t[k].batch, tall ? col : row, tall ? row : col,
