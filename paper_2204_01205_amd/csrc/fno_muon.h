@@ -19,6 +19,10 @@ hipError_t launch_muon_modes(const MuonTensor* t, int count, const MuonScalars& 
 bool muon_is_small(const MuonTensor& t);
 hipError_t launch_muon_small(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);
 
+// Steps of the other real matrices (fno_muon_dense.hip)
+size_t muon_dense_bytes(const MuonTensor* t, int count);
+hipError_t launch_muon_dense(const MuonTensor* t, int count, const MuonScalars& c, double lr, void* ws, hipStream_t s);
+
 namespace {
 
 // What the gradient is multiplied by; false where the norm is not finite.
@@ -35,8 +39,11 @@ __device__ __forceinline__ float muon_momentum(const MuonScalars& c, float g, fl
   m = fmaf(c.mu, m, g);
   return c.nesterov ? fmaf(c.mu, m, g) : m;
 }
-// 1 / (|u|_F + eps); a matrix of zeros stays one.  Squares are in double, which holds those of all floats.
-__device__ __forceinline__ double muon_inverse(double squares, double eps) { return squares == 0.0 ? 0.0 : 1.0 / (sqrt(squares) + eps); }
+// 1 / (|u|_F + eps); a matrix of zeros stays one, one with an infinity becomes NaN as a whole.  Squares are in double, which
+// holds those of all floats.
+__device__ __forceinline__ double muon_inverse(double squares, double eps) {
+  return squares == 0.0 ? 0.0 : squares < __builtin_huge_val() ? 1.0 / (sqrt(squares) + eps) : __builtin_nan("");
+}
 
 }  // namespace
 
