@@ -9,60 +9,75 @@ namespace {
 
 // Tiles of 64 V points of one batch entry.  The last of an entry goes in tiles of 64, a point a lane.
 struct Tile {
-  long long at;              // this lane's first point, in channel 0
-  int left;                  // points of the entry from there on, V at most
+  long long base;            // its first point in channel 0: the same in all lanes
+  unsigned at;               // from there to this lane's first point; past the entry's end, its last one
+  bool mine;                 // not past the end
 };
 template <int V>
 __device__ __forceinline__ long long tiles_each(long long P) { return (P + 64 * V - 1) / (64 * V); }
+// a value that is the same in all lanes, in scalar registers (a division leaves it in a vector register)
+__device__ __forceinline__ long long uniform(long long v) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
 // body(std::integral_constant<int, V or 1>, tile) for tile number `tile` of all entries
 template <int V, class F>
 __device__ __forceinline__ void with_tile(const LayerArgs& a, long long tile, long long each, F&& body) {
-  const long long b = tile / each, p = (tile - b * each) * (64 * V), base = b * a.C * a.P + p;
+  const long long b = uniform(a.B == 1 ? 0 : tile / each), p = (tile - b * each) * (64 * V), base = b * a.C * a.P + p;
   const int lane = threadIdx.x & 63;
   if (a.P - p >= 64 * V) {
-    body(std::integral_constant<int, V>(), Tile{base + lane * V, V});
+    body(std::integral_constant<int, V>(), Tile{base, (unsigned)(lane * V), true});
   } else {
     const int left = (int)(a.P - p);
-    for (int k = 0; k < left; k += 64) body(std::integral_constant<int, 1>(), Tile{base + k + lane, k + lane < left ? 1 : 0});
+    for (int k = 0; k < left; k += 64) body(std::integral_constant<int, 1>(), Tile{base + k, (unsigned)min(lane, left - 1 - k), k + lane < left});
   }
 }
-// V values of K channels; channels from `have` on read that one's again and count for nothing
-template <class T, int K, int V, bool STREAM>
+// V values of K channels; channels from `have` on read the last one again and count for nothing.  LEAST: have is at least that.
+// A channel's place is the one before's and P more: K products with P would be kept in more scalar registers than there are.
+template <class T, int K, int LEAST, int V, bool STREAM>
 __device__ __forceinline__ void load_channels(const LayerArgs& a, const T* x, const Tile& t, int have, float (&v)[K][V]) {
+  const T* from = x + t.base;
 #pragma unroll
   for (int c = 0; c < K; ++c) {
-    const T* const from = x + t.at + (long long)(c < have ? c : have - 1) * a.P;
-    if constexpr (V == 1) v[c][0] = t.left > 0 ? load1(from) : 0.f;
-    else load_values<V, STREAM>(from, v[c]);
+    load_values<V, STREAM && (V > 1)>(from + t.at, v[c]);
+    if (c + 1 < LEAST || c + 1 < have) from += a.P;
   }
 }
 template <class T, int V, bool STREAM>
 __device__ __forceinline__ void store_channel(T* to, const Tile& t, const float (&v)[V]) {
   if constexpr (V == 1) {
-    if (t.left > 0) store1(to, v[0]);
+    if (t.mine) store1(to + t.at, v[0]);
   } else {
-    store_values<V, STREAM>(to, v);
+    store_values<V, STREAM>(to + t.at, v);
   }
 }
 // x becomes x - about; off and rstd of every point
-template <int K, int V>
+template <int K, int LEAST, int V>
 __device__ __forceinline__ void statistics(const LayerArgs& a, float (&x)[K][V], float (&off)[V], float (&rstd)[V]) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     float s = 0.f, o = 0.f, q = 0.f;
 #pragma unroll
-    for (int c = 0; c < K; ++c) s += c < a.C ? x[c][v] : 0.f;
+    for (int c = 0; c < K; ++c) s += c < LEAST || c < a.C ? x[c][v] : 0.f;
     const float about = s * a.inv_c;
 #pragma unroll
     for (int c = 0; c < K; ++c) {
-      const float d = x[c][v] - about;
-      o += c < a.C ? d : 0.f;
-      q = c < a.C ? fmaf(d, d, q) : q;
+      const float d = x[c][v] - about, in = c < LEAST || c < a.C ? d : 0.f;
+      o += in;
+      q = fmaf(in, in, q);
       x[c][v] = d;
     }
     off[v] = o * a.inv_c;
     rstd[v] = rstd_of(a, off[v], q);
   }
+}
+// gamma and beta of a block's channels, ones and zeros where there are none, to LDS: [2][C], in a kernel's first lines
+__device__ __forceinline__ void load_affine(const LayerArgs& a, float* affine) {
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+    affine[c] = a.gamma ? a.gamma[c] : 1.f;
+    affine[a.C + c] = a.beta ? a.beta[c] : 0.f;
+  }
+  __syncthreads();
 }
 
 // A block's waves take K channels each of the same tile.  Sums go through LDS, [stage][wave][point]; the stages lie apart, so
@@ -124,6 +139,8 @@ template <class T, int KC> constexpr int kFwdPoints = 4;
 template <class T, int KC> constexpr int kBwdPoints = sizeof(T) == 4 ? (KC <= 8 ? 4 : 2) : (KC <= 16 ? 4 : 2);
 template <int K> constexpr int kSharedPoints = K <= 16 ? 2 : 1;
 
+// Channels of a lane, and how many of them there are at least
+template <int KC> constexpr int kLeast = KC == 8 ? 1 : KC == 32 ? 25 : KC - 3;
 template <class F>
 void with_narrow(int C, F&& f) {
   if (C <= 8) f(std::integral_constant<int, 8>());

@@ -6,8 +6,10 @@ namespace fno {
 namespace {
 
 template <class T, int KC, int V, int ACT, bool STREAM>
-__global__ __launch_bounds__(kThreads) void first_bwd_kernel(LayerArgs a, long long tiles, const T* x, const T* gy, T* gx) {
-  __shared__ float sums[kThreads / 64][2 * KC];
+__global__ __launch_bounds__(kThreads, KC <= 20 ? 3 : 2) void first_bwd_kernel(LayerArgs a, long long tiles, const T* x, const T* gy, T* gx) {
+  constexpr int LEAST = kLeast<KC>;
+  __shared__ float sums[kThreads / 64][2 * KC], affine[2 * KC];
+  load_affine(a, affine);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   float sg[KC], sb[KC];
 #pragma unroll
@@ -17,20 +19,19 @@ __global__ __launch_bounds__(kThreads) void first_bwd_kernel(LayerArgs a, long l
     with_tile<V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
       float xh[KC][N], g[KC][N], off[N], rstd[N], s1[N], s2[N];
-      load_channels<T, KC, N, STREAM>(a, x, t, a.C, xh);
-      load_channels<T, KC, N, STREAM>(a, gy, t, a.C, g);
-      statistics<KC, N>(a, xh, off, rstd);
+      load_channels<T, KC, LEAST, N, STREAM>(a, x, t, a.C, xh);
+      load_channels<T, KC, LEAST, N, STREAM>(a, gy, t, a.C, g);
+      statistics<KC, LEAST, N>(a, xh, off, rstd);
 #pragma unroll
       for (int u = 0; u < N; ++u) s1[u] = s2[u] = 0.f;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        if (c >= a.C) continue;
-        const float ga = a.gamma ? a.gamma[c] : 1.f, be = a.beta ? a.beta[c] : 0.f;
-        const float gk = ga * kArg<ACT>, bk = be * kArg<ACT>;
+        if (c >= LEAST && c >= a.C) continue;
+        const float ga = affine[c], gk = ga * kArg<ACT>, bk = affine[a.C + c] * kArg<ACT>;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
           const float h = (xh[c][u] - off[u]) * rstd[u], gz = g[c][u] * slope_f<ACT>(fmaf(h, gk, bk));
-          const bool in = N > 1 || t.left > 0;             // a lane past the end may have a NaN for h
+          const bool in = N > 1 || t.mine;
           sb[c] += in ? gz : 0.f;
           sg[c] = in ? fmaf(gz, h, sg[c]) : sg[c];
           xh[c][u] = h;
@@ -40,12 +41,14 @@ __global__ __launch_bounds__(kThreads) void first_bwd_kernel(LayerArgs a, long l
         }
       }
       if (gx == nullptr) return;
+      T* to = gx + t.base;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        if (c >= a.C) continue;
+        if (c >= LEAST && c >= a.C) continue;
 #pragma unroll
         for (int u = 0; u < N; ++u) g[c][u] = rstd[u] * (fmaf(-s1[u], a.inv_c, g[c][u]) - xh[c][u] * (s2[u] * a.inv_c));
-        store_channel<T, N, STREAM>(gx + t.at + (long long)c * a.P, t, g[c]);
+        store_channel<T, N, STREAM>(to, t, g[c]);
+        to += a.P;
       }
     });
   if (a.part == nullptr) return;
@@ -71,28 +74,33 @@ __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long
   extern __shared__ float lds[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, c0 = w * K, lane = threadIdx.x & 63;
   const int have = a.C - c0 < K ? a.C - c0 : K, stage = waves * 64 * V;
+  const float* const affine = lds + 5 * stage + c0;
+  load_affine(a, lds + 5 * stage);
   const long long each = tiles_each<V>(a.P), down = (long long)c0 * a.P;
   float sg = 0.f, sb = 0.f;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x)
     with_tile<V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
       float xh[K][N], g[AGAIN ? 1 : K][N], off[N], rstd[N], s1[N], s2[N];
-      load_channels<T, K, N, STREAM>(a, x + down, t, have, xh);
-      if constexpr (!AGAIN) load_channels<T, K, N, STREAM>(a, gy + down, t, have, g);
+      load_channels<T, K, 1, N, STREAM>(a, x + down, t, have, xh);
+      if constexpr (!AGAIN) load_channels<T, K, 1, N, STREAM>(a, gy + down, t, have, g);
       shared_statistics<K, N>(a, lds, stage, w, waves, have, xh, off, rstd);
 #pragma unroll
       for (int u = 0; u < N; ++u) s1[u] = s2[u] = 0.f;
+      const T* from = gy + down;
 #pragma unroll
       for (int c = 0; c < K; ++c) {
         if (c >= have) continue;
-        const float ga = a.gamma ? a.gamma[c0 + c] : 1.f, be = a.beta ? a.beta[c0 + c] : 0.f;
-        const float gk = ga * kArg<ACT>, bk = be * kArg<ACT>;
-        if constexpr (AGAIN) load_channels<T, 1, N, false>(a, gy + down + (long long)c * a.P, t, 1, g);
+        const float ga = affine[c], gk = ga * kArg<ACT>, bk = affine[a.C + c] * kArg<ACT>;
+        if constexpr (AGAIN) {
+          load_channels<T, 1, 1, N, false>(a, from, t, 1, g);
+          from += a.P;
+        }
         float tg = 0.f, tb = 0.f;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
           const float h = (xh[c][u] - off[u]) * rstd[u], gz = g[AGAIN ? 0 : c][u] * slope_f<ACT>(fmaf(h, gk, bk));
-          const bool in = N > 1 || t.left > 0;             // a lane past the end may have a NaN for h
+          const bool in = N > 1 || t.mine;
           tb += in ? gz : 0.f;
           tg = in ? fmaf(gz, h, tg) : tg;
           xh[c][u] = h;
@@ -112,13 +120,16 @@ __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long
       get_sums<N>(lds + 3 * stage, waves, s1);
       get_sums<N>(lds + 4 * stage, waves, s2);
       if (gx == nullptr) return;
+      T* to = gx + down + t.base;
+      from = gy + down;
 #pragma unroll
       for (int c = 0; c < K; ++c) {
         if (c >= have) continue;
         float o[N];
         if constexpr (AGAIN) {
-          const float ga = a.gamma ? a.gamma[c0 + c] : 1.f, be = a.beta ? a.beta[c0 + c] : 0.f;
-          load_channels<T, 1, N, STREAM>(a, gy + down + (long long)c * a.P, t, 1, g);
+          const float ga = affine[c], be = affine[a.C + c];
+          load_channels<T, 1, 1, N, STREAM>(a, from, t, 1, g);
+          from += a.P;
 #pragma unroll
           for (int u = 0; u < N; ++u) o[u] = ga * g[0][u] * slope_f<ACT>(fmaf(xh[c][u], ga * kArg<ACT>, be * kArg<ACT>));
         } else {
@@ -127,7 +138,8 @@ __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long
         }
 #pragma unroll
         for (int u = 0; u < N; ++u) o[u] = rstd[u] * (fmaf(-s1[u], a.inv_c, o[u]) - xh[c][u] * (s2[u] * a.inv_c));
-        store_channel<T, N, STREAM>(gx + down + t.at + (long long)c * a.P, t, o);
+        store_channel<T, N, STREAM>(to, t, o);
+        to += a.P;
       }
     });
   if (a.part == nullptr || lane >= have) return;
@@ -176,7 +188,8 @@ hipError_t launch_layer_first_bwd(const LayerCall& c, int blocks, hipStream_t s)
       with_shared(a.C, [&](auto k) {
         constexpr int K = decltype(k)::value, V = kSharedPoints<K>;
         const int waves = (a.C + K - 1) / K;
-        hipLaunchKernelGGL((shared_bwd_kernel<T, K, V, ACT, S, K == 64>), dim3(blocks), dim3(64 * waves), 5 * waves * 64 * V * sizeof(float), s,
+        hipLaunchKernelGGL((shared_bwd_kernel<T, K, V, ACT, S, K == 64>), dim3(blocks), dim3(64 * waves), 
+                           (5 * waves * 64 * V + 2 * a.C) * sizeof(float), s,
                            a, tiles_host(c.n, V), x, gy, gx);
       });
     }

@@ -7,21 +7,26 @@ namespace {
 
 template <class T, int KC, int V, int ACT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void first_fwd_kernel(LayerArgs a, long long tiles, const T* x, T* y) {
+  constexpr int LEAST = kLeast<KC>;
+  __shared__ float affine[2 * KC];
+  load_affine(a, affine);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long each = tiles_each<V>(a.P);
   for (long long tile = (long long)blockIdx.x * (kThreads / 64) + w; tile < tiles; tile += (long long)gridDim.x * (kThreads / 64))
     with_tile<V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
       float v[KC][N], off[N], rstd[N];
-      load_channels<T, KC, N, STREAM>(a, x, t, a.C, v);
-      statistics<KC, N>(a, v, off, rstd);
+      load_channels<T, KC, LEAST, N, STREAM>(a, x, t, a.C, v);
+      statistics<KC, LEAST, N>(a, v, off, rstd);
+      T* to = y + t.base;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        if (c >= a.C) continue;
-        const float ga = a.gamma ? a.gamma[c] : 1.f, be = a.beta ? a.beta[c] : 0.f;
+        if (c >= LEAST && c >= a.C) continue;
+        const float ga = affine[c], be = affine[a.C + c];
 #pragma unroll
         for (int u = 0; u < N; ++u) v[c][u] = act_f<ACT>(fmaf((v[c][u] - off[u]) * rstd[u], ga, be));
-        store_channel<T, N, STREAM>(y + t.at + (long long)c * a.P, t, v[c]);
+        store_channel<T, N, STREAM>(to, t, v[c]);
+        to += a.P;
       }
     });
 }
@@ -30,21 +35,25 @@ template <class T, int K, int V, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void shared_fwd_kernel(LayerArgs a, long long tiles, const T* x, T* y) {
   extern __shared__ float lds[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, c0 = w * K;
-  const int have = a.C - c0 < K ? a.C - c0 : K;
+  const int have = a.C - c0 < K ? a.C - c0 : K, stage = waves * 64 * V;
+  const float* const affine = lds + 3 * stage + c0;
+  load_affine(a, lds + 3 * stage);
   const long long each = tiles_each<V>(a.P), down = (long long)c0 * a.P;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x)
     with_tile<V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
       float v[K][N], off[N], rstd[N];
-      load_channels<T, K, N, STREAM>(a, x + down, t, have, v);
-      shared_statistics<K, N>(a, lds, waves * 64 * V, w, waves, have, v, off, rstd);
+      load_channels<T, K, 1, N, STREAM>(a, x + down, t, have, v);
+      shared_statistics<K, N>(a, lds, stage, w, waves, have, v, off, rstd);
+      T* to = y + down + t.base;
 #pragma unroll
       for (int c = 0; c < K; ++c) {
         if (c >= have) continue;
-        const float ga = a.gamma ? a.gamma[c0 + c] : 1.f, be = a.beta ? a.beta[c0 + c] : 0.f;
+        const float ga = affine[c], be = affine[a.C + c];
 #pragma unroll
         for (int u = 0; u < N; ++u) v[c][u] = act_f<ACT>(fmaf((v[c][u] - off[u]) * rstd[u], ga, be));
-        store_channel<T, N, STREAM>(y + down + t.at + (long long)c * a.P, t, v[c]);
+        store_channel<T, N, STREAM>(to, t, v[c]);
+        to += a.P;
       }
     });
 }
@@ -72,7 +81,8 @@ hipError_t launch_layer_first_fwd(const LayerCall& c, hipStream_t s) {
         constexpr int K = decltype(k)::value, V = kSharedPoints<K>;
         const int waves = (a.C + K - 1) / K;
         const long long tiles = tiles_host(c.n, V);
-        hipLaunchKernelGGL((shared_fwd_kernel<T, K, V, ACT, S>), dim3(grid_of(tiles)), dim3(64 * waves), 3 * waves * 64 * V * sizeof(float),
+        hipLaunchKernelGGL((shared_fwd_kernel<T, K, V, ACT, S>), dim3(grid_of(tiles)), dim3(64 * waves),
+                           (3 * waves * 64 * V + 2 * a.C) * sizeof(float),
                            s, a, tiles, x, y);
       });
     }

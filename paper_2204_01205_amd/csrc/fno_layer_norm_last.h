@@ -24,27 +24,28 @@ struct Rows {
   long long rows;
   int lg;                    // G = 2^lg lanes a row
 };
-// A tile's values between memory and LDS
-template <class T, bool STREAM>
+// A tile's values between memory and LDS: E pieces a lane (kPasses rows of C <= E G channels for each of 64 / G groups).  Pieces past
+// the end read the last one again, so that no load waits behind a branch.
+template <int E, bool STREAM, class T>
 __device__ __forceinline__ void tile_in(const T* from, T* to, int count) {
   constexpr int V = kVec<T>;
   const int lane = threadIdx.x & 63, whole = count / V;
-  pack<T> q[8];
+  if (whole > 0) {
+    pack<T> q[E];
 #pragma unroll
-  for (int u = 0; u < 8; ++u)
-    if (u * 64 + lane < whole) q[u] = load_pack<STREAM>(from + (u * 64 + lane) * V);
+    for (int u = 0; u < E; ++u) q[u] = load_pack<STREAM>(from + (unsigned)min(u * 64 + lane, whole - 1) * V);
 #pragma unroll
-  for (int u = 0; u < 8; ++u)
-    if (u * 64 + lane < whole) *reinterpret_cast<pack<T>*>(to + (u * 64 + lane) * V) = q[u];
+    for (int u = 0; u < E; ++u) *reinterpret_cast<pack<T>*>(to + min(u * 64 + lane, whole - 1) * V) = q[u];
+  }
   if (whole * V + lane < count) to[whole * V + lane] = from[whole * V + lane];
 }
-template <class T, bool STREAM>
+template <int E, bool STREAM, class T>
 __device__ __forceinline__ void tile_out(const T* from, T* to, int count) {
   constexpr int V = kVec<T>;
   const int lane = threadIdx.x & 63, whole = count / V;
 #pragma unroll
-  for (int u = 0; u < 8; ++u)
-    if (u * 64 + lane < whole) store_pack<STREAM>(to + (u * 64 + lane) * V, *reinterpret_cast<const pack<T>*>(from + (u * 64 + lane) * V));
+  for (int u = 0; u < E; ++u)
+    if (u * 64 + lane < whole) store_pack<STREAM>(to + (unsigned)(u * 64 + lane) * V, *reinterpret_cast<const pack<T>*>(from + (u * 64 + lane) * V));
   if (whole * V + lane < count) to[whole * V + lane] = from[whole * V + lane];
 }
 // E values of a row in LDS, `have` of them this lane's.  ALIGNED: they start at a multiple of their length, or of 16 bytes.

@@ -23,9 +23,10 @@ __global__ __launch_bounds__(kThreads) void tile_bwd_kernel(LayerArgs a, Rows r,
   for (long long tile = (long long)blockIdx.x * (kThreads / 64) + w; tile < tiles; tile += (long long)gridDim.x * (kThreads / 64)) {
     const long long row0 = tile * rows;
     const int count = (int)(r.rows - row0 < rows ? r.rows - row0 : rows);
-    tile_in<T, STREAM>(x + row0 * a.C, mine, count * a.C);
-    tile_in<T, STREAM>(gy + row0 * a.C, cot, count * a.C);
+    tile_in<E, STREAM>(x + row0 * a.C, mine, count * a.C);
+    tile_in<E, STREAM>(gy + row0 * a.C, cot, count * a.C);
     wave_fence();
+#pragma unroll 1
     for (int row = group; row < count; row += 64 >> r.lg) {
       const int at = row * a.C + (have > 0 ? first : 0);
       float v[E], g[E], s1 = 0.f, s2 = 0.f;
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(kThreads) void tile_bwd_kernel(LayerArgs a, Rows r,
       lds_write<E, ALIGNED>(cot + at, have, g);
     }
     wave_fence();
-    if (gx != nullptr) tile_out<T, STREAM>(cot, gx + row0 * a.C, count * a.C);
+    if (gx != nullptr) tile_out<E, STREAM>(cot, gx + row0 * a.C, count * a.C);
     wave_fence();
   }
   if (a.part == nullptr) return;

@@ -22,8 +22,9 @@ __global__ __launch_bounds__(kThreads) void tile_fwd_kernel(LayerArgs a, Rows r,
   for (long long tile = (long long)blockIdx.x * (kThreads / 64) + w; tile < tiles; tile += (long long)gridDim.x * (kThreads / 64)) {
     const long long row0 = tile * rows;
     const int count = (int)(r.rows - row0 < rows ? r.rows - row0 : rows);
-    tile_in<T, STREAM>(x + row0 * a.C, mine, count * a.C);
+    tile_in<E, STREAM>(x + row0 * a.C, mine, count * a.C);
     wave_fence();
+#pragma unroll 1
     for (int row = group; row < count; row += 64 >> r.lg) {      // lanes of a group go through it together
       T* const at = mine + row * a.C + (have > 0 ? first : 0);
       float v[E];
@@ -34,7 +35,7 @@ __global__ __launch_bounds__(kThreads) void tile_fwd_kernel(LayerArgs a, Rows r,
       lds_write<E, ALIGNED>(at, have, v);
     }
     wave_fence();
-    tile_out<T, STREAM>(mine, y + row0 * a.C, count * a.C);
+    tile_out<E, STREAM>(mine, y + row0 * a.C, count * a.C);
     wave_fence();
   }
 }
