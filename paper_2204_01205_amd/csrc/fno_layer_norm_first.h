@@ -10,26 +10,40 @@ namespace {
 // Tiles of 64 V points of one batch entry.  The last of an entry goes in tiles of 64, a point a lane.
 struct Tile {
   long long base;            // its first point in channel 0: the same in all lanes
-  unsigned at;               // from there to this lane's first point; past the entry's end, its last one
+  unsigned at;               // from there to this lane's first point, in bytes; past the entry's end, its last one
   bool mine;                 // not past the end
 };
 template <int V>
 __device__ __forceinline__ long long tiles_each(long long P) { return (P + 64 * V - 1) / (64 * V); }
+// A value that the compiler takes for a new one: it makes a copy of a loop for every uniform condition that does not change in it,
+// sixteen of these for four conditions.
+template <class V>
+__device__ __forceinline__ V opaque(V v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+// a scalar base and 32 bits of a lane's own, which is an address of the instructions
+template <class T>
+__device__ __forceinline__ T* place(T* base, const Tile& t) {
+  typedef typename std::conditional<std::is_const<T>::value, const char, char>::type byte;
+  return reinterpret_cast<T*>(reinterpret_cast<byte*>(base) + t.at);
+}
 // a value that is the same in all lanes, in scalar registers (a division leaves it in a vector register)
 __device__ __forceinline__ long long uniform(long long v) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
   return (long long)((unsigned long long)hi << 32 | lo);
 }
 // body(std::integral_constant<int, V or 1>, tile) for tile number `tile` of all entries
-template <int V, class F>
+template <class T, int V, class F>
 __device__ __forceinline__ void with_tile(const LayerArgs& a, long long tile, long long each, F&& body) {
   const long long b = uniform(a.B == 1 ? 0 : tile / each), p = (tile - b * each) * (64 * V), base = b * a.C * a.P + p;
   const int lane = threadIdx.x & 63;
+  asm volatile("" ::: "memory");       // gamma and beta stay in LDS: kept for all tiles they would take 60 registers of 20 channels
   if (a.P - p >= 64 * V) {
-    body(std::integral_constant<int, V>(), Tile{base, (unsigned)(lane * V), true});
+    body(std::integral_constant<int, V>(), Tile{base, (unsigned)(lane * V * sizeof(T)), true});
   } else {
     const int left = (int)(a.P - p);
-    for (int k = 0; k < left; k += 64) body(std::integral_constant<int, 1>(), Tile{base + k, (unsigned)min(lane, left - 1 - k), k + lane < left});
+    for (int k = 0; k < left; k += 64) body(std::integral_constant<int, 1>(), Tile{base + k, (unsigned)(min(lane, left - 1 - k) * sizeof(T)), k + lane < left});
   }
 }
 // V values of K channels; channels from `have` on read the last one again and count for nothing.  LEAST: have is at least that.
@@ -39,30 +53,30 @@ __device__ __forceinline__ void load_channels(const LayerArgs& a, const T* x, co
   const T* from = x + t.base;
 #pragma unroll
   for (int c = 0; c < K; ++c) {
-    load_values<V, STREAM && (V > 1)>(from + t.at, v[c]);
+    load_values<V, STREAM && (V > 1)>(place(from, t), v[c]);
     if (c + 1 < LEAST || c + 1 < have) from += a.P;
   }
 }
 template <class T, int V, bool STREAM>
 __device__ __forceinline__ void store_channel(T* to, const Tile& t, const float (&v)[V]) {
   if constexpr (V == 1) {
-    if (t.mine) store1(to + t.at, v[0]);
+    if (t.mine) store1(place(to, t), v[0]);
   } else {
-    store_values<V, STREAM>(to + t.at, v);
+    store_values<V, STREAM>(place(to, t), v);
   }
 }
 // x becomes x - about; off and rstd of every point
 template <int K, int LEAST, int V>
-__device__ __forceinline__ void statistics(const LayerArgs& a, float (&x)[K][V], float (&off)[V], float (&rstd)[V]) {
+__device__ __forceinline__ void statistics(const LayerArgs& a, int have, float (&x)[K][V], float (&off)[V], float (&rstd)[V]) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     float s = 0.f, o = 0.f, q = 0.f;
 #pragma unroll
-    for (int c = 0; c < K; ++c) s += c < LEAST || c < a.C ? x[c][v] : 0.f;
+    for (int c = 0; c < K; ++c) s += c < LEAST || c < have ? x[c][v] : 0.f;
     const float about = s * a.inv_c;
 #pragma unroll
     for (int c = 0; c < K; ++c) {
-      const float d = x[c][v] - about, in = c < LEAST || c < a.C ? d : 0.f;
+      const float d = x[c][v] - about, in = c < LEAST || c < have ? d : 0.f;
       o += in;
       q = fmaf(in, in, q);
       x[c][v] = d;

@@ -6,7 +6,7 @@ namespace fno {
 namespace {
 
 template <class T, int KC, int V, int ACT, bool STREAM>
-__global__ __launch_bounds__(kThreads, KC <= 20 ? 3 : 2) void first_bwd_kernel(LayerArgs a, long long tiles, const T* x, const T* gy, T* gx) {
+__global__ __launch_bounds__(kThreads) void first_bwd_kernel(LayerArgs a, long long tiles, const T* x, const T* gy, T* gx) {
   constexpr int LEAST = kLeast<KC>;
   __shared__ float sums[kThreads / 64][2 * KC], affine[2 * KC];
   load_affine(a, affine);
@@ -16,17 +16,18 @@ __global__ __launch_bounds__(kThreads, KC <= 20 ? 3 : 2) void first_bwd_kernel(L
   for (int c = 0; c < KC; ++c) sg[c] = sb[c] = 0.f;
   const long long each = tiles_each<V>(a.P);
   for (long long tile = (long long)blockIdx.x * (kThreads / 64) + w; tile < tiles; tile += (long long)gridDim.x * (kThreads / 64))
-    with_tile<V>(a, tile, each, [&](auto points, Tile t) {
+    with_tile<T, V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
+      const int have = opaque(a.C);
       float xh[KC][N], g[KC][N], off[N], rstd[N], s1[N], s2[N];
-      load_channels<T, KC, LEAST, N, STREAM>(a, x, t, a.C, xh);
-      load_channels<T, KC, LEAST, N, STREAM>(a, gy, t, a.C, g);
-      statistics<KC, LEAST, N>(a, xh, off, rstd);
+      load_channels<T, KC, LEAST, N, STREAM>(a, x, t, have, xh);
+      load_channels<T, KC, LEAST, N, STREAM>(a, gy, t, have, g);
+      statistics<KC, LEAST, N>(a, have, xh, off, rstd);
 #pragma unroll
       for (int u = 0; u < N; ++u) s1[u] = s2[u] = 0.f;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        if (c >= LEAST && c >= a.C) continue;
+        if (c >= LEAST && c >= have) continue;
         const float ga = affine[c], gk = ga * kArg<ACT>, bk = affine[a.C + c] * kArg<ACT>;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -40,11 +41,11 @@ __global__ __launch_bounds__(kThreads, KC <= 20 ? 3 : 2) void first_bwd_kernel(L
           s2[u] = fmaf(g[c][u], h, s2[u]);
         }
       }
-      if (gx == nullptr) return;
+      if (opaque(__builtin_amdgcn_readfirstlane(gx != nullptr)) == 0) return;
       T* to = gx + t.base;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        if (c >= LEAST && c >= a.C) continue;
+        if (c >= LEAST && c >= have) continue;
 #pragma unroll
         for (int u = 0; u < N; ++u) g[c][u] = rstd[u] * (fmaf(-s1[u], a.inv_c, g[c][u]) - xh[c][u] * (s2[u] * a.inv_c));
         store_channel<T, N, STREAM>(to, t, g[c]);
@@ -59,6 +60,7 @@ __global__ __launch_bounds__(kThreads, KC <= 20 ? 3 : 2) void first_bwd_kernel(L
       sums[w][c] = g;
       sums[w][KC + c] = b;
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
   __syncthreads();
   for (int k = threadIdx.x; k < 2 * KC; k += kThreads) {
@@ -73,14 +75,15 @@ template <class T, int K, int V, int ACT, bool STREAM, bool AGAIN>
 __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long tiles, const T* x, const T* gy, T* gx) {
   extern __shared__ float lds[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, c0 = w * K, lane = threadIdx.x & 63;
-  const int have = a.C - c0 < K ? a.C - c0 : K, stage = waves * 64 * V;
+  const int share = a.C - c0 < K ? a.C - c0 : K, stage = waves * 64 * V;
   const float* const affine = lds + 5 * stage + c0;
   load_affine(a, lds + 5 * stage);
   const long long each = tiles_each<V>(a.P), down = (long long)c0 * a.P;
   float sg = 0.f, sb = 0.f;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x)
-    with_tile<V>(a, tile, each, [&](auto points, Tile t) {
+    with_tile<T, V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
+      const int have = opaque(__builtin_amdgcn_readfirstlane(share));
       float xh[K][N], g[AGAIN ? 1 : K][N], off[N], rstd[N], s1[N], s2[N];
       load_channels<T, K, 1, N, STREAM>(a, x + down, t, have, xh);
       if constexpr (!AGAIN) load_channels<T, K, 1, N, STREAM>(a, gy + down, t, have, g);
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long
       __syncthreads();
       get_sums<N>(lds + 3 * stage, waves, s1);
       get_sums<N>(lds + 4 * stage, waves, s2);
-      if (gx == nullptr) return;
+      if (opaque(__builtin_amdgcn_readfirstlane(gx != nullptr)) == 0) return;
       T* to = gx + down + t.base;
       from = gy + down;
 #pragma unroll
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long
         to += a.P;
       }
     });
-  if (a.part == nullptr || lane >= have) return;
+  if (a.part == nullptr || lane >= share) return;
   float* const to = a.part + (long long)blockIdx.x * 2 * a.C + c0 + lane;
   to[0] = sg;
   to[a.C] = sb;

@@ -13,15 +13,16 @@ __global__ __launch_bounds__(kThreads) void first_fwd_kernel(LayerArgs a, long l
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long each = tiles_each<V>(a.P);
   for (long long tile = (long long)blockIdx.x * (kThreads / 64) + w; tile < tiles; tile += (long long)gridDim.x * (kThreads / 64))
-    with_tile<V>(a, tile, each, [&](auto points, Tile t) {
+    with_tile<T, V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
+      const int have = opaque(a.C);
       float v[KC][N], off[N], rstd[N];
-      load_channels<T, KC, LEAST, N, STREAM>(a, x, t, a.C, v);
-      statistics<KC, LEAST, N>(a, v, off, rstd);
+      load_channels<T, KC, LEAST, N, STREAM>(a, x, t, have, v);
+      statistics<KC, LEAST, N>(a, have, v, off, rstd);
       T* to = y + t.base;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        if (c >= LEAST && c >= a.C) continue;
+        if (c >= LEAST && c >= have) continue;
         const float ga = affine[c], be = affine[a.C + c];
 #pragma unroll
         for (int u = 0; u < N; ++u) v[c][u] = act_f<ACT>(fmaf((v[c][u] - off[u]) * rstd[u], ga, be));
@@ -35,13 +36,14 @@ template <class T, int K, int V, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void shared_fwd_kernel(LayerArgs a, long long tiles, const T* x, T* y) {
   extern __shared__ float lds[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, c0 = w * K;
-  const int have = a.C - c0 < K ? a.C - c0 : K, stage = waves * 64 * V;
+  const int share = a.C - c0 < K ? a.C - c0 : K, stage = waves * 64 * V;
   const float* const affine = lds + 3 * stage + c0;
   load_affine(a, lds + 3 * stage);
   const long long each = tiles_each<V>(a.P), down = (long long)c0 * a.P;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x)
-    with_tile<V>(a, tile, each, [&](auto points, Tile t) {
+    with_tile<T, V>(a, tile, each, [&](auto points, Tile t) {
       constexpr int N = decltype(points)::value;
+      const int have = opaque(__builtin_amdgcn_readfirstlane(share));
       float v[K][N], off[N], rstd[N];
       load_channels<T, K, 1, N, STREAM>(a, x + down, t, have, v);
       shared_statistics<K, N>(a, lds, stage, w, waves, have, v, off, rstd);

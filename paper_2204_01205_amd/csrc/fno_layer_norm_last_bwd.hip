@@ -127,14 +127,42 @@ __global__ __launch_bounds__(kRowThreads<W>) void wide_bwd_kernel(LayerArgs a, l
     }
   }
   if (a.part == nullptr) return;
-  // W == 1: the four waves' rows are shares of their own
-  float* const to = a.part + ((long long)blockIdx.x * PER + w) * 2 * a.C + first;
+  float* const to = a.part + (long long)blockIdx.x * 2 * a.C + first;
+  if constexpr (W == 1) {              // the four waves' sums one after the other: [ggamma, gbeta][C]
+    extern __shared__ float sums[];
+    for (int turn = 0; turn < 4; ++turn) {
+      if (turn > 0) __syncthreads();
+      if (turn != w) continue;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        float og[V], ob[V];
+#pragma unroll
+        for (int u = 0; u < V; ++u) og[u] = ob[u] = 0.f;
+        if (turn > 0) {
+          load_some<V, false>(sums + first + k * STEP, left - k * STEP, og);
+          load_some<V, false>(sums + a.C + first + k * STEP, left - k * STEP, ob);
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+          sg[k][u] += og[u];
+          sb[k][u] += ob[u];
+        }
+        if (turn < 3) {
+          store_some<V, false>(sums + first + k * STEP, left - k * STEP, sg[k]);
+          store_some<V, false>(sums + a.C + first + k * STEP, left - k * STEP, sb[k]);
+        }
+      }
+    }
+    if (w != 3) return;
+  }
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     store_some<V, false>(to + k * STEP, left - k * STEP, sg[k]);
     store_some<V, false>(to + a.C + k * STEP, left - k * STEP, sb[k]);
   }
 }
+
+// ------------------------------------------------------------------------------------------ launches
 
 // A lane's chain of additions is 256 rows or tiles long at most where more than `most` blocks would not fill the chip better.
 int blocks_for(long long items, int each, int most) {
@@ -145,17 +173,16 @@ int blocks_for(long long items, int each, int most) {
 
 }  // namespace
 
-// Shares of the sums: blocks, of which those with a row a wave have four.
 int layer_last_blocks(const LayerShape& n) {
   if (n.C <= kTileChannels) return blocks_for(row_tiles(n), 4, 1024);
-  int shares = 0;
+  int blocks = 0;
   auto count = [&](auto w, auto) {
     constexpr int W = decltype(w)::value;
-    shares = W == 1 ? 4 * blocks_for(n.B * n.P, 4, 256) : blocks_for(n.B * n.P, 1, W == 4 ? 1024 : 512);
+    blocks = W == 1 ? blocks_for(n.B * n.P, 4, 1024) : blocks_for(n.B * n.P, 1, W == 4 ? 1024 : 512);
   };
   if (n.bf16) with_row<2>(n.C, count);
   else with_row<4>(n.C, count);
-  return shares;
+  return blocks;
 }
 
 hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) {
@@ -178,8 +205,8 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
     } else {
       with_row<sizeof(T)>(a.C, [&](auto w, auto n) {
         constexpr int W = decltype(w)::value;
-        hipLaunchKernelGGL((wide_bwd_kernel<T, W, decltype(n)::value, ACT, S>), dim3(W == 1 ? blocks / 4 : blocks), dim3(kRowThreads<W>), 0, s,
-                           a, rows, x, gy, gx);
+        hipLaunchKernelGGL((wide_bwd_kernel<T, W, decltype(n)::value, ACT, S>), dim3(blocks), dim3(kRowThreads<W>),
+                           W == 1 ? 2 * a.C * sizeof(float) : 0, s, a, rows, x, gy, gx);
       });
     }
   });
