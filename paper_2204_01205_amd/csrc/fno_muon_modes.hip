@@ -5,9 +5,9 @@
 // only (20 is five; tiles of 16 or 32 would be two or three times the work), and neighbouring modes lie side by side in memory.  A
 // lane is (mode, column of a tile), a register a row.  Wave J of a block owns the columns of tile J of X, in registers.  An
 // iteration, with A and B Hermitian, so that a row of either is the conjugate of a column:
-//   A = X X^H and B = b A + c A A: wave J takes the tiles (J, J .. J + m/8), around the corner, of which the other half are
+//   A = X X^H and B = a + b A + c A A: wave J takes the tiles (J, J .. J + m/8), around the corner, of which the other half are
 //   the mirrors, operands from LDS (X by rows, A by columns);
-//   X = a X + B X: its own columns, B from LDS.
+//   X = B X: its own columns, B from LDS.
 // X, A and B take turns in one LDS buffer, [row][tile][mode][column] with one entry of padding a row: a tile read by columns
 // is contiguous, one read by rows has its four rows in neighbouring banks.
 #include "fno_muon.h"
@@ -36,6 +36,12 @@ struct ModesList {
 
 __device__ __forceinline__ v4f mfma4(float a, float b, v4f c) { return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, 0, 0, 0); }
 
+// A place that the compiler takes for a new one: it would keep the addresses of all rows between the loads and the stores.
+__device__ __forceinline__ long long opaque_place(long long at) {
+  asm volatile("" : "+v"(at));
+  return at;
+}
+
 template <int TM>
 __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalars c) {
   constexpr int M = 4 * TM, ND = TM / 2 + 1, RA = 64 * TM + 1;
@@ -54,40 +60,78 @@ __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalar
   const bool here = mode < t.modes && col < t.n;
   const long long at = (col < t.n ? col : t.n - 1) * t.sj + (mode < t.modes ? mode : t.modes - 1);
 
-  // what lies past the matrix or the last mode is a zero that stays one and is not stored
+  // What lies past the matrix or the last mode is a zero that stays one and is not stored; of rows, the last three may.
   float xr[M], xi[M];
   {
-    float2 g[M], o[M];
+    constexpr int PART = TM > 4 ? M / 2 : M;               // rows that are on their way at a time: registers
+    const float2 *gp = t.g + at, *mp = t.mom + at;
+    float2* to = t.mom + at;
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      const long long e = at + (i < t.m ? i : t.m - 1) * t.si;
-      g[i] = t.g[e];
-      o[i] = t.mom[e];
-    }
+    for (int part = 0; part < M; part += PART) {
+      float2 g[PART], o[PART];
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      const float ur = muon_momentum(c, g[i].x * scale, o[i].x), ui = muon_momentum(c, g[i].y * scale, o[i].y);
-      if (here && i < t.m) t.mom[at + i * t.si] = o[i];
-      xr[i] = here && i < t.m ? ur : 0.f;
-      xi[i] = here && i < t.m ? ui : 0.f;
+      for (int i = 0; i < PART; ++i) {
+        g[i] = *gp;
+        o[i] = *mp;
+        if (part + i < M - 4 || part + i + 1 < t.m) {
+          gp += t.si;
+          mp += t.si;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < PART; ++i) {
+        const float ur = muon_momentum(c, g[i].x * scale, o[i].x), ui = muon_momentum(c, g[i].y * scale, o[i].y);
+        const bool in = here && (part + i < M - 3 || part + i < t.m);
+        xr[part + i] = in ? ur : 0.f;
+        xi[part + i] = in ? ui : 0.f;
+      }
+      if (here) {
+        to = t.mom + opaque_place(to - t.mom);
+#pragma unroll
+        for (int i = 0; i < PART; ++i) {
+          if (part + i < M - 3 || part + i < t.m) *to = o[i];
+          to += t.si;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   {
-    double sum = 0.0;
+    // |u|^2 in float where that holds its squares, else in double
+    auto total = [&](auto zero) {
+      typedef decltype(zero) real;
+      real sum = zero;
 #pragma unroll
-    for (int i = 0; i < M; ++i) sum = fma((double)xr[i], (double)xr[i], fma((double)xi[i], (double)xi[i], sum));
-    sum += __shfl_xor(sum, 1);
-    sum += __shfl_xor(sum, 2);
-    double* const red = reinterpret_cast<double*>(lds);
-    if (j == 0) red[w * kModes + b] = sum;
-    __syncthreads();
-    sum = 0.0;
-    for (int v = 0; v < TN; ++v) sum += red[v * kModes + b];
-    const double inv = muon_inverse(sum, c.eps);
+      for (int i = 0; i < M; ++i) {
+        sum += (real)xr[i] * (real)xr[i];
+        sum += (real)xi[i] * (real)xi[i];
+      }
+      sum += __shfl_xor(sum, 1);
+      sum += __shfl_xor(sum, 2);
+      real* const red = reinterpret_cast<real*>(lds);
+      __syncthreads();
+      if (j == 0) red[w * kModes + b] = sum;
+      __syncthreads();
+      sum = zero;
+      for (int v = 0; v < TN; ++v) sum += red[v * kModes + b];
+      return sum;
+    };
+    auto times = [&](auto by) {
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      xr[i] = (float)(xr[i] * inv);
-      xi[i] = (float)(xi[i] * inv);
+      for (int i = 0; i < M; ++i) {
+        xr[i] = (float)(xr[i] * by);
+        xi[i] = (float)(xi[i] * by);
+      }
+    };
+    const float squares = total(0.f);
+    // (a matrix takes its own way, whatever its neighbours are)
+    const bool plain = squares > 1e-28f && squares < 1e30f;
+    const float inv = 1.0f / (sqrtf(squares) + (float)c.eps);
+    if (__all(plain)) {
+      times(inv);
+    } else {
+      const double fine = muon_inverse(total(0.0), c.eps);
+      times(plain ? (double)inv : fine);
     }
   }
 
@@ -143,13 +187,12 @@ __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalar
     __syncthreads();
     if (w < TM) put();
     __syncthreads();
-    // B = b A + c A A, with (A A)(w, J) = sum over k of conj A(k, w) A(k, J)
+    // B = a + b A + c A A, with (A A)(w, J) = sum over k of conj A(k, w) A(k, J)
     if (w < TM) {
-      v4f sr[ND], si[ND];
       const float2* colp[ND];
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
-        sr[d] = si[d] = v4f{0.f, 0.f, 0.f, 0.f};
+        ar[d] = ai[d] = v4f{0.f, 0.f, 0.f, 0.f};
         colp[d] = lds + tile[d] * 64 + lane;
       }
       for (int kt = 0; kt < TM; ++kt) {
@@ -161,13 +204,13 @@ __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalar
           const float ni = -v[0].y;
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            sr[d] = mfma4(v[0].x, v[d].x, sr[d]);
-            si[d] = mfma4(v[0].x, v[d].y, si[d]);
+            ar[d] = mfma4(v[0].x, v[d].x, ar[d]);
+            ai[d] = mfma4(v[0].x, v[d].y, ai[d]);
           }
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            sr[d] = mfma4(v[0].y, v[d].y, sr[d]);
-            si[d] = mfma4(ni, v[d].x, si[d]);
+            ar[d] = mfma4(v[0].y, v[d].y, ar[d]);
+            ai[d] = mfma4(ni, v[d].x, ai[d]);
           }
         }
       }
@@ -175,22 +218,19 @@ __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalar
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          ar[d][r] = fmaf(c.b, ar[d][r], c.c * sr[d][r]);
-          ai[d][r] = fmaf(c.b, ai[d][r], c.c * si[d][r]);
+          const float2 own = colp[d][(4 * w + r) * RA];
+          ar[d][r] = fmaf(c.b, own.x, c.c * ar[d][r]);
+          if (d == 0) ar[d][r] += r == j ? c.a : 0.f;
+          ai[d][r] = fmaf(c.b, own.y, c.c * ai[d][r]);
         }
     }
     __syncthreads();
     if (w < TM) put();
     __syncthreads();
-    // X(I, w) = a X(I, w) + sum over k of conj B(k, I) X(k, w)
+    // X(I, w) = sum over k of conj B(k, I) X(k, w)
     v4f yr[TM], yi[TM];
 #pragma unroll
-    for (int I = 0; I < TM; ++I)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        yr[I][r] = c.a * xr[4 * I + r];
-        yi[I][r] = c.a * xi[4 * I + r];
-      }
+    for (int I = 0; I < TM; ++I) yr[I] = yi[I] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int q = 0; q < M; ++q) {
       float2 v[TM];
@@ -217,12 +257,20 @@ __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalar
       }
   }
 
+  if (!here) return;
   float2 p[M];
+  const float2* from = t.p + at;
 #pragma unroll
-  for (int i = 0; i < M; ++i) p[i] = t.p[at + (i < t.m ? i : t.m - 1) * t.si];
+  for (int i = 0; i < M; ++i) {
+    p[i] = *from;
+    if (i < M - 4 || i + 1 < t.m) from += t.si;
+  }
+  float2* to = t.p + opaque_place(at);
 #pragma unroll
-  for (int i = 0; i < M; ++i)
-    if (here && i < t.m) t.p[at + i * t.si] = make_float2(fmaf(p[i].x, t.keep, -t.move * xr[i]), fmaf(p[i].y, t.keep, -t.move * xi[i]));
+  for (int i = 0; i < M; ++i) {
+    if (i < M - 3 || i < t.m) *to = make_float2(fmaf(p[i].x, t.keep, -t.move * xr[i]), fmaf(p[i].y, t.keep, -t.move * xi[i]));
+    to += t.si;
+  }
 }
 
 template <int TM>
@@ -266,7 +314,7 @@ hipError_t launch_muon_modes(const MuonTensor* t, int count, const MuonScalars& 
       };
       for (int k = 0; k < count; ++k) {
         const int rows = t[k].rows, cols = t[k].cols, m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-        if (!t[k].modes || (m + 3) / 4 != tm || (n + 3) / 4 != tn) continue;
+        if (!t[k].modes || muon_is_modes5(t[k]) || (m + 3) / 4 != tm || (n + 3) / 4 != tn) continue;
         const long long row = (long long)cols * t[k].batch, column = t[k].batch, blocks = (t[k].batch + kModes - 1) / kModes;
         for (long long done = 0; done < blocks;) {
           if (l.count == kPerLaunch || l.blocks == kMost) {
