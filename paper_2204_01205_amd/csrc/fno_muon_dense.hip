@@ -18,7 +18,6 @@ namespace fno {
 
 namespace {
 
-typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef _Float16 half;
@@ -194,89 +193,127 @@ __device__ __forceinline__ TileOf tile_of(const DenseEntry& t, unsigned local, u
   return o;
 }
 
-__device__ __forceinline__ h4 parts_of(v4f v, h4& second) {
-  h4 first;
+// Sixteen consecutive values of a row as pairs: half of a piece of 32
+__device__ __forceinline__ void put_pairs(half* at, const float (&v)[16]) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    first[u] = (half)v[u];
-    second[u] = (half)(v[u] - (float)first[u]);
+  for (int k = 0; k < 16; k += 8) {
+    h8 first, second;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      first[u] = (half)v[k + u];
+      second[u] = (half)(v[k + u] - (float)first[u]);
+    }
+    *reinterpret_cast<h8*>(at + k) = first;
+    *reinterpret_cast<h8*>(at + k + 32) = second;
   }
-  return first;
 }
-__device__ __forceinline__ v4f value_of(const half* p) {
-  const h4 a = *reinterpret_cast<const h4*>(p), b = *reinterpret_cast<const h4*>(p + 32);
-  v4f v;
+__device__ __forceinline__ void get_pairs(const half* at, float (&v)[16]) {
 #pragma unroll
-  for (int u = 0; u < 4; ++u) v[u] = (float)a[u] + (float)b[u];
-  return v;
-}
-// Four consecutive rows of a column: one piece of the array by columns, four places of the array by rows.
-__device__ __forceinline__ void put_columns(half* p, int ld, int row, int col, v4f v) {
-  h4 second;
-  const h4 first = parts_of(v, second);
-  half* const at = p + pair_at(col, ld, row);
-  *reinterpret_cast<h4*>(at) = first;
-  *reinterpret_cast<h4*>(at + 32) = second;
-}
-__device__ __forceinline__ void put_rows(half* p, int ld, int row, int col, v4f v) {
-  h4 second;
-  const h4 first = parts_of(v, second);
-  half* const at = p + pair_at(row, ld, col);
+  for (int k = 0; k < 16; k += 8) {
+    const h8 first = *reinterpret_cast<const h8*>(at + k), second = *reinterpret_cast<const h8*>(at + k + 32);
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    at[(long long)u * 2 * ld] = first[u];
-    at[(long long)u * 2 * ld + 32] = second[u];
+    for (int u = 0; u < 8; ++u) v[k + u] = (float)first[u] + (float)second[u];
   }
+}
+// A matrix's step for 16 consecutive values, `count` of which are there
+__device__ __forceinline__ void step_values(const DenseEntry& t, float* p, int count, const float (&x)[16]) {
+  typedef v4f loose __attribute__((aligned(4)));
+  const float move = t.move * (1.f / kX);
+  if (count >= 16) {
+    v4f q[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q[k] = *reinterpret_cast<const loose*>(p + 4 * k);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) q[k][u] = fmaf(q[k][u], t.keep, -move * x[4 * k + u]);
+      *reinterpret_cast<loose*>(p + 4 * k) = q[k];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (k < count) p[k] = fmaf(p[k], t.keep, -move * x[k]);
+  }
+}
+__device__ __forceinline__ void wave_fence() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// What becomes of a 32 x 32 piece of a sum: lane's column, four rows at a time.
+// What becomes of a 32 x 32 piece of a sum.  Its values go through a wave's own LDS, so that memory is read and written in
+// 16-byte pieces along rows, and along columns for the array by columns (for A and B the mirror).
+constexpr int kTurn = 32 * 33;         // floats of it
 template <int PHASE>
 __device__ __forceinline__ void finish(const DenseEntry& t, const Region& r, const TileOf& o, const MuonScalars& c, int it, int row0,
-                                       int col0, const v16f& acc) {
-  const int lane = threadIdx.x & 63, col = col0 + (lane & 31);
+                                       int col0, const v16f& acc, float* turn) {
+  const int lane = threadIdx.x & 63, line = lane >> 1, part = (lane & 1) * 16;
+  wave_fence();
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int row = row0 + 8 * q + 4 * (lane >> 5);
-    v4f v = {acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
-    if constexpr (PHASE == 0) {
-      v *= kA / (kX * kX);
-      put_rows(r.a, t.mp, row, col, v);
-      if (o.mirror) put_columns(r.a, t.mp, row, col, v);
-    } else if constexpr (PHASE == 1) {
-      const v4f a = value_of(r.a + pair_at(col, t.mp, row));
+  for (int q = 0; q < 16; ++q) turn[(8 * (q / 4) + 4 * (lane >> 5) + q % 4) * 33 + (lane & 31)] = acc[q];
+  wave_fence();
+  float v[16];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = fmaf(c.b * (kB / kA), a[u], c.c * (kB / (kA * kA)) * v[u]);
-      put_rows(r.b, t.mp, row, col, v);
-      if (o.mirror) put_columns(r.b, t.mp, row, col, v);
-    } else {
-      const v4f x = value_of(r.xt + (it & 1) * r.next + pair_at(col, t.mp, row));
+  for (int k = 0; k < 16; ++k) v[k] = turn[line * 33 + part + k];
+  const bool over = PHASE == 2 && it + 1 >= c.iterations, tall = t.rows > t.cols;
+  if constexpr (PHASE == 0) {
+    half* const at = r.a + pair_at(row0 + line, t.mp, col0 + part);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = fmaf(c.a, x[u], v[u] * (1.f / kB));
-      if (it + 1 < c.iterations) {
-        put_rows(r.x, t.np, row, col, v);
-        put_columns(r.xt + ((it + 1) & 1) * r.next, t.mp, row, col, v);
-      } else if (col < t.n) {
-        const bool tall = t.rows > t.cols;
-        const long long base = (long long)o.matrix * t.rows * t.cols;
+    for (int k = 0; k < 16; ++k) v[k] *= kA / (kX * kX);
+    put_pairs(at, v);
+  } else if constexpr (PHASE == 1) {
+    float a[16];
+    get_pairs(r.a + pair_at(row0 + line, t.mp, col0 + part), a);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (row + u >= t.m) continue;
-          float* const p = t.p + base + (tall ? (long long)col * t.cols + row + u : (long long)(row + u) * t.cols + col);
-          *p = fmaf(*p, t.keep, -t.move * (v[u] * (1.f / kX)));
-        }
-      }
+    for (int k = 0; k < 16; ++k) v[k] = fmaf(c.b * (kB / kA), a[k], c.c * (kB / (kA * kA)) * v[k]);
+    put_pairs(r.b + pair_at(row0 + line, t.mp, col0 + part), v);
+  } else {
+    half* const at = r.x + pair_at(row0 + line, t.np, col0 + part);
+    float x[16];
+    get_pairs(at, x);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = fmaf(c.a, x[k], v[k] * (1.f / kB));
+    if (!over) {
+      put_pairs(at, v);
+    } else if (!tall) {
+      if (row0 + line < t.m)
+        step_values(t, t.p + ((long long)o.matrix * t.rows + row0 + line) * t.cols + col0 + part, t.n - col0 - part, v);
+      return;
     }
+  }
+  if (PHASE < 2 && !o.mirror) return;
+  wave_fence();
+#pragma unroll
+  for (int k = 0; k < 16; ++k) turn[line * 33 + part + k] = v[k];
+  wave_fence();
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = turn[(part + k) * 33 + line];
+  if constexpr (PHASE == 2) {
+    if (!over) put_pairs(r.xt + ((it + 1) & 1) * r.next + pair_at(col0 + line, t.mp, row0 + part), v);
+    else if (col0 + line < t.n)
+      step_values(t, t.p + ((long long)o.matrix * t.rows + col0 + line) * t.cols + row0 + part, t.m - row0 - part, v);
+  } else {
+    put_pairs((PHASE == 0 ? r.a : r.b) + pair_at(col0 + line, t.mp, row0 + part), v);
   }
 }
 
 template <int T>
 __device__ __forceinline__ long long partial_at(unsigned local) { return (long long)local * T * T; }
 
+
+// Waits until a wave has read all it asked for from LDS and at most COUNT of its loads are on their way.  (The fence of a barrier
+// waits for all loads.)
+template <int COUNT>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(COUNT) : "memory");
+}
+template <int T> constexpr int kStages = T == 64 ? 4 : 2;
+
 // A T x T tile, or a share of its sum.  PHASE 0: A = X X^T; 1: B = b A + c A A; 2: X = a X + B X.
 template <int T, int PHASE>
 __global__ __launch_bounds__(kThreads) void dense_product_kernel(DenseList l, MuonScalars c, int it) {
   constexpr int W = T / 2, N = W / 32, LINE = 128, SIDE = T * LINE;       // a wave's share of the tile; bytes of an operand in LDS
-  __shared__ __align__(16) char lds[2][2 * SIDE];
+  constexpr int STAGES = kStages<T>, LOADS = T / 16;                      // steps in LDS or on their way; a wave's loads of one
+  __shared__ __align__(16) char lds[STAGES][2 * SIDE];
   float scale;
   if (!muon_scale(c, scale)) return;
   const DenseEntry& t = entry_of(l, [](const DenseEntry& e) { return e.first[PHASE]; });
@@ -321,12 +358,18 @@ __global__ __launch_bounds__(kThreads) void dense_product_kernel(DenseList l, Mu
     for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-  if (s0 < s1) load(0);
+  for (int k = 0; k < STAGES - 1; ++k)
+    if (s0 + k < s1) load(k);
   for (int s = s0; s < s1; ++s) {
-    const int buffer = (s - s0) & 1;
-    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): this step's pieces are there
-    __syncthreads();                             // for all waves, which are done with the other buffer
-    if (s + 1 < s1) load(buffer ^ 1);
+    const int buffer = (s - s0) % STAGES, ahead = s1 - 1 - s;              // steps after this one: STAGES - 2 of them are on their way
+    if (STAGES > 3 && ahead >= 2) wait_loads<2 * LOADS>();
+    else if (STAGES > 2 && ahead >= 1) wait_loads<LOADS>();
+    else wait_loads<0>();
+    // this wave's pieces of the step are there; with the barrier all waves' are, and all waves are done with the step before,
+    // whose buffer is the next to be filled
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (s + STAGES - 1 < s1) load((s - s0 + STAGES - 1) % STAGES);
     const char *const a = lds[buffer] + wr * LINE, *const b = lds[buffer] + SIDE + wc * LINE;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -359,40 +402,46 @@ __global__ __launch_bounds__(kThreads) void dense_product_kernel(DenseList l, Mu
               v4f{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     return;
   }
+  __syncthreads();
+  float* const turn = reinterpret_cast<float*>(lds[0]) + w * kTurn;
+  static_assert(4 * kTurn * sizeof(float) <= sizeof(lds), "the operands' LDS is used again");
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int j = 0; j < N; ++j) finish<PHASE>(t, r, o, c, it, o.row + wr + i * 32, o.col + wc + j * 32, acc[i][j]);
+    for (int j = 0; j < N; ++j) finish<PHASE>(t, r, o, c, it, o.row + wr + i * 32, o.col + wc + j * 32, acc[i][j], turn);
 }
 
-// Adds the shares of the tiles whose sums are split, in their order.
+// Adds the shares of the tiles whose sums are split, in their order; a block takes one 32 x 32 piece of every wave's.
 template <int T, int PHASE>
 __global__ __launch_bounds__(kThreads) void dense_sum_kernel(DenseList l, MuonScalars c, int it) {
   constexpr int W = T / 2, N = W / 32;
+  __shared__ float turns[4][kTurn];
   float scale;
   if (!muon_scale(c, scale)) return;
-  const DenseEntry& t = entry_of(l, [](const DenseEntry& e) { return e.first_sum[PHASE]; });
-  const unsigned local = blockIdx.x - t.first_sum[PHASE], tiles = tiles_of<T, PHASE>(t), splits = t.splits[PHASE];
+  const unsigned block = blockIdx.x / (N * N), i = blockIdx.x / N % N, j = blockIdx.x % N;
+  int k = 0;
+  while (k + 1 < l.count && l.t[k + 1].first_sum[PHASE] <= block) ++k;
+  const DenseEntry& t = l.t[k];
+  const unsigned local = block - t.first_sum[PHASE], tiles = tiles_of<T, PHASE>(t), splits = t.splits[PHASE];
   const TileOf o = tile_of<T, PHASE>(t, local, 1);
   const Region r = region_of(t, o.matrix);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = (w >> 1) * W, wc = (w & 1) * W;
-  const float* const from = l.part + t.part_at[PHASE] + partial_at<T>(o.matrix * splits * tiles + o.tile) + w * (T * T / 4) + lane * 4;
+  const float* const from = l.part + t.part_at[PHASE] + partial_at<T>(o.matrix * splits * tiles + o.tile) + w * (T * T / 4) + lane * 4 +
+                            (i * N + j) * 1024;
+  v4f v[4];
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+  for (int q = 0; q < 4; ++q) v[q] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (unsigned n = 0; n < splits; ++n) {
+    const float* const at = from + partial_at<T>(n * tiles);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      v16f acc;
+    for (int q = 0; q < 4; ++q) v[q] += *reinterpret_cast<const v4f*>(at + q * 256);
+  }
+  v16f acc;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v4f v = {0.f, 0.f, 0.f, 0.f};
-        for (unsigned k = 0; k < splits; ++k)
-          v += *reinterpret_cast<const v4f*>(from + partial_at<T>(k * tiles) + ((i * N + j) * 4 + q) * 256);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[4 * q + u] = v[u];
-      }
-      finish<PHASE>(t, r, o, c, it, o.row + wr + i * 32, o.col + wc + j * 32, acc);
-    }
+  for (int q = 0; q < 16; ++q) acc[q] = v[q / 4][q % 4];
+  finish<PHASE>(t, r, o, c, it, o.row + wr + (int)i * 32, o.col + wc + (int)j * 32, acc, turns[w]);
 }
 
 // ------------------------------------------------------------------------------------------ launches
@@ -515,7 +564,7 @@ hipError_t launch_product(const Group& g, const MuonScalars& c, int it, hipStrea
   hipLaunchKernelGGL((dense_product_kernel<T, PHASE>), dim3(g.blocks[PHASE]), dim3(kThreads), 0, s, g.l, c, it);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.sums[PHASE] == 0) return e;
-  hipLaunchKernelGGL((dense_sum_kernel<T, PHASE>), dim3(g.sums[PHASE]), dim3(kThreads), 0, s, g.l, c, it);
+  hipLaunchKernelGGL((dense_sum_kernel<T, PHASE>), dim3(g.sums[PHASE] * (T / 64) * (T / 64)), dim3(kThreads), 0, s, g.l, c, it);
   return hipGetLastError();
 }
 template <int T>
