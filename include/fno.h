@@ -236,7 +236,7 @@ int fno_adam_step(int64_t n, float* param, const float* grad, float* m, float* v
  * the adjoint gy, and gy (x - mean) where it counts in the sums, from 1e-30 to 1e36.  (The adjoint starts from the saved mean, a
  * float: its xh is off by up to 2^-24 |mean| rstd, the forward call's is not.)
  * activation: FNO_ACT_IDENTITY, FNO_ACT_GELU or FNO_ACT_SILU (z / (1 + exp(-z))). */
-enum { FNO_ACT_SILU = 2 };       /* fno_group_norm_fwd and fno_group_norm_bwd only */
+enum { FNO_ACT_SILU = 2 };       /* the group norm's and the layer norm's calls only */
 enum { FNO_LAYOUT_CHANNELS_FIRST = 0, FNO_LAYOUT_CHANNELS_LAST = 1 };
 enum { FNO_DTYPE_F32 = 0, FNO_DTYPE_BF16 = 1 };
 typedef struct {

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libfno.so")
 
 FNO_OK, FNO_EINVAL, FNO_EUNSUPPORTED, FNO_ENOSPC, FNO_EHIP = 0, -1, -2, -3, -4
 FNO_ACT_IDENTITY, FNO_ACT_GELU = 0, 1
-FNO_ACT_SILU = 2                 # group norm only
+FNO_ACT_SILU = 2                 # group norm and layer norm only
 FNO_LAYOUT_CHANNELS_FIRST, FNO_LAYOUT_CHANNELS_LAST = 0, 1
 FNO_DTYPE_F32, FNO_DTYPE_BF16 = 0, 1
 FNO_MUON_MATRICES, FNO_MUON_MODES = 0, 1
@@ -423,46 +423,49 @@ def alloc_layer_norm_workspace(desc: FnoLayerNormDesc, device="cuda") -> torch.T
     return torch.empty(max(fno_layer_norm_workspace_bytes(desc), 256), dtype=torch.uint8, device=device)
 
 
-def _layer_norm_stream(desc, device) -> tuple:
-    """Type and number of a field's values, and the current stream of the GPU that the field lives on, which has to be the
-    current one."""
-    current = torch.cuda.current_device()
-    if device.index != current:
-        raise ValueError(f"the tensors live on {device}, the current device is cuda:{current}")
-    dtype = torch.bfloat16 if desc.dtype == FNO_DTYPE_BF16 else torch.float32
-    return dtype, desc.batch * desc.channels * desc.npoints, _raw_stream(current)
-
-
-def _one_device(device, **tensors) -> None:
-    for name, t in tensors.items():
+def _one_device(device, *tensors) -> None:
+    for t in tensors:
         if t is not None and t.device != device:
-            raise ValueError(f"{name} lives on {t.device}, not on {device}")
+            raise ValueError(f"tensors live on {device} and on {t.device}")
+
+
+def _here(x: torch.Tensor) -> int:
+    """The current stream, for a call whose tensors live on the current GPU: the call goes to that stream alone."""
+    if not x.is_cuda:
+        raise ValueError("the tensors must live on the GPU")
+    current = torch.cuda.current_device()
+    if x.device.index != current:
+        raise ValueError(f"the tensors live on {x.device}, the current device is cuda:{current}")
+    return _raw_stream(current)
+
+
+def _layer_norm_sizes(desc) -> tuple:
+    """Type and number of a field's values; number of channels."""
+    dtype = torch.bfloat16 if desc.dtype == FNO_DTYPE_BF16 else torch.float32
+    channels = desc.channels
+    return dtype, desc.batch * channels * desc.npoints, channels
 
 
 def fno_layer_norm_fwd(desc, x, gamma, beta, y) -> None:
-    _one_device(x.device, gamma=gamma, beta=beta, y=y)
-    if not x.is_cuda:
-        raise ValueError("x must live on the GPU")
-    dtype, field, stream = _layer_norm_stream(desc, x.device)
-    channels, f32 = desc.channels, torch.float32
+    dtype, field, channels = _layer_norm_sizes(desc)
+    f32 = torch.float32
+    _one_device(x.device, gamma, beta, y)
     status = lib().fno_layer_norm_fwd(
         ctypes.byref(desc), _address(x, dtype, field, "x"), _address(gamma, f32, channels, "gamma"),
-        _address(beta, f32, channels, "beta"), _address(y, dtype, field, "y"), stream)
+        _address(beta, f32, channels, "beta"), _address(y, dtype, field, "y"), _here(x))
     if status:
         _check(status)
 
 
 def fno_layer_norm_bwd(desc, x, gamma, beta, gy, gx, ggamma, gbeta, ws) -> None:
-    _one_device(x.device, gamma=gamma, beta=beta, gy=gy, gx=gx, ggamma=ggamma, gbeta=gbeta, ws=ws)
-    if not x.is_cuda:
-        raise ValueError("x must live on the GPU")
-    dtype, field, stream = _layer_norm_stream(desc, x.device)
-    channels, f32 = desc.channels, torch.float32
+    dtype, field, channels = _layer_norm_sizes(desc)
+    f32 = torch.float32
+    _one_device(x.device, gamma, beta, gy, gx, ggamma, gbeta, ws)
     status = lib().fno_layer_norm_bwd(
         ctypes.byref(desc), _address(x, dtype, field, "x"), _address(gamma, f32, channels, "gamma"),
         _address(beta, f32, channels, "beta"), _address(gy, dtype, field, "gy"), _address(gx, dtype, field, "gx"),
         _address(ggamma, f32, channels, "ggamma"), _address(gbeta, f32, channels, "gbeta"),
-        _address(ws, torch.uint8, ws.numel(), "ws"), ws.numel(), stream)
+        _address(ws, torch.uint8, ws.numel(), "ws"), ws.numel(), _here(x))
     if status:
         _check(status)
 
@@ -523,7 +526,7 @@ def fno_muon_step(tensors: MuonTensors, lr, momentum, ws, iterations=5, coeffici
                   nesterov=True, grad_norm=None, max_norm=1.0) -> None:
     stream = _list_stream(tensors)
     if tensors.device is not None:
-        _one_device(tensors.device, ws=ws, grad_norm=grad_norm)
+        _one_device(tensors.device, ws, grad_norm)
     options = FnoMuonOptions(lr, momentum, eps, *coefficients, iterations, 1 if nesterov else 0)
     status = lib().fno_muon_step(tensors.count, tensors.array, ctypes.addressof(options),
                                  _address(grad_norm, torch.float32, 1, "grad_norm"), max_norm,

@@ -18,13 +18,14 @@ __device__ __forceinline__ void wave_fence() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_wave_barrier();
 }
-template <class T> constexpr int kPasses = sizeof(T) == 4 ? 4 : 8;       // rows of a lane group in a tile: tiles start at multiples of 16 bytes
+template <class T> constexpr int kPasses = sizeof(T) == 4 ? 4 : 8;       // rows of a lane group in a tile, at most
 
 struct Rows {
   long long rows;
   int lg;                    // G = 2^lg lanes a row
+  int each;                  // rows of a tile
 };
-// A tile's values between memory and LDS: E pieces a lane (kPasses rows of C <= E G channels for each of 64 / G groups).  Pieces past
+// A tile's values between memory and LDS: E pieces a lane (at most kPasses rows of C <= E G channels for each of 64 / G groups).  Pieces past
 // the end read the last one again, so that no load waits behind a branch.
 template <int E, bool STREAM, class T>
 __device__ __forceinline__ void tile_in(const T* from, T* to, int count) {
@@ -186,13 +187,21 @@ void with_row(int C, F&& f) {
   else if constexpr (SIZE == 4) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
 }
 inline int size_of(const LayerShape& n) { return n.bf16 ? 2 : 4; }
+// Tiles start at multiples of 16 bytes.  They are as long as kPasses allows where that makes 2048 of them, eight waves a compute
+// unit, else shorter: 53760 rows of 27 in bf16 took 8.9 us with 420 tiles.
+inline Rows rows_of(const LayerShape& n) {
+  Rows r{n.B * n.P, lanes_of(n.C), 0};
+  int passes = n.bf16 ? kPasses<u16> : kPasses<float>;
+  const int group = 64 >> r.lg;
+  while (passes > 1 && group * (passes / 2) * n.C * size_of(n) % 16 == 0 && r.rows < 2048ll * group * passes) passes /= 2;
+  r.each = group * passes;
+  return r;
+}
 inline long long row_tiles(const LayerShape& n) {
-  const int rows = (64 >> lanes_of(n.C)) * (n.bf16 ? kPasses<u16> : kPasses<float>);
-  return (n.B * n.P + rows - 1) / rows;
+  const Rows r = rows_of(n);
+  return (r.rows + r.each - 1) / r.each;
 }
-inline size_t tile_bytes(const LayerShape& n) {                   // of a block's four waves
-  return (size_t)4 * (64 >> lanes_of(n.C)) * (n.bf16 ? kPasses<u16> : kPasses<float>) * n.C * size_of(n);
-}
+inline size_t tile_bytes(const LayerShape& n) { return (size_t)4 * rows_of(n).each * n.C * size_of(n); }      // of a block's four waves
 
 }  // namespace
 

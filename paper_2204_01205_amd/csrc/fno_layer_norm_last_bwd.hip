@@ -9,7 +9,7 @@ template <class T, int E, bool ALIGNED, int ACT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void tile_bwd_kernel(LayerArgs a, Rows r, const T* x, const T* gy, T* gx) {
   extern __shared__ __align__(16) char mem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = (64 >> r.lg) * kPasses<T>, group = lane >> r.lg, first = (lane & ((1 << r.lg) - 1)) * E;
+  const int rows = r.each, group = lane >> r.lg, first = (lane & ((1 << r.lg) - 1)) * E;
   const int have = a.C - first < 0 ? 0 : a.C - first < E ? a.C - first : E;
   T *const mine = reinterpret_cast<T*>(mem) + (size_t)w * 2 * rows * a.C, *const cot = mine + rows * a.C;
   float ga[E], be[E], sg[E], sb[E];
@@ -200,7 +200,7 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
           const size_t sums = (size_t)8 * a.C * sizeof(float), bytes = 2 * tile_bytes(c.n) > sums ? 2 * tile_bytes(c.n) : sums;
           const auto kernel = tile_bwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>;
           if (bytes > 64 * 1024) set = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-          if (set == hipSuccess) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, s, a, Rows{rows, lanes_of(a.C)}, x, gy, gx);
+          if (set == hipSuccess) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, s, a, rows_of(c.n), x, gy, gx);
       });
     } else {
       with_row<sizeof(T)>(a.C, [&](auto w, auto n) {

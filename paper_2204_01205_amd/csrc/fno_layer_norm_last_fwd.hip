@@ -9,7 +9,7 @@ template <class T, int E, bool ALIGNED, int ACT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void tile_fwd_kernel(LayerArgs a, Rows r, const T* x, T* y) {
   extern __shared__ __align__(16) char mem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = (64 >> r.lg) * kPasses<T>, group = lane >> r.lg, first = (lane & ((1 << r.lg) - 1)) * E;
+  const int rows = r.each, group = lane >> r.lg, first = (lane & ((1 << r.lg) - 1)) * E;
   const int have = a.C - first < 0 ? 0 : a.C - first < E ? a.C - first : E;
   T* const mine = reinterpret_cast<T*>(mem) + (size_t)w * rows * a.C;
   float ga[E], be[E];
@@ -86,7 +86,7 @@ hipError_t launch_layer_last_fwd(const LayerCall& c, hipStream_t s) {
     if (a.C <= kTileChannels) {
       with_channels<sizeof(T)>(a.C, [&](auto e, auto whole) {
         hipLaunchKernelGGL((tile_fwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>), dim3(grid_of((row_tiles(c.n) + 3) / 4)),
-                             dim3(kThreads), tile_bytes(c.n), s, a, Rows{rows, lanes_of(a.C)}, x, y);
+                             dim3(kThreads), tile_bytes(c.n), s, a, rows_of(c.n), x, y);
       });
     } else {
       with_row<sizeof(T)>(a.C, [&](auto w, auto n) {

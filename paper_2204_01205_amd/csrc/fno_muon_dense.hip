@@ -310,14 +310,19 @@ template <int T> constexpr int kStages = T == 64 ? 4 : 2;
 
 // A T x T tile, or a share of its sum.  PHASE 0: A = X X^T; 1: B = b A + c A A; 2: X = a X + B X.
 template <int T, int PHASE>
-__global__ __launch_bounds__(kThreads) void dense_product_kernel(DenseList l, MuonScalars c, int it) {
+__global__ __launch_bounds__(kThreads) void dense_product_kernel(DenseList l, MuonScalars c, int it, unsigned blocks) {
   constexpr int W = T / 2, N = W / 32, LINE = 128, SIDE = T * LINE;       // a wave's share of the tile; bytes of an operand in LDS
   constexpr int STAGES = kStages<T>, LOADS = T / 16;                      // steps in LDS or on their way; a wave's loads of one
   __shared__ __align__(16) char lds[STAGES][2 * SIDE];
   float scale;
   if (!muon_scale(c, scale)) return;
-  const DenseEntry& t = entry_of(l, [](const DenseEntry& e) { return e.first[PHASE]; });
-  const unsigned local = blockIdx.x - t.first[PHASE], splits = t.splits[PHASE];
+  // an XCD has a contiguous share of the tiles, whose operands overlap: they stay in its L2
+  const unsigned item = (unsigned)xcd_contiguous_item(blockIdx.x, gridDim.x);
+  if (item >= blocks) return;
+  int e = 0;
+  while (e + 1 < l.count && l.t[e + 1].first[PHASE] <= item) ++e;
+  const DenseEntry& t = l.t[e];
+  const unsigned local = item - t.first[PHASE], splits = t.splits[PHASE];
   const TileOf o = tile_of<T, PHASE>(t, local, splits);
   const Region r = region_of(t, o.matrix);
   const int inner = PHASE == 0 ? t.np : t.mp, steps = inner / kStep, share = (steps + (int)splits - 1) / (int)splits;
@@ -448,7 +453,7 @@ __global__ __launch_bounds__(kThreads) void dense_sum_kernel(DenseList l, MuonSc
 
 constexpr long long kGroupBytes = 1ll << 30;     // scratch of the matrices that go through their launches together, where they are several
 constexpr unsigned kMostBlocks = 1u << 22;       // of a launch
-constexpr int kWantBlocks = 512, kLeastSteps = 8;
+constexpr int kWantBlocks = 256, kLeastSteps = 8;
 
 long long tiles_host(long long mp, long long np, int T, int phase) {
   const long long tm = mp / T;
@@ -561,7 +566,7 @@ bool next_group(const MuonTensor* t, int count, double lr, int& k, long long& do
 
 template <int T, int PHASE>
 hipError_t launch_product(const Group& g, const MuonScalars& c, int it, hipStream_t s) {
-  hipLaunchKernelGGL((dense_product_kernel<T, PHASE>), dim3(g.blocks[PHASE]), dim3(kThreads), 0, s, g.l, c, it);
+  hipLaunchKernelGGL((dense_product_kernel<T, PHASE>), dim3((g.blocks[PHASE] + 7) / 8 * 8), dim3(kThreads), 0, s, g.l, c, it, g.blocks[PHASE]);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.sums[PHASE] == 0) return e;
   hipLaunchKernelGGL((dense_sum_kernel<T, PHASE>), dim3(g.sums[PHASE] * (T / 64) * (T / 64)), dim3(kThreads), 0, s, g.l, c, it);
