@@ -1,6 +1,7 @@
 // What layer norm's kernels share: accesses, statistics, and the sums of the gradients of gamma and beta.
 #pragma once
 #include "fno_norm_device.h"
+#include <algorithm>
 
 namespace fno {
 

@@ -151,11 +151,10 @@ __global__ __launch_bounds__(1024) void shared_bwd_kernel(LayerArgs a, long long
   to[a.C] = sb;
 }
 
-// A lane's chain of additions is 256 tiles long at most; 2048 blocks fill the chip.
+// 2048 blocks fill the chip; more where a lane's chain of additions would be longer than 256 tiles.  2^20 is past any memory.
 int blocks_for(long long tiles, int waves) {
-  long long b = (tiles + waves - 1) / waves;
-  const long long most = b / 256 > 2048 ? b / 256 : 2048;
-  return (int)(b < most ? b : most);
+  const long long b = (tiles + waves - 1) / waves;
+  return (int)std::min(b, std::clamp(b / 256, 2048ll, 1ll << 20));
 }
 
 }  // namespace

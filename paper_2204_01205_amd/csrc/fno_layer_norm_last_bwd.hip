@@ -164,11 +164,10 @@ __global__ __launch_bounds__(kRowThreads<W>) void wide_bwd_kernel(LayerArgs a, l
 
 // ------------------------------------------------------------------------------------------ launches
 
-// A lane's chain of additions is 256 rows or tiles long at most where more than `most` blocks would not fill the chip better.
+// `most` blocks, more where a lane's chain of additions would be longer than 256 rows or tiles; 2^20 is past any memory.
 int blocks_for(long long items, int each, int most) {
-  long long b = (items + each - 1) / each;
-  const long long cap = b / 256 > most ? b / 256 : most;
-  return (int)(b < cap ? b : cap);
+  const long long b = (items + each - 1) / each;
+  return (int)std::min(b, std::clamp(b / 256, (long long)most, 1ll << 20));
 }
 
 }  // namespace
@@ -199,7 +198,7 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
       with_channels<sizeof(T)>(a.C, [&](auto e, auto whole) {
           const size_t sums = (size_t)8 * a.C * sizeof(float), bytes = 2 * tile_bytes(c.n) > sums ? 2 * tile_bytes(c.n) : sums;
           const auto kernel = tile_bwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>;
-          if (bytes > 64 * 1024) set = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+          set = ask_local_memory(reinterpret_cast<const void*>(kernel), bytes);
           if (set == hipSuccess) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, s, a, rows_of(c.n), x, gy, gx);
       });
     } else {

@@ -166,8 +166,7 @@ hipError_t launch_muon_small(const MuonTensor* t, int count, const MuonScalars& 
   auto flush = [&]() {
     hipError_t e = hipSuccess;
     if (l.count > 0) {
-      if (bytes > 60 * 1024)
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(muon_small_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+      e = ask_local_memory(reinterpret_cast<const void*>(muon_small_kernel), bytes + kSmallThreads / 64 * sizeof(double));
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(muon_small_kernel, dim3((unsigned)blocks), dim3(kSmallThreads), bytes, s, l, c);
       e = hipGetLastError();
