@@ -35,9 +35,11 @@ def parse():
                          "projection, relative L2 loss, backward, Adam) instead of one block")
     ap.add_argument("--group-norm", type=int, default=0, metavar="GROUPS",
                     help="with --network: blocks without an activation, each followed by a group norm with GELU")
-    ap.add_argument("--optimizer", choices=("adam", "adamw", "adamw8"), default="adam",
-                    help="with --network: Adam tensor by tensor, or AdamW over all tensors with clipping by the norm of all "
-                         "gradients, moments in 32 or in 8 bits")
+    ap.add_argument("--layer-norm", action="store_true",
+                    help="with --network: blocks without an activation, each followed by a layer norm with GELU")
+    ap.add_argument("--optimizer", choices=("adam", "adamw", "adamw8", "muon"), default="adam",
+                    help="with --network: Adam tensor by tensor, or with clipping by the norm of all gradients AdamW over all "
+                         "tensors, moments in 32 or in 8 bits, or Muon for matrices and spectral weights with AdamW for vectors")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="only run plain device copies of 4 GiB (reference reading for rocprofv3 --pmc "
                          "FETCH_SIZE / WRITE_SIZE), then exit")
@@ -163,7 +165,15 @@ def network_step_bench(args, torch, B, synth):
                       dtype=torch.float32, device="cuda")
     loss = torch.empty(1, device="cuda")
     params = [lw, lb, w1, b1, w2, b2] + [t for blk in blocks for t in blk]
-    groups = args.group_norm
+    groups, layered = args.group_norm, args.layer_norm
+    if groups and layered:
+        raise SystemExit("--group-norm and --layer-norm: one of them")
+    if layered:
+        bare = B.make_desc(batch, width, width, grid, modes, 0, B.FNO_ACT_IDENTITY)
+        ndesc = B.make_layer_norm_desc(batch, width, npts, activation=B.FNO_ACT_GELU)
+        nws = B.alloc_layer_norm_workspace(ndesc)
+        affine = [(1 + 0.1 * rn(width), 0.1 * rn(width)) for _ in range(nblocks)]
+        params += [t for pair in affine for t in pair]
     if groups:                                 # the norms' parameters and what they keep for the backward pass
         bare = B.make_desc(batch, width, width, grid, modes, 0, B.FNO_ACT_IDENTITY)
         ndesc = B.make_norm_desc(batch, width, groups, npts, activation=B.FNO_ACT_GELU)
@@ -177,6 +187,16 @@ def network_step_bench(args, torch, B, synth):
     gflat = [torch.view_as_real(t).reshape(-1) if t.is_complex() else t.reshape(-1) for t in grads]
     if args.optimizer == "adam":
         moms = [(torch.zeros_like(f), torch.zeros_like(f)) for f in flat]
+    elif args.optimizer == "muon":
+        pick = lambda ts, least, most: [t for t, p in zip(ts, params) if least <= p.dim() <= most]
+        matrices, vectors = pick(params, 2, 6), pick(params, 1, 1)
+        muon = B.make_muon_tensors(matrices, pick(grads, 2, 6), [torch.zeros_like(p) for p in matrices],
+                                   [max(1.0, p.shape[0] / p.shape[1]) ** 0.5 for p in matrices], 0.01)
+        tensors = B.make_adamw_tensors(vectors, pick(grads, 1, 1), *([torch.zeros_like(p) for p in vectors] for _ in range(2)),
+                                       None, [0.0] * len(vectors))
+        everything = B.make_grad_tensors(grads)
+        gnorm, gws = torch.empty(1, device="cuda"), B.alloc_grad_norm_workspace(everything)
+        mws = B.alloc_muon_workspace(muon)
     else:
         kind = torch.uint8 if args.optimizer == "adamw8" else torch.float32
         mom, sq = ([torch.zeros(f.numel(), dtype=kind, device="cuda") for f in flat] for _ in range(2))
@@ -195,6 +215,9 @@ def network_step_bench(args, torch, B, synth):
             if groups:
                 B.fno_block_fwd(bare, v, R, W, b, out, None, None, ws)
                 B.fno_group_norm_fwd(ndesc, out, *affine[k], out, None, None, nws)
+            elif layered:
+                B.fno_block_fwd(bare, v, R, W, b, out, None, None, ws)
+                B.fno_layer_norm_fwd(ndesc, out, *affine[k], out)
             else:
                 B.fno_block_fwd(desc, v, R, W, b, out, None, None, ws)
         B.fno_pointwise_mlp2(batch, width, hidden, 1, npts, vs[nblocks & 1], w1, b1, w2, b2, u)
@@ -208,6 +231,9 @@ def network_step_bench(args, torch, B, synth):
             if groups:
                 B.fno_block_fwd(bare, vs[k], R, W, b, zs[k], None, xhs[k], ws)
                 B.fno_group_norm_fwd(ndesc, zs[k], *affine[k], vs[k + 1], *stats[k], nws)
+            elif layered:
+                B.fno_block_fwd(bare, vs[k], R, W, b, zs[k], None, xhs[k], ws)
+                B.fno_layer_norm_fwd(ndesc, zs[k], *affine[k], vs[k + 1])
             else:
                 B.fno_block_fwd(desc, vs[k], R, W, b, vs[k + 1], zs[k], xhs[k], ws)
         B.fno_pointwise_mlp2(batch, width, hidden, 1, npts, vs[-1], w1, b1, w2, b2, u)
@@ -216,13 +242,20 @@ def network_step_bench(args, torch, B, synth):
         gin, gout = gva, gvb
         for k in reversed(range(nblocks)):
             R, W, b = blocks[k]
+            at = 6 + 3 * nblocks + 2 * k
             if groups:
-                at = 6 + 3 * nblocks + 2 * k
                 B.fno_group_norm_bwd(ndesc, zs[k], *affine[k], *stats[k], gin, gin, grads[at], grads[at + 1], nws)
-            B.fno_block_bwd(bare if groups else desc, vs[k], R, W, zs[k], xhs[k], gin, gout, gblk[k][0], gblk[k][1],
+            elif layered:
+                B.fno_layer_norm_bwd(ndesc, zs[k], *affine[k], gin, gin, grads[at], grads[at + 1], nws)
+            B.fno_block_bwd(bare if groups or layered else desc, vs[k], R, W, zs[k], xhs[k], gin, gout, gblk[k][0], gblk[k][1],
                             gblk[k][2], ws)
             gin, gout = gout, gin
         B.fno_pointwise_linear_bwd(batch, c_in, width, npts, a, lw, gin, None, glw, glb, pws)
+        if args.optimizer == "muon":
+            B.fno_grad_norm(everything, gnorm, gws)
+            B.fno_muon_step(muon, 1e-2, 0.95, mws, grad_norm=gnorm, max_norm=1.0)
+            B.fno_adamw_step(tensors, 1e-3, 0.9, 0.999, 1e-8, state["step"], grad_norm=gnorm, max_norm=1.0)
+            return
         if args.optimizer != "adam":
             B.fno_grad_norm(tensors, gnorm, gws)
             B.fno_adamw_step(tensors, 1e-3, 0.9, 0.999, 1e-8, state["step"], grad_norm=gnorm, max_norm=1.0, seed=0)
@@ -239,8 +272,9 @@ def network_step_bench(args, torch, B, synth):
     torch.cuda.synchronize()
     ms = 1e3 * (time.perf_counter() - t0) / args.steps
     pc = float(batch) * width * npts
-    step_text = {"adam": "Adam", "adamw": "AdamW with clipping", "adamw8": "AdamW with clipping, moments in 8 bits"}
-    norm_text = f", group norm of {groups} groups behind every block" if groups else ""
+    step_text = {"adam": "Adam", "adamw": "AdamW with clipping", "adamw8": "AdamW with clipping, moments in 8 bits",
+                 "muon": "Muon for matrices and spectral weights and AdamW for vectors with clipping"}
+    norm_text = f", group norm of {groups} groups behind every block" if groups else ", layer norm behind every block" if layered else ""
     print(json.dumps({
         "metric": "FNO spectral layer Gpoint-channels/s + achieved HBM GB/s on 1 MI355X",
         "value": nblocks * pc / (ms * 1e-3) / 1e9, "unit": "Gpoint-channels/s", "n_gpus": 1, "steps": args.steps,
