@@ -12,8 +12,10 @@ struct MuonScalars {
   const float* norm;      // device scalar, nullable
 };
 
-// Steps of the spectral weights: five tiles of four channels on either side (fno_muon_modes5.hip), and all others
-// (fno_muon_modes.hip)
+// Steps of the spectral weights: two (fno_muon_modes2.hip) or five tiles of four channels on either side (fno_muon_modes5.hip), and
+// all others (fno_muon_modes.hip)
+bool muon_is_modes2(const MuonTensor& t);
+hipError_t launch_muon_modes2(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);
 bool muon_is_modes5(const MuonTensor& t);
 hipError_t launch_muon_modes5(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);
 hipError_t launch_muon_modes(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s);

@@ -10,7 +10,7 @@
 //   X = B X: its own columns, B from LDS.
 // X, A and B take turns in one LDS buffer, [row][tile][mode][column] with one entry of padding a row: a tile read by columns
 // is contiguous, one read by rows has its four rows in neighbouring banks.
-#include "fno_muon.h"
+#include "fno_muon_modes.h"
 
 namespace fno {
 
@@ -33,8 +33,6 @@ struct ModesList {
   int count;
   unsigned blocks;
 };
-
-__device__ __forceinline__ v4f mfma4(float a, float b, v4f c) { return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, 0, 0, 0); }
 
 // A place that the compiler takes for a new one: it would keep the addresses of all rows between the loads and the stores.
 __device__ __forceinline__ long long opaque_place(long long at) {
@@ -313,7 +311,7 @@ hipError_t launch_muon_modes(const MuonTensor* t, int count, const MuonScalars& 
       };
       for (int k = 0; k < count; ++k) {
         const int rows = t[k].rows, cols = t[k].cols, m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-        if (!t[k].modes || muon_is_modes5(t[k]) || (m + 3) / 4 != tm || (n + 3) / 4 != tn) continue;
+        if (!t[k].modes || muon_is_modes5(t[k]) || muon_is_modes2(t[k]) || (m + 3) / 4 != tm || (n + 3) / 4 != tn) continue;
         const long long row = (long long)cols * t[k].batch, column = t[k].batch, blocks = (t[k].batch + kModes - 1) / kModes;
         for (long long done = 0; done < blocks;) {
           if (l.count == kPerLaunch || l.blocks == kMost) {

@@ -11,7 +11,7 @@
 //   tiles' worth.
 // X, A and B take turns in a wave's 13 KB of LDS, [row][column][mode] with four places of padding a row: rows and columns of a tile
 // are read without bank conflicts.  The fifth column of X has a place of its own beside them.
-#include "fno_muon.h"
+#include "fno_muon_modes.h"
 
 #include <type_traits>
 
@@ -37,32 +37,6 @@ struct Modes5List {
   int count;
   unsigned waves;
 };
-
-__device__ __forceinline__ v4f mfma4(float a, float b, v4f c) { return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, 0, 0, 0); }
-// LDS accesses of a wave are worked in order; this keeps the compiler to it.
-__device__ __forceinline__ void own_fence() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_wave_barrier();
-}
-// A complex tile.  In sums with a conjugate the imaginary part is i - h: an operand's sign would take an instruction a step.
-struct Tile4 {
-  v4f r, i, h;
-};
-__device__ __forceinline__ void clear(Tile4& t) { t.r = t.i = t.h = v4f{0.f, 0.f, 0.f, 0.f}; }
-// t += a conj b
-__device__ __forceinline__ void add_conj_right(Tile4& t, float2 a, float2 b) {
-  t.r = mfma4(a.x, b.x, t.r);
-  t.i = mfma4(a.y, b.x, t.i);
-  t.h = mfma4(a.x, b.y, t.h);
-  t.r = mfma4(a.y, b.y, t.r);
-}
-// t += conj a b
-__device__ __forceinline__ void add_conj_left(Tile4& t, float2 a, float2 b) {
-  t.r = mfma4(a.x, b.x, t.r);
-  t.i = mfma4(a.x, b.y, t.i);
-  t.h = mfma4(a.y, b.x, t.h);
-  t.r = mfma4(a.y, b.y, t.r);
-}
 
 __global__ __launch_bounds__(64, 2) void muon_modes5_kernel(Modes5List l, MuonScalars c) {
   __shared__ float2 S[kRows * kPitch];
