@@ -25,7 +25,7 @@ typedef _Float16 half;
 constexpr float kX = 1024.f, kA = 256.f, kB = 64.f;
 constexpr int kPerLaunch = 16;         // matrices or stacks whose addresses go with one launch's arguments
 constexpr int kPieces = 256;           // partial sums of a matrix's norm, at most
-constexpr int kPieceValues = 4096;
+constexpr int kPieceValues = 16 * kThreads;
 constexpr int kStep = 32;              // inner dimension that goes to LDS at a time
 
 struct DenseEntry {
@@ -98,7 +98,28 @@ __global__ __launch_bounds__(kThreads) void dense_momentum_kernel(DenseList l, M
   const float* const g = t.g + matrix * values;
   float* const mom = t.mom + matrix * values;
   double sum = 0.0;
-  for (long long i = begin + threadIdx.x; i < end; i += kThreads) {
+  long long at = begin;
+  for (; at + kPieceValues <= end; at += kPieceValues) {
+    typedef v4f loose __attribute__((aligned(4)));
+    v4f u[4], mo[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      u[q] = *reinterpret_cast<const loose*>(g + at + (q * kThreads + threadIdx.x) * 4);
+      mo[q] = *reinterpret_cast<const loose*>(mom + at + (q * kThreads + threadIdx.x) * 4);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float m = mo[q][k];
+        const float v = muon_momentum(c, u[q][k] * scale, m);
+        mo[q][k] = m;
+        sum = fma((double)v, (double)v, sum);
+      }
+      *reinterpret_cast<loose*>(mom + at + (q * kThreads + threadIdx.x) * 4) = mo[q];
+    }
+  }
+  for (long long i = at + threadIdx.x; i < end; i += kThreads) {
     float mo = mom[i];
     const float u = muon_momentum(c, g[i] * scale, mo);
     mom[i] = mo;
