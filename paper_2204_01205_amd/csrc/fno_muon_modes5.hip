@@ -20,7 +20,7 @@ namespace fno {
 namespace {
 
 constexpr int kSide = 5, kRows = 4 * kSide, kPitch = 4 * kRows + 4;    // places of a row
-constexpr int kWaveModes = 4;
+constexpr int kWaveModes = 4, kWaves = 4;
 constexpr int kPerLaunch = 32;
 
 struct Modes5Entry {
@@ -28,28 +28,29 @@ struct Modes5Entry {
   const float2* g;
   float2* mom;
   long long modes, si, sj;             // si, sj: distance of rows and columns of X, in values
-  unsigned first, skip;                // first wave of the launch that belongs to this tensor; waves of it in earlier launches
+  unsigned first, skip;                // first block of the launch that belongs to this tensor; blocks of it in earlier launches
   int m, n;
   float keep, move;                    // 1 - lr weight_decay, lr scale
 };
 struct Modes5List {
   Modes5Entry t[kPerLaunch];
   int count;
-  unsigned waves;
+  unsigned blocks;
 };
 
-__global__ __launch_bounds__(64, 2) void muon_modes5_kernel(Modes5List l, MuonScalars c) {
-  __shared__ float2 S[kRows * kPitch];
-  __shared__ float2 last[kRows * 16];              // column 16 + j of X: [row][j][mode]
+__global__ __launch_bounds__(64 * kWaves, 2) void muon_modes5_kernel(Modes5List l, MuonScalars c) {
+  __shared__ float2 matrices[kWaves][kRows * kPitch], fifths[kWaves][kRows * 16];
   const unsigned item = (unsigned)xcd_contiguous_item(blockIdx.x, gridDim.x);
-  if (item >= l.waves) return;
+  if (item >= l.blocks) return;
   float scale;
   if (!muon_scale(c, scale)) return;
   int k = 0;
   while (k + 1 < l.count && l.t[k + 1].first <= item) ++k;
   const Modes5Entry& t = l.t[k];
-  const int lane = threadIdx.x, j = lane & 3, md = (lane >> 2) & 3, s = lane >> 4;
-  const long long mode0 = ((long long)(item - t.first) + t.skip) * kWaveModes;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 3, md = (lane >> 2) & 3, s = lane >> 4;
+  float2 *const S = matrices[w], *const last = fifths[w];              // last: column 16 + j of X, [row][j][mode]
+  const long long mode0 = (((long long)(item - t.first) + t.skip) * kWaves + w) * kWaveModes;
+  if (mode0 >= t.modes) return;
   const int have = t.modes - mode0 < kWaveModes ? (int)(t.modes - mode0) : kWaveModes;
   const bool here = md < have, here5 = here && 16 + j < t.n;
 
@@ -244,27 +245,27 @@ __global__ __launch_bounds__(64, 2) void muon_modes5_kernel(Modes5List l, MuonSc
         float2 v[kSide];
 #pragma unroll
         for (int T = 0; T < kSide; ++T) v[T] = tiles[n * kPitch + 16 * T];
-        const float2 vs = own[n * kPitch], w = fifth[n * 16];
+        const float2 vs = own[n * kPitch], f = fifth[n * 16];
         // (here the sign costs less than seven more accumulators)
-        const float nx = -x[n].x, nw = -w.x;
+        const float nx = -x[n].x, nf = -f.x;
 #pragma unroll
         for (int T = 0; T < kSide; ++T) {
           u[T].r = mfma4(v[T].x, x[n].x, u[T].r);
           u[T].i = mfma4(v[T].x, x[n].y, u[T].i);
         }
-        uy.r = mfma4(vs.x, w.x, uy.r);
-        uy.i = mfma4(vs.x, w.y, uy.i);
-        uz.r = mfma4(v[4].x, w.x, uz.r);
-        uz.i = mfma4(v[4].x, w.y, uz.i);
+        uy.r = mfma4(vs.x, f.x, uy.r);
+        uy.i = mfma4(vs.x, f.y, uy.i);
+        uz.r = mfma4(v[4].x, f.x, uz.r);
+        uz.i = mfma4(v[4].x, f.y, uz.i);
 #pragma unroll
         for (int T = 0; T < kSide; ++T) {
           u[T].r = mfma4(v[T].y, x[n].y, u[T].r);
           u[T].i = mfma4(v[T].y, nx, u[T].i);
         }
-        uy.r = mfma4(vs.y, w.y, uy.r);
-        uy.i = mfma4(vs.y, nw, uy.i);
-        uz.r = mfma4(v[4].y, w.y, uz.r);
-        uz.i = mfma4(v[4].y, nw, uz.i);
+        uy.r = mfma4(vs.y, f.y, uy.r);
+        uy.i = mfma4(vs.y, nf, uy.i);
+        uz.r = mfma4(v[4].y, f.y, uz.r);
+        uz.i = mfma4(v[4].y, nf, uz.i);
       }
     }
 #pragma unroll
@@ -302,34 +303,34 @@ bool muon_is_modes5(const MuonTensor& t) {
   return t.modes && t.rows > 16 && t.rows <= 20 && t.cols > 16 && t.cols <= 20 && 20 * (t.cols + 1) * t.batch < (1ll << 29);
 }
 
-// Launches of 2^22 waves at most.
+// Launches of 2^20 blocks at most.
 hipError_t launch_muon_modes5(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s) {
-  constexpr long long kMost = 1ll << 22;
+  constexpr long long kMost = 1ll << 20;
   Modes5List l;
   l.count = 0;
-  l.waves = 0;
+  l.blocks = 0;
   auto flush = [&]() {
-    if (l.count > 0) hipLaunchKernelGGL(muon_modes5_kernel, dim3((l.waves + 7) / 8 * 8), dim3(64), 0, s, l, c);
+    if (l.count > 0) hipLaunchKernelGGL(muon_modes5_kernel, dim3((l.blocks + 7) / 8 * 8), dim3(64 * kWaves), 0, s, l, c);
     const hipError_t e = l.count > 0 ? hipGetLastError() : hipSuccess;
     l.count = 0;
-    l.waves = 0;
+    l.blocks = 0;
     return e;
   };
   for (int k = 0; k < count; ++k) {
     if (!muon_is_modes5(t[k])) continue;
     const bool tall = t[k].rows > t[k].cols;
-    const long long row = (long long)t[k].cols * t[k].batch, column = t[k].batch, waves = (t[k].batch + kWaveModes - 1) / kWaveModes;
-    for (long long done = 0; done < waves;) {
-      if (l.count == kPerLaunch || l.waves == kMost) {
+    const long long row = (long long)t[k].cols * t[k].batch, column = t[k].batch, blocks = (t[k].batch + kWaves * kWaveModes - 1) / (kWaves * kWaveModes);
+    for (long long done = 0; done < blocks;) {
+      if (l.count == kPerLaunch || l.blocks == kMost) {
         const hipError_t e = flush();
         if (e != hipSuccess) return e;
       }
-      const long long here = waves - done < kMost - l.waves ? waves - done : kMost - l.waves;
+      const long long here = blocks - done < kMost - l.blocks ? blocks - done : kMost - l.blocks;
       l.t[l.count++] = Modes5Entry{reinterpret_cast<float2*>(t[k].p), reinterpret_cast<const float2*>(t[k].g),
-                                   reinterpret_cast<float2*>(t[k].m), (long long)t[k].batch, tall ? column : row, tall ? row : column, l.waves,
+                                   reinterpret_cast<float2*>(t[k].m), (long long)t[k].batch, tall ? column : row, tall ? row : column, l.blocks,
                                    (unsigned)done, tall ? t[k].cols : t[k].rows, tall ? t[k].rows : t[k].cols,
                                    (float)(1.0 - lr * t[k].decay), (float)(lr * t[k].scale)};
-      l.waves += (unsigned)here;
+      l.blocks += (unsigned)here;
       done += here;
     }
   }
