@@ -129,12 +129,12 @@ __device__ __forceinline__ float lanes_sum(float v, int lg) {
 }
 __device__ __forceinline__ float wave_sum(float v) { return lanes_sum(v, 6); }
 
+// out of the memory-side cache's reach: the nontemporal hint
+inline bool streams(const LayerShape& n) { return (double)n.B * n.C * (double)n.P * (n.bf16 ? 2 : 4) > (double)kStreamBytes; }
 template <class F>
 hipError_t with_layer_kind(const LayerShape& n, F&& f) {
   auto stream = [&](auto t, auto act) {
-    // out of the memory-side cache's reach: the nontemporal hint
-    const double bytes = (double)n.B * n.C * (double)n.P * sizeof(t);
-    if (bytes > (double)kStreamBytes) f(t, act, std::true_type());
+    if (streams(n)) f(t, act, std::true_type());
     else f(t, act, std::false_type());
   };
   auto act = [&](auto t) {

@@ -1,5 +1,6 @@
-// Layer norm of fields [B][C][P]: a lane has V consecutive points.  Up to 32 channels all of a point's are in one lane's registers
-// and waves need nothing of each other; more are dealt to the waves of a block, which exchange their sums through LDS.
+// Layer norm of fields [B][C][P]: a lane has V consecutive points.  Up to 12 channels, and up to 24 of
+// many points, all of a point's are in one lane's registers and waves need nothing of each other; else they are dealt to the waves of a
+// block, which exchange their sums through LDS.
 #pragma once
 #include "fno_layer_norm.h"
 
@@ -147,22 +148,29 @@ __device__ __forceinline__ void shared_statistics(const LayerArgs& a, float* lds
   }
 }
 
-constexpr int kNarrow = 32;
-// Points of a lane: as many registers as leave three or four waves a SIMD.
-template <class T, int KC> constexpr int kFwdPoints = 4;
-template <class T, int KC> constexpr int kBwdPoints = sizeof(T) == 4 ? (KC <= 8 ? 4 : 2) : (KC <= 16 ? 4 : 2);
+// All channels of a point in a lane's registers: up to 12 always, up to 24 where there are points enough to hide a lane's chain over
+// them.  us, forward and adjoint, a lane's own against shared: 24 channels in f32 at 2^17 points 9.3 and 16.4 against 7.0 and 15.9,
+// bf16 at 2^18 8.4 and 18.7 against 8.9 and 20.3, 20 channels in f32 at 2^24 542 and 752 against 500 and 958; 32 channels at 2^21 133
+// and 268 against 84 and 195.
+constexpr long long kEnoughPoints = 1ll << 18;
+inline bool is_narrow(const LayerShape& n) { return n.C <= 12 || (n.C <= 24 && n.B * n.P >= kEnoughPoints); }
+// Points of a lane: what leaves registers for enough waves.  us: bf16 forward, 16 channels, 2^21 points 26.9 with two, 30.4 with four; f32,
+// 8 channels, 23.5 with four, 26.8 with two.  Adjoint: bf16, 16 channels, 50.6 with two, 89.9 with four; f32, 20 channels, 112 with
+// one, 127 with two, 165 with four, but out of the caches (128 x 128 x 64 x 32 points) 1544 with two, 1600 with one.
+template <class T, int KC> constexpr int kFwdPoints = sizeof(T) == 4 || KC <= 8 ? 4 : 2;
+template <class T, int KC, bool STREAM> constexpr int kBwdPoints = KC <= 8 ? 4 : sizeof(T) == 4 && KC >= 16 && !STREAM ? 1 : 2;
+// Of a lane that shares its points: 64 channels, bf16, 2^19 points, us forward and adjoint 28 and 63 with two, 38 and 78 with one.
 template <int K> constexpr int kSharedPoints = K <= 16 ? 2 : 1;
 
 // Channels of a lane, and how many of them there are at least
-template <int KC> constexpr int kLeast = KC == 8 ? 1 : KC == 32 ? 25 : KC - 3;
+template <int KC> constexpr int kLeast = KC == 8 ? 1 : KC - 3;
 template <class F>
 void with_narrow(int C, F&& f) {
   if (C <= 8) f(std::integral_constant<int, 8>());
   else if (C <= 12) f(std::integral_constant<int, 12>());
   else if (C <= 16) f(std::integral_constant<int, 16>());
   else if (C <= 20) f(std::integral_constant<int, 20>());
-  else if (C <= 24) f(std::integral_constant<int, 24>());
-  else f(std::integral_constant<int, 32>());
+  else f(std::integral_constant<int, 24>());
 }
 // Channels of a wave, so that there are at most 16 waves
 template <class F>

@@ -161,10 +161,10 @@ int blocks_for(long long tiles, int waves) {
 
 int layer_first_blocks(const LayerShape& n) {
   int blocks = 0;
-  if (n.C <= kNarrow) {
+  if (is_narrow(n)) {
     with_narrow(n.C, [&](auto kc) {
       constexpr int KC = decltype(kc)::value;
-      const int v = n.bf16 ? kBwdPoints<u16, KC> : kBwdPoints<float, KC>;
+      const int v = n.bf16 ? kBwdPoints<u16, KC, true> : streams(n) ? kBwdPoints<float, KC, true> : kBwdPoints<float, KC, false>;
       blocks = blocks_for(tiles_host(n, v), kThreads / 64);
     });
   } else {
@@ -181,9 +181,9 @@ hipError_t launch_layer_first_bwd(const LayerCall& c, int blocks, hipStream_t s)
     constexpr bool S = decltype(stream)::value;
     const T *x = static_cast<const T*>(c.x), *gy = static_cast<const T*>(c.gy);
     T* const gx = static_cast<T*>(c.out);
-    if (a.C <= kNarrow) {
+    if (is_narrow(c.n)) {
       with_narrow(a.C, [&](auto kc) {
-        constexpr int KC = decltype(kc)::value, V = kBwdPoints<T, KC>;
+        constexpr int KC = decltype(kc)::value, V = kBwdPoints<T, KC, S>;
         hipLaunchKernelGGL((first_bwd_kernel<T, KC, V, ACT, S>), dim3(blocks), dim3(kThreads), 0, s, a, tiles_host(c.n, V), x, gy, gx);
       });
     } else {

@@ -72,7 +72,7 @@ hipError_t launch_layer_first_fwd(const LayerCall& c, hipStream_t s) {
     const LayerArgs a = layer_args(c);
     const T* const x = static_cast<const T*>(c.x);
     T* const y = static_cast<T*>(c.out);
-    if (a.C <= kNarrow) {
+    if (is_narrow(c.n)) {
       with_narrow(a.C, [&](auto kc) {
         constexpr int KC = decltype(kc)::value, V = kFwdPoints<T, KC>;
         const long long tiles = tiles_host(c.n, V);

@@ -1,6 +1,6 @@
 // Layer norm of rows: fields [B][P][C], channels last.
 //
-// Up to 512 channels a wave takes a tile of rows, a stretch of memory that starts at a multiple of 16 bytes whatever C is: it goes
+// Up to some 400 channels (512 that are no whole 16-byte pieces) a wave takes a tile of rows, a stretch of memory that starts at a multiple of 16 bytes whatever C is: it goes
 // to LDS in 16-byte pieces, a group of G lanes (a power of two) takes a row, E = 4 .. 8 channels each, and the results
 // go the same way back.  A wave's LDS is its own, so waves need no barrier.  More channels: a row a wave or a block, in
 // registers, straight from memory.
@@ -154,8 +154,6 @@ __device__ __forceinline__ float wide_statistics(const LayerArgs& a, int left, f
 template <int W> constexpr int kRowThreads = W == 1 ? 256 : 64 * W;
 // ------------------------------------------------------------------------------------------ launches
 
-constexpr int kTileChannels = 512;
-
 inline int lanes_of(int C) {
   int lg = 0;
   while ((C + (1 << lg) - 1) >> lg > 8) ++lg;
@@ -175,20 +173,26 @@ void with_channels(int C, F&& f) {
   else if (e == 7) f(std::integral_constant<int, 7>(), std::false_type());
   else f(std::integral_constant<int, 8>(), std::false_type());
 }
-// Waves of a row and 16-byte pieces of a lane
-template <int SIZE, class F>
+// Waves of a row and 16-byte pieces of a lane: two or four of them, whose sums are the less work the fewer waves have a row (16384 rows
+// of 1024 in bf16, adjoint: 33.6 us with one, 102 with four), as far as the registers go (8192 rows of 8192 in bf16, adjoint: 308 us with
+// four waves, 204 with sixteen).
+template <int SIZE, bool BWD, class F>
 void with_row(int C, F&& f) {
   const int pieces = (C * SIZE + 1023) / 1024;             // of a wave
   if (pieces <= 2) f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
   else if (pieces <= 4) f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
   else if (pieces <= 8) f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
-  else if (pieces <= 16) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+  else if (pieces <= 16 && !(BWD && SIZE == 2)) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
   else if (pieces <= 32) f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
   else if constexpr (SIZE == 4) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
 }
 inline int size_of(const LayerShape& n) { return n.bf16 ? 2 : 4; }
+// Rows that are wide enough go without LDS, in bf16 where they are whole 16-byte pieces.  us for 65536 rows, forward and adjoint, in
+// tiles against registers: f32 of 512 50 and 101 against 42 and 93, of 300 30 and 59 against 33 and 64; bf16 of 512 37 and 83 against
+// 37 and 69, of 448 34 and 86 against 41 and 78, of 511 42 and 97 against 51 and 120.
+inline bool in_tiles(const LayerShape& n) { return n.C < (n.bf16 ? 480 : 384) || (n.bf16 && n.C <= 512 && n.C % 8 != 0); }
 // Tiles start at multiples of 16 bytes.  They are as long as kPasses allows where that makes 2048 of them, eight waves a compute
-// unit, else shorter: 53760 rows of 27 in bf16 took 8.9 us with 420 tiles.
+// unit, else shorter: 53760 rows of 27 in bf16 take 6.6 us, 8.9 with 420 tiles.
 inline Rows rows_of(const LayerShape& n) {
   Rows r{n.B * n.P, lanes_of(n.C), 0};
   int passes = n.bf16 ? kPasses<u16> : kPasses<float>;

@@ -173,14 +173,14 @@ int blocks_for(long long items, int each, int most) {
 }  // namespace
 
 int layer_last_blocks(const LayerShape& n) {
-  if (n.C <= kTileChannels) return blocks_for(row_tiles(n), 4, 1024);
+  if (in_tiles(n)) return blocks_for(row_tiles(n), 4, 1024);
   int blocks = 0;
   auto count = [&](auto w, auto) {
     constexpr int W = decltype(w)::value;
     blocks = W == 1 ? blocks_for(n.B * n.P, 4, 1024) : blocks_for(n.B * n.P, 1, W == 4 ? 1024 : 512);
   };
-  if (n.bf16) with_row<2>(n.C, count);
-  else with_row<4>(n.C, count);
+  if (n.bf16) with_row<2, true>(n.C, count);
+  else with_row<4, true>(n.C, count);
   return blocks;
 }
 
@@ -194,7 +194,7 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
     const T *x = static_cast<const T*>(c.x), *gy = static_cast<const T*>(c.gy);
     T* const gx = static_cast<T*>(c.out);
     const long long rows = a.B * a.P;
-    if (a.C <= kTileChannels) {
+    if (in_tiles(c.n)) {
       with_channels<sizeof(T)>(a.C, [&](auto e, auto whole) {
           const size_t sums = (size_t)8 * a.C * sizeof(float), bytes = 2 * tile_bytes(c.n) > sums ? 2 * tile_bytes(c.n) : sums;
           const auto kernel = tile_bwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>;
@@ -202,7 +202,7 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
           if (set == hipSuccess) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, s, a, rows_of(c.n), x, gy, gx);
       });
     } else {
-      with_row<sizeof(T)>(a.C, [&](auto w, auto n) {
+      with_row<sizeof(T), true>(a.C, [&](auto w, auto n) {
         constexpr int W = decltype(w)::value;
         hipLaunchKernelGGL((wide_bwd_kernel<T, W, decltype(n)::value, ACT, S>), dim3(blocks), dim3(kRowThreads<W>),
                            W == 1 ? 2 * a.C * sizeof(float) : 0, s, a, rows, x, gy, gx);

@@ -83,13 +83,13 @@ hipError_t launch_layer_last_fwd(const LayerCall& c, hipStream_t s) {
     const T* const x = static_cast<const T*>(c.x);
     T* const y = static_cast<T*>(c.out);
     const long long rows = a.B * a.P;
-    if (a.C <= kTileChannels) {
+    if (in_tiles(c.n)) {
       with_channels<sizeof(T)>(a.C, [&](auto e, auto whole) {
         hipLaunchKernelGGL((tile_fwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>), dim3(grid_of((row_tiles(c.n) + 3) / 4)),
                              dim3(kThreads), tile_bytes(c.n), s, a, rows_of(c.n), x, y);
       });
     } else {
-      with_row<sizeof(T)>(a.C, [&](auto w, auto n) {
+      with_row<sizeof(T), false>(a.C, [&](auto w, auto n) {
         constexpr int W = decltype(w)::value;
         hipLaunchKernelGGL((wide_fwd_kernel<T, W, decltype(n)::value, ACT, S>), dim3(grid_of(W == 1 ? (rows + 3) / 4 : rows)),
                            dim3(kRowThreads<W>), 0, s, a, rows, x, y);

@@ -146,6 +146,56 @@ def test_many_points(layout, act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [13, 15, 16, 17, 19, 20, 21, 22, 24, 25])
+def test_channels_of_many_points(c, dtype):
+    """Channels first, where a lane takes all channels of a point only with enough points: that many, and one fewer."""
+    for b, p in ((1, 2 ** 18), (1, 2 ** 18 - 1), (2, 2 ** 17 + 77)):
+        n = Layer(b, c, p, "first", dtype, "identity", seed=c)
+        n.check_forward(n.forward())
+        n.check_backward(*n.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout,c,p,dtype", [("first", 20, 3400003, "f32"), ("first", 8, 8400001, "f32"), ("first", 16, 8500007, "bf16"),
+                                              ("first", 64, 1050005, "f32"), ("last", 27, 5000001, "bf16"), ("last", 1024, 132001, "bf16"),
+                                              ("last", 300, 224001, "f32")])
+def test_fields_beyond_the_caches(layout, c, p, dtype):
+    """More than 256 MB: sampled points against the oracle, the gradients of gamma and beta against sums in double over all."""
+    n = Layer(1, c, 1, layout, dtype, "identity", seed=15)
+    desc = B.make_layer_norm_desc(1, c, p, layout=n.desc.layout, dtype=n.desc.dtype, activation=B.FNO_ACT_IDENTITY)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(c)
+    shape = (c, p) if layout == "first" else (p, c)
+    x, gy = ((torch.randn(shape, device="cuda", generator=gen) + 0.5).to(n.torch_dtype) for _ in range(2))
+    assert x.numel() * x.element_size() > 2 ** 28
+    y, gx, ws = torch.empty_like(x), torch.empty_like(x), B.alloc_layer_norm_workspace(desc)
+    ws.fill_(255)
+    (ga, be), gg, gb = n.affine(), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    B.fno_layer_norm_fwd(desc, x, ga, be, y)
+    B.fno_layer_norm_bwd(desc, x, ga, be, gy, gx, gg, gb, ws)
+    torch.cuda.synchronize()
+    by_point = lambda t: t if layout == "first" else t.t()                      # [c][p]
+    at = torch.cat([torch.arange(700), torch.arange(p - 700, p), torch.randint(p, (3000,), generator=torch.Generator().manual_seed(1))]).cuda()
+    n.x, n.gy, y, gx = (by_point(t)[:, at].float().cpu().numpy()[None] for t in (x, gy, y, gx))
+    n.check_forward(y)
+    sums = [torch.zeros(c, dtype=torch.float64, device="cuda") for _ in range(5)]
+    for k in range(0, p, 200000):
+        v, g = (by_point(t)[:, k:k + 200000].double() for t in (x, gy))
+        mean = v.mean(0, keepdim=True)
+        rstd = 1.0 / ((v - mean).square().mean(0, keepdim=True) + n.eps).sqrt()
+        xh, m = (v - mean) * rstd, min(c, 64)
+        e = U * (xh.abs() * (m / 2 + 6) + m + 1 + m * m * U * mean.abs() * rstd)
+        for s, t in zip(sums, (g * xh, g, (g * xh).abs(), g.abs(), g.abs() * e)):
+            s += t.sum(1)
+    wg, wb, tg, tb, errors = (s.cpu().numpy() for s in sums)
+    assert np.all(np.abs(gg.cpu().numpy() - wg) <= errors + 516 * U * tg) and np.all(np.abs(gb.cpu().numpy() - wb) <= 516 * U * tb)
+    # of the sampled points, gx alone
+    ref = O.layer_norm_bwd(n.x, n.gamma, n.beta, n.eps, n.gy, "identity")
+    n.check_backward(gx, ref["ggamma"], ref["gbeta"])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("c,p,layout,dtype", [(20, 777, "first", "f32"), (27, 500, "last", "bf16"), (48, 300, "first", "bf16"), (2048, 40, "last", "f32")])
 def test_without_gamma_and_beta(c, p, layout, dtype):
     n = Layer(2, c, p, layout, dtype, "gelu", seed=9)
