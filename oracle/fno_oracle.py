@@ -562,8 +562,12 @@ def newton_schulz(u, iterations=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1
     x = x / np.where(size == 0, 1.0, size + eps)
     a, b, c = coefficients
     for _ in range(iterations):
-        A = x @ np.conj(np.swapaxes(x, -1, -2))
-        x = a * x + (b * A + c * (A @ A)) @ x
+        if x.shape[-2] > x.shape[-1]:                     # X (b H + c H^2) with H = X^H X is the same, on the shorter side
+            H = np.conj(np.swapaxes(x, -1, -2)) @ x
+            x = a * x + x @ (b * H + c * (H @ H))
+        else:
+            A = x @ np.conj(np.swapaxes(x, -1, -2))
+            x = a * x + (b * A + c * (A @ A)) @ x
     return x
 
 

@@ -327,6 +327,8 @@ template <int COUNT>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(COUNT) : "memory");
 }
+// (the same matrices, all in tiles of 128: 1430 us with three stages, 1469 with four, 1311 with two, which leave room for two blocks a
+// compute unit)
 template <int T> constexpr int kStages = T == 64 ? 4 : 2;
 
 // A T x T tile, or a share of its sum.  PHASE 0: A = X X^T; 1: B = b A + c A A; 2: X = a X + B X.
@@ -474,6 +476,8 @@ __global__ __launch_bounds__(kThreads) void dense_sum_kernel(DenseList l, MuonSc
 
 constexpr long long kGroupBytes = 1ll << 30;     // scratch of the matrices that go through their launches together, where they are several
 constexpr unsigned kMostBlocks = 1u << 22;       // of a launch
+// 4 x 1024 x 1024, 1024 x 4096, 4096 x 1024 and 1000 x 1536 together: 1277 us with 256 blocks wanted, 1311 with 512, 1470 with 1024; shares of 16 or
+// 32 steps at least are slower too.
 constexpr int kWantBlocks = 256, kLeastSteps = 8;
 
 long long tiles_host(long long mp, long long np, int T, int phase) {
@@ -491,16 +495,18 @@ struct Group {
 };
 bool is_dense(const MuonTensor& t) { return !t.modes && !muon_is_small(t); }
 
-// Tiles of 128 are worth it for matrices that have a few of them on a side, where all tensors together fill the chip.
+// Tiles of 128 read half as much for a product, and are worth it for matrices that have a few of them on a side, where all tensors together
+// fill the chip with them.  us a step with tiles of 64 and of 128: 1024 x 4096 481 and 420, eight of 1024 x 1024 912 and 788, 32 of
+// 512 x 512 562 and 529, but four of 1024 x 1024 526 and 541, 16 of 512 x 512 336 and 400, 64 of 192 x 192 172 and 244.
 int tile_side(const MuonTensor* t, int count, int k) {
   const int m = t[k].rows < t[k].cols ? t[k].rows : t[k].cols;
   if (m <= 192) return 64;
-  double tiles = 0.0;
+  double steps = 0.0;
   for (int i = 0; i < count; ++i) {
-    const int mi = t[i].rows < t[i].cols ? t[i].rows : t[i].cols;
-    if (is_dense(t[i]) && mi > 192) tiles += (double)t[i].batch * (double)tiles_host(padded(mi, 128), 0, 128, 0);
+    const int mi = t[i].rows < t[i].cols ? t[i].rows : t[i].cols, ni = t[i].rows + t[i].cols - mi;
+    if (is_dense(t[i]) && mi > 192) steps += (double)t[i].batch * (double)tiles_host(padded(mi, 128), 0, 128, 0) * (padded(ni, 128) / kStep);
   }
-  return tiles >= 128.0 ? 128 : 64;
+  return steps >= 4500.0 ? 128 : 64;
 }
 
 template <int T>

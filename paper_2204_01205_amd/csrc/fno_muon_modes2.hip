@@ -156,7 +156,11 @@ __global__ __launch_bounds__(64 * kWaves) void muon_modes2_kernel(Modes2List l, 
 
 }  // namespace
 
-bool muon_is_modes2(const MuonTensor& t) { return t.modes && t.rows > 4 && t.rows <= 8 && t.cols > 4 && t.cols <= 8; }
+// us a step of 8 x 8, here and in fno_muon_modes.hip: 1536 modes 11 and 16, 24576 32 and 39, 49152 51 and 55, 110592 125 and 109 (there half
+// of a Hermitian product's tiles are mirrored, here all four are worked out, and all a wave has are four modes of a cache line).
+bool muon_is_modes2(const MuonTensor& t) {
+  return t.modes && t.rows > 4 && t.rows <= 8 && t.cols > 4 && t.cols <= 8 && t.batch <= 65536;
+}
 
 // Launches of 2^22 blocks at most.
 hipError_t launch_muon_modes2(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s) {

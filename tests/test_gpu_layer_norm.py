@@ -196,6 +196,28 @@ def test_fields_beyond_the_caches(layout, c, p, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout,b,c,p", [("first", 2, 20, 55000003), ("first", 3, 100, 7200001), ("last", 2, 27, 40000001), ("last", 1, 1000, 2200003)])
+def test_offsets_past_32_bits(layout, b, c, p):
+    """More than 2^31 values in bf16: sampled points of every batch entry against the oracle, in place."""
+    n = Layer(1, c, 1, layout, "bf16", "gelu", seed=16)
+    desc = B.make_layer_norm_desc(b, c, p, layout=n.desc.layout, dtype=n.desc.dtype, activation=B.FNO_ACT_GELU)
+    shape = (b, c, p) if layout == "first" else (b, p, c)
+    x = torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_()
+    gy = torch.empty_like(x).normal_()
+    assert x.numel() > 2 ** 31
+    at = torch.cat([torch.arange(130), torch.arange(p // 2, p // 2 + 130), torch.arange(p - 130, p)]).cuda()
+    pick = lambda t: (t[:, :, at] if layout == "first" else t[:, at].transpose(1, 2)).float().cpu().numpy()
+    n.x, n.gy, (ga, be) = pick(x), pick(gy), n.affine()
+    ws = B.alloc_layer_norm_workspace(desc)
+    B.fno_layer_norm_bwd(desc, x, ga, be, gy, gy, None, None, ws)
+    B.fno_layer_norm_fwd(desc, x, ga, be, x)
+    torch.cuda.synchronize()
+    n.check_forward(pick(x))
+    ref = O.layer_norm_bwd(n.x, n.gamma, n.beta, n.eps, n.gy, "gelu")
+    n.check_backward(pick(gy), ref["ggamma"], ref["gbeta"])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("c,p,layout,dtype", [(20, 777, "first", "f32"), (27, 500, "last", "bf16"), (48, 300, "first", "bf16"), (2048, 40, "last", "f32")])
 def test_without_gamma_and_beta(c, p, layout, dtype):
     n = Layer(2, c, p, layout, dtype, "gelu", seed=9)

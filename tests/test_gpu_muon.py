@@ -117,6 +117,43 @@ def test_modes(ci):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(32, 512), (32, 513), (513, 32), (512, 31), (31, 528), (31, 529), (1, 16384), (16385, 1), (16384, 1), (2, 8191), (8192, 2), (4, 4096),
+                                   (3, 5461), (5, 3276), (3276, 5), (8, 2048), (7, 2341), (9, 1820), (16, 1024), (1024, 16), (17, 963), (4, 128), (4, 129), (8, 64),
+                                   (8, 65), (65, 6), (3, 200)], ids=lambda s: f"{s[0]}x{s[1]}")
+def test_the_largest_matrices_of_a_block_and_folded_ones(shape):
+    Muon([(shape, False)], seed=shape[0]).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(8, 8, 65536), (8, 8, 65537), (5, 8, 65540), (7, 6, 70001)])
+def test_many_modes_of_few_channels(shape):
+    Muon([(shape, True)], seed=2).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,is_complex", [((20, 20, 1270001), True), ((20, 20, 1350003), True), ((32, 32, 1100003), True), ((8, 7, 20000003), True),
+                                              ((2200001, 32, 32), False), ((300007, 90, 100), False)])
+def test_offsets_past_32_bits(shape, is_complex):
+    """Tensors of some 2^32 bytes and of more: sampled matrices against the oracle."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(shape[0])
+    dtype = torch.complex64 if is_complex else torch.float32
+    draws = [torch.randn(shape, dtype=dtype, device="cuda", generator=gen) for _ in range(2)]
+    params, (grads, momentum) = torch.zeros_like(draws[0]), draws
+    size = params.numel() * params.element_size()
+    assert size > 0.94 * 2 ** 32
+    count = shape[-1] if is_complex else shape[0]
+    at = torch.tensor([0, 1, 5, count // 3, count // 2 + 1, count - 17, count - 3, count - 2, count - 1], device="cuda")
+    pick = lambda t: np.ascontiguousarray(stack((t[..., at] if is_complex else t[at]).cpu().numpy()))
+    u = 0.9 * (pick(grads) + 0.9 * pick(momentum).astype(np.complex128 if is_complex else np.float64)) + pick(grads)
+    tensors = B.make_muon_tensors([params], [grads], [momentum], scale=-1.0)
+    B.fno_muon_step(tensors, 1.0, 0.9, B.alloc_muon_workspace(tensors))
+    torch.cuda.synchronize()
+    error = np.sqrt((np.abs(pick(params) - O.newton_schulz(u)) ** 2).sum((1, 2)))
+    assert np.all(error <= bounds(u, 5)), (error / bounds(u, 5)).max()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("iterations", [0, 1, 2, 5, 8])
 @pytest.mark.parametrize("nesterov", [True, False])
 def test_iterations(iterations, nesterov):

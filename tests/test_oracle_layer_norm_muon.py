@@ -89,3 +89,17 @@ def test_muon_step_of_modes_is_that_of_every_matrix():
         assert np.allclose(got_p[at], p[at] * 0.98 - 0.15 * O.newton_schulz(u))
     real = O.muon_step(p.real[..., 0], g.real[..., 0], m.real[..., 0], 0.1, 0.9, nesterov=False)
     assert np.allclose(real[0][2], p.real[2, ..., 0] - 0.1 * O.newton_schulz(real[1][2]))
+
+
+@pytest.mark.parametrize("is_complex", [False, True])
+def test_tall_matrices_are_wide_ones_transposed(is_complex):
+    rng = np.random.default_rng(21)
+    u = rng.standard_normal((3, 9, 4)) + (1j * rng.standard_normal((3, 9, 4)) if is_complex else 0)
+    x = O.newton_schulz(u)
+    assert np.abs(x - np.conj(np.swapaxes(O.newton_schulz(np.conj(np.swapaxes(u, 1, 2))), 1, 2))).max() <= 1e-12
+    for k in range(3):                                        # and as the formula has it, with the longer side's Gram matrix
+        y = u[k] / (np.linalg.norm(u[k]) + 1e-7)
+        for _ in range(5):
+            A = y @ y.conj().T
+            y = 3.4445 * y + (-4.7750 * A + 2.0315 * A @ A) @ y
+        assert np.abs(x[k] - y).max() <= 1e-12
