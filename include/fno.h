@@ -361,8 +361,10 @@ int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* c
  * kind FNO_MUON_MODES: complex [rows][cols][batch], the layout of the spectral weights R [Cin][Cout][modes]: one complex matrix
  * for every kept mode, the map that the mode mix applies there.  rows, cols <= 32 (FNO_EUNSUPPORTED beyond).
  *
- * Products: single precision, or sums of products of 16-bit parts that carry 22 bits of the largest value of a matrix (real
- * matrices with more than 32 on their shorter side).
+ * Products: single precision for spectral weights and for real matrices with up to 32 on their shorter side and 16384 values;
+ * for the others sums of products of 16-bit parts that carry 22 bits of a value, as long as X stays within 64, A within 256 and
+ * b A + c A A within 1024 (singular values of X up to 1.2, which the usual coefficients keep, are far from that; what leaves these
+ * ranges becomes infinite or NaN).  Sums in float in a fixed order: the same bits on every run of the same list.
  *
  * tensors, options: host memory, read during the call only; pointers in tensors are device pointers, param, grad and momentum
  * 4-byte aligned (8-byte: complex ones).  Tensors must not overlap.  Empty tensors (batch, rows or cols 0) and count = 0 are

@@ -488,7 +488,7 @@ def make_muon_tensors(params, grads, momentum, scale=1.0, weight_decay=0.0) -> M
     scale, decay = each(scale), each(weight_decay)
     if not (len(grads) == len(momentum) == len(scale) == len(decay) == count):
         raise ValueError("params, grads, momentum, scale and weight_decay must have one entry a tensor")
-    array, devices = (FnoMuonTensor * max(count, 1))(), set()
+    array, devices, written = (FnoMuonTensor * max(count, 1))(), set(), set()
     for k in range(count):
         p, is_complex = params[k], params[k].is_complex()
         if p.dim() < 2 or (not is_complex and p.dim() > 3):
@@ -501,8 +501,12 @@ def make_muon_tensors(params, grads, momentum, scale=1.0, weight_decay=0.0) -> M
         for name, t in (("params", p), ("grads", grads[k]), ("momentum", momentum[k])):
             if t.shape != p.shape or t.dtype != dtype:
                 raise ValueError(f"{name}[{k}] is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(p.shape)}")
-            if t.is_conj():
-                raise ValueError(f"{name}[{k}] is a conjugate view")
+            if t.is_conj() or t.is_neg():
+                raise ValueError(f"{name}[{k}] is a conjugate or negative view: its memory holds other values")
+            if name != "grads" and t.numel():              # two updates of one tensor would race
+                if t.data_ptr() in written:
+                    raise ValueError(f"{name}[{k}] is in the list already")
+                written.add(t.data_ptr())
         array[k] = FnoMuonTensor(_ptr(p, name=f"params[{k}]"), _ptr(grads[k], name=f"grads[{k}]"),
                                  _ptr(momentum[k], name=f"momentum[{k}]"), batch, rows, cols,
                                  FNO_MUON_MODES if is_complex else FNO_MUON_MATRICES, scale[k], decay[k])

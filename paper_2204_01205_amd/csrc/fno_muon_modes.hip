@@ -8,6 +8,8 @@
 //   A = X X^H and B = a + b A + c A A: wave J takes the tiles (J, J .. J + m/8), around the corner, of which the other half are
 //   the mirrors, operands from LDS (X by rows, A by columns);
 //   X = B X: its own columns, B from LDS.
+// Matrix instructions bound it: 110592 modes of 16 x 16 take 86 us an iteration, of which these are 52; the rest are the waits of a block's
+// waves for each other and for LDS.  Loads and stores alone take 275 us (4.1 TB/s).
 // X, A and B take turns in one LDS buffer, [row][tile][mode][column] with one entry of padding a row: a tile read by columns
 // is contiguous, one read by rows has its four rows in neighbouring banks.
 #include "fno_muon_modes.h"

@@ -6,6 +6,7 @@
 //   A = X X^T: a wave adds up its own columns', and the sums of all waves go through LDS: one barrier an iteration;
 //   B = a + b A + c A A, by every wave for itself, and X = B X, its own columns': with the steps of a product taken in the order 4 g + r the
 //   registers of a result are the operands of the next one, A and B being symmetric.
+// 8 x 8 takes 0.5 us an iteration, 32 x 32 1.7, 32 x 256 4.1 (a thread for every entry of a product: 1.0, 5.0 and 24).
 // Short wide matrices are folded: with m <= 8 (4) two (four) stretches of columns lie one below the other, and the blocks on the
 // diagonal of their Gram matrix add up to A.
 #include "fno_muon.h"

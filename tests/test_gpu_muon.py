@@ -400,3 +400,19 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     tensors = B.make_muon_tensors([good], [z(4, 5)], [z(4, 5)])
     with pytest.raises(ValueError):
         B.fno_muon_step(tensors, 0.1, 0.9, B.alloc_muon_workspace(tensors), grad_norm=torch.zeros(2, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_a_tensor_twice_and_lazy_views():
+    z = lambda *s, **k: torch.zeros(*s, device="cuda", **k)
+    p, other = z(4, 5), z(4, 5)
+    for params, momentum in (([p, p], [z(4, 5), z(4, 5)]), ([p, other], [z(4, 5)] * 2), ([p, other], [z(4, 5), p])):
+        with pytest.raises(ValueError, match="already"):
+            B.make_muon_tensors(params, [z(4, 5), z(4, 5)], momentum)
+    B.make_muon_tensors([z(0, 5), z(0, 5)], [z(0, 5)] * 2, [z(0, 5)] * 2)
+    g = z(4, 5)
+    B.make_muon_tensors([p, other], [g, g], [z(4, 5), z(4, 5)])                   # a gradient that is only read may be
+    c = lambda: z(3, 4, 5, dtype=torch.complex64)
+    for bad in (([c().conj()], [c()], [c()]), ([c()], [c().conj()], [c()]), ([c()], [c()], [c().conj()]), ([p], [torch._neg_view(g)], [other])):
+        with pytest.raises(ValueError, match="view"):
+            B.make_muon_tensors(*bad)
