@@ -275,7 +275,7 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
  *   y = act(gamma xh + beta), gamma and beta [C], one value a channel.
  * Layouts, dtypes and activations as for the group norm above (rows of any other model are FNO_LAYOUT_CHANNELS_LAST).
  * Statistics and sums over channels are in float, about a mean of their own, so that a point's values may lie anywhere beside
- * their spread; bf16 results are rounded once, to nearest even.  Range: x to 1e18 in size; squares of deviations below
+ * their spread; bf16 results are rounded once, to nearest even.  Range: x to 5e16 in size (1e18 with up to 32 channels); squares of deviations below
  * 1e-38 are lost, which shows where eps is as small.  A NaN or an infinity makes all channels of its point NaN, and no other
  * point.  One channel gives xh = 0. */
 typedef struct {

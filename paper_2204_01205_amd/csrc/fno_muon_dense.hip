@@ -502,24 +502,24 @@ bool is_dense(const MuonTensor& t) { return !t.modes && !muon_is_small(t); }
 // Tiles of 128 read half as much for a product, and are worth it for matrices that have a few of them on a side, where all tensors together
 // fill the chip with them.  us a step with tiles of 64 and of 128: 1024 x 4096 481 and 420, eight of 1024 x 1024 912 and 788, 32 of
 // 512 x 512 562 and 529, but four of 1024 x 1024 526 and 541, 16 of 512 x 512 336 and 400, 64 of 192 x 192 172 and 244.
-int tile_side(const MuonTensor* t, int count, int k) {
-  const int m = t[k].rows < t[k].cols ? t[k].rows : t[k].cols;
-  if (m <= 192) return 64;
+constexpr int kNarrowSide = 192;
+int shorter_side(const MuonTensor& t) { return t.rows < t.cols ? t.rows : t.cols; }
+bool tiles_of_128(const MuonTensor* t, int count) {
   double steps = 0.0;
-  for (int i = 0; i < count; ++i) {
-    const int mi = t[i].rows < t[i].cols ? t[i].rows : t[i].cols, ni = t[i].rows + t[i].cols - mi;
-    if (is_dense(t[i]) && mi > 192) steps += (double)t[i].batch * (double)tiles_host(padded(mi, 128), 0, 128, 0) * (padded(ni, 128) / kStep);
+  for (int k = 0; k < count; ++k) {
+    const int m = shorter_side(t[k]), n = t[k].rows + t[k].cols - m;
+    if (is_dense(t[k]) && m > kNarrowSide) steps += (double)t[k].batch * (double)tiles_host(padded(m, 128), 0, 128, 0) * (padded(n, 128) / kStep);
   }
-  return steps >= 4500.0 ? 128 : 64;
+  return steps >= 4500.0;
 }
 
 template <int T>
-bool next_group(const MuonTensor* t, int count, double lr, int& k, long long& done, Group* g) {
+bool next_group(const MuonTensor* t, int count, bool wide, double lr, int& k, long long& done, Group* g) {
   g->l.count = 0;
   g->bytes = 0;
   long long part = 0;
   for (; k < count && g->l.count < kPerLaunch; ++k, done = 0) {
-    if (!is_dense(t[k]) || tile_side(t, count, k) != T) continue;
+    if (!is_dense(t[k]) || (wide && shorter_side(t[k]) > kNarrowSide) != (T == 128)) continue;
     const bool tall = t[k].rows > t[k].cols;
     DenseEntry e{};
     e.rows = t[k].rows;
@@ -621,9 +621,10 @@ hipError_t launch_group(Group& g, const MuonScalars& c, void* ws, hipStream_t s)
 }
 template <int T>
 hipError_t launch_side(const MuonTensor* t, int count, const MuonScalars& c, double lr, void* ws, hipStream_t s) {
+  const bool wide = tiles_of_128(t, count);
   int k = 0;
   long long done = 0;
-  for (Group g; next_group<T>(t, count, lr, k, done, &g);) {
+  for (Group g; next_group<T>(t, count, wide, lr, k, done, &g);) {
     const hipError_t e = launch_group<T>(g, c, ws, s);
     if (e != hipSuccess) return e;
   }
@@ -631,10 +632,11 @@ hipError_t launch_side(const MuonTensor* t, int count, const MuonScalars& c, dou
 }
 template <int T>
 size_t side_bytes(const MuonTensor* t, int count) {
+  const bool wide = tiles_of_128(t, count);
   size_t most = 0;
   int k = 0;
   long long done = 0;
-  for (Group g; next_group<T>(t, count, 0.0, k, done, &g);) most = (size_t)g.bytes > most ? (size_t)g.bytes : most;
+  for (Group g; next_group<T>(t, count, wide, 0.0, k, done, &g);) most = (size_t)g.bytes > most ? (size_t)g.bytes : most;
   return most;
 }
 

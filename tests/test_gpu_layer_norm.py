@@ -226,6 +226,42 @@ def test_without_gamma_and_beta(c, p, layout, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["first", "last"])
+@pytest.mark.parametrize("b,c,p", [(65535, 8, 1), (65535, 20, 5), (4097, 20, 64), (3000, 40, 65), (700, 300, 3)])
+def test_many_batch_entries_of_few_points(b, c, p, layout, dtype):
+    n = Layer(b, c, p, layout, dtype, "identity", seed=17)
+    n.check_forward(n.forward())
+    n.check_backward(*n.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c,p,layout", [(20, 300, "first"), (100, 70, "first"), (27, 300, "last"), (1000, 20, "last"), (5000, 9, "last")])
+@pytest.mark.parametrize("there", ["gamma", "beta"])
+def test_gamma_or_beta_alone(c, p, layout, there):
+    """The one that is not there stands for ones or zeros."""
+    n = Layer(2, c, p, layout, "f32", "gelu", seed=18)
+    if there == "gamma":
+        n.beta[:] = 0
+    else:
+        n.gamma[:] = 1
+    n.affine = lambda on=True: tuple(torch.from_numpy(t).cuda() if name == there else None for name, t in (("gamma", n.gamma), ("beta", n.beta)))
+    n.check_forward(n.forward())
+    n.check_backward(*n.backward())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c,layout", [(20, "first"), (32, "first"), (1000, "first"), (32, "last"), (383, "last"), (16384, "last")])
+def test_large_values(c, layout):
+    """The largest that the header names: squares of deviations and their sums stay within float."""
+    n = Layer(1, c, 70, layout, "f32", "identity", seed=19)
+    plain = n.forward()
+    size = np.float32(2.0 ** 59 if c <= 32 else 2.0 ** 55) / 2.0 ** np.ceil(np.log2(np.abs(n.x).max()))
+    n.x = (n.x * size).astype(np.float32)
+    assert np.abs(plain - n.forward()).max() <= 1e-4                # eps is gone beside them
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["first", "last"])
 @pytest.mark.parametrize("c", [20, 100, 700])
 def test_points_far_from_zero(layout, c):

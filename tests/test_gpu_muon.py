@@ -416,3 +416,22 @@ def test_the_binding_refuses_a_tensor_twice_and_lazy_views():
     for bad in (([c().conj()], [c()], [c()]), ([c()], [c().conj()], [c()]), ([c()], [c()], [c().conj()]), ([p], [torch._neg_view(g)], [other])):
         with pytest.raises(ValueError, match="view"):
             B.make_muon_tensors(*bad)
+
+
+@pytest.mark.gpu
+def test_graphs_of_kernels_that_ask_for_local_memory():
+    """More than 64 KB a block is asked of the runtime by every call, a captured one too."""
+    net = Muon([((32, 32, 40), True), ((32, 512), False), ((24, 31, 9), True)], seed=22)
+    eager = net.run(zero=False, lr=0.1)
+    for t, s in zip(net.dp + net.dm, net.params + net.momentum):
+        t.copy_(torch.from_numpy(s))
+    tensors = B.make_muon_tensors(net.dp, net.dg, net.dm, scale=-1.0)
+    ws, graph = B.alloc_muon_workspace(tensors), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.fno_muon_step(tensors, 0.1, 0.9, ws)
+    for _ in range(3):
+        for t, s in zip(net.dp + net.dm, net.params + net.momentum):
+            t.copy_(torch.from_numpy(s))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(t.cpu().numpy(), r) for t, r in zip(net.dp + net.dm, eager[0] + eager[1]))
