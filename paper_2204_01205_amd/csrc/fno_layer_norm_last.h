@@ -1,9 +1,9 @@
 // Layer norm of rows: fields [B][P][C], channels last.
 //
-// Up to some 400 channels (512 that are no whole 16-byte pieces) a wave takes a tile of rows, a stretch of memory that starts at a multiple of 16 bytes whatever C is: it goes
-// to LDS in 16-byte pieces, a group of G lanes (a power of two) takes a row, E = 4 .. 8 channels each, and the results
-// go the same way back.  A wave's LDS is its own, so waves need no barrier.  More channels: a row a wave or a block, in
-// registers, straight from memory.
+// Up to some 400 channels (512 that are no whole 16-byte pieces) a wave takes a tile of rows, a stretch of memory that starts at a
+// multiple of 16 bytes whatever C is: it goes to LDS in 16-byte pieces, a group of G lanes (a power of two) takes a row, E = 4 .. 8
+// channels each, and the results go the same way back.  A wave's LDS is its own, so waves need no barrier.  More channels: a row a wave
+// or a block, in registers, straight from memory.
 #pragma once
 #include "fno_layer_norm.h"
 

@@ -1,5 +1,6 @@
-// One Muon step over a list of matrices: which kernels take which tensor.  Spectral weights go mode by mode
-// (fno_muon_modes2.hip, fno_muon_modes5.hip, fno_muon_modes.hip), small real matrices a block each (fno_muon_small.hip), the others tile by tile (fno_muon_dense.hip).
+// One Muon step over a list of matrices: which kernels take which tensor.  Spectral weights go mode by mode (fno_muon_modes2.hip,
+// fno_muon_modes5.hip, fno_muon_modes.hip), small real matrices a block each (fno_muon_small.hip), the others tile by tile
+// (fno_muon_dense.hip).
 #include "fno_muon.h"
 
 namespace fno {

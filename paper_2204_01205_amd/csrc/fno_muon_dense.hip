@@ -10,9 +10,10 @@
 // is stored in pieces of 32 values, 64 bytes of first parts and 64 of second parts, a cache line that goes to LDS as it is; the
 // 16-byte pieces of a row are permuted by the row, so that the 16 rows that a phase of an LDS read takes lie in different banks.
 //
-// Five iterations of 4 x 1024 x 1024, 1024 x 4096, 4096 x 1024 and 1000 x 1536 (254 GFLOP) take 1.23 ms: 620 TFLOP/s of 16-bit products, where a
-// product of 8192^3 by the library reaches 1070; X = a X + B X alone runs at 770, the symmetric products, with fewer tiles than fit the chip
-// twice, at 590.  Smaller matrices are bound by their launches, three or four of 7 to 9 us an iteration (256 x 256).
+// Five iterations of 4 x 1024 x 1024, 1024 x 4096, 4096 x 1024 and 1000 x 1536 (254 GFLOP) take 1.23 ms: 620 TFLOP/s of 16-bit
+// products, where a product of 8192^3 by the library reaches 1070; X = a X + B X alone runs at 770, the symmetric products, with fewer
+// tiles than fit the chip twice, at 590.  Smaller matrices are bound by their launches, three or four of 7 to 9 us an iteration (256 x
+// 256).
 //
 // All matrices of a list go through a launch together, tile by tile.  Where these are too few for the chip, the sums are split over
 // blocks and added by a launch of their own.
@@ -480,8 +481,8 @@ __global__ __launch_bounds__(kThreads) void dense_sum_kernel(DenseList l, MuonSc
 
 constexpr long long kGroupBytes = 1ll << 30;     // scratch of the matrices that go through their launches together, where they are several
 constexpr unsigned kMostBlocks = 1u << 22;       // of a launch
-// 4 x 1024 x 1024, 1024 x 4096, 4096 x 1024 and 1000 x 1536 together: 1277 us with 256 blocks wanted, 1311 with 512, 1470 with 1024; shares of 16 or
-// 32 steps at least are slower too.
+// 4 x 1024 x 1024, 1024 x 4096, 4096 x 1024 and 1000 x 1536 together: 1277 us with 256 blocks wanted, 1311 with 512, 1470 with 1024;
+// shares of 16 or 32 steps at least are slower too.
 constexpr int kWantBlocks = 256, kLeastSteps = 8;
 
 long long tiles_host(long long mp, long long np, int T, int phase) {

@@ -1,10 +1,11 @@
 // The Muon step of spectral weights with 5 to 8 channels on either side: two tiles of 4 x 4 by two, four modes a wave.
 //
 // The weights of such a network are small (8 channels, 1536 modes: 0.8 MB), and what counts is the time that five iterations of three
-// dependent products take: 0.9 us each (fno_muon_modes.hip, with six barriers: 2.0).  The 16 outer products of a v_mfma_f32_4x4x1 are four modes times their four tiles, so that a product of
-// eight steps is 32 instructions, and nothing waits for another wave.  Lane 16 s + 4 md + j: tile (s / 2, s % 2), mode md, column
-// (or row) j of the tile; a register is a row.  X, A = X X^H and B = a + b A + c A A have a place each in a wave's LDS,
-// [row][column][mode] with four places of padding a row: rows and columns of a tile are read without bank conflicts.
+// dependent products take: 0.9 us each (fno_muon_modes.hip, with six barriers: 2.0).  The 16 outer products of a v_mfma_f32_4x4x1 are
+// four modes times their four tiles, so that a product of eight steps is 32 instructions, and nothing waits for another wave.  Lane 16
+// s + 4 md + j: tile (s / 2, s % 2), mode md, column (or row) j of the tile; a register is a row.  X, A = X X^H and B = a + b A + c A A
+// have a place each in a wave's LDS, [row][column][mode] with four places of padding a row: rows and columns of a tile are read without
+// bank conflicts.
 #include "fno_muon_modes.h"
 
 namespace fno {

@@ -1,18 +1,19 @@
 // The Muon step of spectral weights with 17 to 20 channels on either side: five tiles of 4 x 4 by five, four modes a wave.
 //
 // Five columns of tiles do not go evenly over the four vector units of a compute unit, and in a block that shares a mode's matrices
-// every phase waits for the slowest wave (fno_muon_modes.hip takes 1563 us for five iterations of 110592 modes, of
-// which matrix instructions are 540).  Here a wave has four modes to itself and nothing waits for another wave: the 16 outer products of a v_mfma_f32_4x4x1
-// are four modes times four tiles.  Lane 16 s + 4 md + j: tile slot s, mode md, column (or row) j of a tile.
+// every phase waits for the slowest wave (fno_muon_modes.hip takes 1563 us for five iterations of 110592 modes, of which matrix
+// instructions are 540).  Here a wave has four modes to itself and nothing waits for another wave: the 16 outer products of a
+// v_mfma_f32_4x4x1 are four modes times four tiles.  Lane 16 s + 4 md + j: tile slot s, mode md, column (or row) j of a tile.
 //   X: columns 4 s + j of all rows in registers (`x`), and of the fifth column of tiles, row tile s (`y`) and row tile 4 (`z`, in
 //   slot 0; the other slots work it out too).
-//   A = X X^H, B = b A + c A A: tiles (s, s), (s, s + 1), (s, s + 2) around the corner of five, and (4, 4), (4, 0), (4, 1) in slots 0 .. 2:
+//   A = X X^H, B = b A + c A A: tiles (s, s), (s, s + 1), (s, s + 2) around the corner of five, and (4, 4), (4, 0), (4, 1) in slots
+//   0 to 2:
 //   all 15 pairs.  X = a X + B X: five row tiles in four slots, and the fifth column in two turns: 28 instructions a step for 25
 //   tiles' worth.
-// 110592 modes take 1005 us, 154 an iteration (108 of matrix instructions, the rest vector instructions and LDS that the two waves of a vector
-// unit do not hide); loads and stores alone 529 us, nearly all behind the other waves' iterations.
-// X, A and B take turns in a wave's 13 KB of LDS, [row][column][mode] with four places of padding a row: rows and columns of a tile
-// are read without bank conflicts.  The fifth column of X has a place of its own beside them.
+// 110592 modes take 1005 us, 154 an iteration (108 of matrix instructions, the rest vector instructions and LDS that the two waves of
+// a vector unit do not hide); loads and stores alone 529 us, nearly all behind the other waves' iterations.
+// X, A and B take turns in a wave's 13 KB of LDS, [row][column][mode] with four places of padding a row: rows and columns of a tile are
+// read without bank conflicts.  The fifth column of X has a place of its own beside them.
 #include "fno_muon_modes.h"
 
 #include <type_traits>
@@ -322,7 +323,8 @@ hipError_t launch_muon_modes5(const MuonTensor* t, int count, const MuonScalars&
   for (int k = 0; k < count; ++k) {
     if (!muon_is_modes5(t[k])) continue;
     const bool tall = t[k].rows > t[k].cols;
-    const long long row = (long long)t[k].cols * t[k].batch, column = t[k].batch, blocks = (t[k].batch + kWaves * kWaveModes - 1) / (kWaves * kWaveModes);
+    const long long row = (long long)t[k].cols * t[k].batch, column = t[k].batch;
+    const long long blocks = (t[k].batch + kWaves * kWaveModes - 1) / (kWaves * kWaveModes);
     for (long long done = 0; done < blocks;) {
       if (l.count == kPerLaunch || l.blocks == kMost) {
         const hipError_t e = flush();

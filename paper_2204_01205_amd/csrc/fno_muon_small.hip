@@ -248,8 +248,8 @@ __global__ __launch_bounds__(64 * kMostWaves) void muon_small_kernel(SmallList l
 
 }  // namespace
 
-// What fits a block's LDS.  us a step of one matrix, here and tile by tile (fno_muon_dense.hip): 8 x 8 8 and 60, 32 x 256 30 and 73, 32 x 512 49
-// and 84; of 1024 of 32 x 512 210 and 835.
+// What fits a block's LDS.  us a step of one matrix, here and tile by tile (fno_muon_dense.hip): 8 x 8 8 and 60, 32 x 256 30 and 73, 32
+// x 512 49 and 84; of 1024 of 32 x 512 210 and 835.
 bool muon_is_small(const MuonTensor& t) {
   const int m = t.rows < t.cols ? t.rows : t.cols;
   return !t.modes && m <= 32 && (long long)t.rows * t.cols <= 16384;
