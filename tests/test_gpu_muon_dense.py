@@ -27,9 +27,10 @@ STACK = [((9, 1023, 1025), False)]
 AT_LEAST = [((1024, 4000), False)]                       # 36 tiles of a symmetric product, 128 steps each
 BELOW = [((1024, 3968), False)]                          # 124 steps
 SQUARES = [((4, 1024, 1024), False), ((1000, 1536), False)]
+ONE = [((1640, 1660), False)]                             # 169 tiles of the last product, whose sums are split too
 MIXED = [((150, 700), False), ((1000, 4100), False), ((4, 64, 65), False), ((20, 20, 33), True), ((193, 257), False), ((192, 900), False),
          ((2, 300, 250), False), ((20, 128), False)]
-IN_128 = dict(wide=WIDE, tall=TALL, stack=STACK, at_least=AT_LEAST, squares=SQUARES, mixed=MIXED)
+IN_128 = dict(wide=WIDE, tall=TALL, stack=STACK, at_least=AT_LEAST, squares=SQUARES, one=ONE, mixed=MIXED)
 IN_64 = [(33, 33), (33, 40), (48, 200), (64, 64), (65, 64), (96, 130), (129, 128), (200, 333), (256, 256), (37, 512), (1000, 36), (257, 600), (512, 384),
          (192, 1000)]
 
