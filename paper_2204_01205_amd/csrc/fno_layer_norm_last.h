@@ -179,12 +179,13 @@ void with_channels(int C, F&& f) {
 template <int SIZE, bool BWD, class F>
 void with_row(int C, F&& f) {
   const int pieces = (C * SIZE + 1023) / 1024;             // of a wave
-  if (pieces <= 2) f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-  else if (pieces <= 4) f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-  else if (pieces <= 8) f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
-  else if (pieces <= 16 && !(BWD && SIZE == 2)) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-  else if (pieces <= 32) f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
-  else if constexpr (SIZE == 4) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
+  if (pieces <= 2) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+  if (pieces <= 4) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+  if (pieces <= 8) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+  if constexpr (!(BWD && SIZE == 2))
+    if (pieces <= 16) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+  if (pieces <= 32) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+  if constexpr (SIZE == 4) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
 }
 inline int size_of(const LayerShape& n) { return n.bf16 ? 2 : 4; }
 // Rows that are wide enough go without LDS, in bf16 where they are whole 16-byte pieces.  us for 65536 rows, forward and adjoint, in
