@@ -206,6 +206,9 @@ inline long long row_tiles(const LayerShape& n) {
   const Rows r = rows_of(n);
   return (r.rows + r.each - 1) / r.each;
 }
+// A wave's tile is at most 64 lanes by 8 channels in each of its passes.
+static_assert(2 * 4 * 64 * 8 * kPasses<float> * sizeof(float) <= 65536 && 2 * 4 * 64 * 8 * kPasses<u16> * sizeof(u16) <= 65536,
+              "the adjoint's two tiles of four waves stay within what a block has without asking");
 inline size_t tile_bytes(const LayerShape& n) { return (size_t)4 * rows_of(n).each * n.C * size_of(n); }      // of a block's four waves
 
 }  // namespace

@@ -185,8 +185,7 @@ int layer_last_blocks(const LayerShape& n) {
 }
 
 hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) {
-  hipError_t set = hipSuccess;
-  const hipError_t e = with_layer_kind(c.n, [&](auto t, auto act, auto stream) {
+  return with_layer_kind(c.n, [&](auto t, auto act, auto stream) {
     using T = decltype(t);
     constexpr int ACT = decltype(act)::value;
     constexpr bool S = decltype(stream)::value;
@@ -197,9 +196,8 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
     if (in_tiles(c.n)) {
       with_channels<sizeof(T)>(a.C, [&](auto e, auto whole) {
           const size_t sums = (size_t)8 * a.C * sizeof(float), bytes = 2 * tile_bytes(c.n) > sums ? 2 * tile_bytes(c.n) : sums;
-          const auto kernel = tile_bwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>;
-          set = ask_local_memory(reinterpret_cast<const void*>(kernel), bytes);
-          if (set == hipSuccess) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, s, a, rows_of(c.n), x, gy, gx);
+          hipLaunchKernelGGL((tile_bwd_kernel<T, decltype(e)::value, decltype(whole)::value, ACT, S>), dim3(blocks), dim3(kThreads), bytes, s, a,
+                             rows_of(c.n), x, gy, gx);
       });
     } else {
       with_row<sizeof(T), true>(a.C, [&](auto w, auto n) {
@@ -209,7 +207,6 @@ hipError_t launch_layer_last_bwd(const LayerCall& c, int blocks, hipStream_t s) 
       });
     }
   });
-  return set != hipSuccess ? set : e;
 }
 
 }  // namespace fno
