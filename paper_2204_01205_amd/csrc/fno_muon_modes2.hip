@@ -21,7 +21,7 @@ struct Modes2Entry {
   const float2* g;
   float2* mom;
   long long modes;
-  unsigned first, skip;                // first block of the launch that belongs to this tensor; blocks of it in earlier launches
+  unsigned first;                      // first block of the launch that belongs to this tensor
   int m, n;
   float keep, move;                    // 1 - lr weight_decay, lr scale
 };
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * kWaves) void muon_modes2_kernel(Modes2List l, 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 3, md = (lane >> 2) & 3;
   const int I = lane >> 5, J = (lane >> 4) & 1, row0 = 4 * I, col = 4 * J + j;
   float2 *const X = lds[w], *const A = X + kMatrix, *const B = A + kMatrix;
-  const long long mode = (((long long)(item - t.first) + t.skip) * kWaves + w) * kWaveModes + md;
+  const long long mode = ((long long)(item - t.first) * kWaves + w) * kWaveModes + md;
   const bool here = mode < t.modes && col < t.n;
 
   // What lies past the matrix or the last mode is read from its last place, becomes a zero that stays one, and is not stored.
@@ -163,9 +163,9 @@ bool muon_is_modes2(const MuonTensor& t) {
   return t.modes && t.rows > 4 && t.rows <= 8 && t.cols > 4 && t.cols <= 8 && t.batch <= 65536;
 }
 
-// Launches of 2^22 blocks at most.
+// 32 tensors a launch: 2^17 blocks at most.
 hipError_t launch_muon_modes2(const MuonTensor* t, int count, const MuonScalars& c, double lr, hipStream_t s) {
-  constexpr long long kMost = 1ll << 22, kModes = kWaves * kWaveModes;
+  constexpr int kModes = kWaves * kWaveModes;
   Modes2List l;
   l.count = 0;
   l.blocks = 0;
@@ -178,19 +178,14 @@ hipError_t launch_muon_modes2(const MuonTensor* t, int count, const MuonScalars&
   };
   for (int k = 0; k < count; ++k) {
     if (!muon_is_modes2(t[k])) continue;
-    const long long blocks = (t[k].batch + kModes - 1) / kModes;
-    for (long long done = 0; done < blocks;) {
-      if (l.count == kPerLaunch || l.blocks == kMost) {
-        const hipError_t e = flush();
-        if (e != hipSuccess) return e;
-      }
-      const long long here = blocks - done < kMost - l.blocks ? blocks - done : kMost - l.blocks;
-      l.t[l.count++] = Modes2Entry{reinterpret_cast<float2*>(t[k].p), reinterpret_cast<const float2*>(t[k].g),
-                                   reinterpret_cast<float2*>(t[k].m), (long long)t[k].batch, l.blocks, (unsigned)done, t[k].rows, t[k].cols,
-                                   (float)(1.0 - lr * t[k].decay), (float)(lr * t[k].scale)};
-      l.blocks += (unsigned)here;
-      done += here;
+    if (l.count == kPerLaunch) {
+      const hipError_t e = flush();
+      if (e != hipSuccess) return e;
     }
+    l.t[l.count++] = Modes2Entry{reinterpret_cast<float2*>(t[k].p), reinterpret_cast<const float2*>(t[k].g),
+                                 reinterpret_cast<float2*>(t[k].m), (long long)t[k].batch, l.blocks, t[k].rows, t[k].cols,
+                                 (float)(1.0 - lr * t[k].decay), (float)(lr * t[k].scale)};
+    l.blocks += (unsigned)((t[k].batch + kModes - 1) / kModes);
   }
   return flush();
 }
