@@ -256,10 +256,12 @@ inline int ilog2(int v) { int l = 0; while ((1 << l) < v) ++l; return l; }
 
 }  // namespace
 
-// Asks for `bytes` of local memory a block, which 64 KB need not be asked for.  A refusal leaves no error for the next call.
-inline hipError_t ask_local_memory(const void* kernel, size_t bytes) {
+// Before a launch with `bytes` of local memory a block: 64 KB need not be asked for; for more a kernel asks for `most`, the largest of its
+// launches, whatever this one takes, since another thread may launch the same kernel at the same time.  A refusal leaves no error for
+// the next call.
+inline hipError_t ask_local_memory(const void* kernel, size_t bytes, size_t most) {
   if (bytes <= 64 * 1024) return hipSuccess;
-  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
   if (e != hipSuccess) (void)hipGetLastError();
   return e;
 }

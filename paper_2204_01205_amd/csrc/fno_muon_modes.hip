@@ -275,9 +275,9 @@ __global__ __launch_bounds__(512) void muon_modes_kernel(ModesList l, MuonScalar
 
 template <int TM>
 hipError_t launch_tiles(int tn, const ModesList& l, const MuonScalars& c, hipStream_t s) {
-  const int rx = 64 * tn + 1;
-  const size_t bytes = (size_t)4 * TM * rx * sizeof(float2);
-  const hipError_t e = ask_local_memory(reinterpret_cast<const void*>(muon_modes_kernel<TM>), bytes);
+  auto rows = [](int tn) { return (size_t)4 * TM * (64 * tn + 1) * sizeof(float2); };
+  const size_t bytes = rows(tn);
+  const hipError_t e = ask_local_memory(reinterpret_cast<const void*>(muon_modes_kernel<TM>), bytes, rows(8));
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(muon_modes_kernel<TM>, dim3((l.blocks + 7) / 8 * 8), dim3(64 * tn), bytes, s, l, c);
   return hipGetLastError();

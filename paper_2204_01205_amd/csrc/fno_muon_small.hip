@@ -248,11 +248,15 @@ __global__ __launch_bounds__(64 * kMostWaves) void muon_small_kernel(SmallList l
 
 }  // namespace
 
+// A block's LDS at most: 16384 values; in each of 32 rows up to 3 more for the folds and 67 of padding; 8192 of sums.
+constexpr int kMostValues = 16384;
+constexpr size_t kMostLocal = (kMostValues + 32 * (3 + 67) + 8192) * sizeof(float);
+
 // What fits a block's LDS.  us a step of one matrix, here and tile by tile (fno_muon_dense.hip): 8 x 8 8 and 60, 32 x 256 30 and 73, 32
 // x 512 49 and 84; of 1024 of 32 x 512 210 and 835.
 bool muon_is_small(const MuonTensor& t) {
   const int m = t.rows < t.cols ? t.rows : t.cols;
-  return !t.modes && m <= 32 && (long long)t.rows * t.cols <= 16384;
+  return !t.modes && m <= 32 && (long long)t.rows * t.cols <= kMostValues;
 }
 
 // Stacks go in launches of 2^22 matrices at most.
@@ -266,7 +270,7 @@ hipError_t launch_muon_small(const MuonTensor* t, int count, const MuonScalars& 
   auto flush = [&]() {
     hipError_t e = hipSuccess;
     if (l.count > 0) {
-      e = ask_local_memory(reinterpret_cast<const void*>(muon_small_kernel), bytes + kMostWaves * sizeof(double));
+      e = ask_local_memory(reinterpret_cast<const void*>(muon_small_kernel), bytes, kMostLocal);
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(muon_small_kernel, dim3((unsigned)blocks), dim3(64 * waves), bytes, s, l, c);
       e = hipGetLastError();
