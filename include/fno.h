@@ -277,10 +277,10 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
  * Statistics and sums over channels are in float, about a mean of their own, so that a point's values may lie anywhere beside
  * their spread; bf16 results are rounded once, to nearest even.  Range: x to 5e16 in size (1e18 with up to 32 channels); squares of deviations below
  * 1e-38 are lost, which shows where eps is as small.  A NaN or an infinity makes all channels of its point NaN, and no other
- * point.  One channel gives xh = 0. */
+ * point.  One channel gives xh = 0; so do equal channels of any value v, within 1e-11 |v| / sqrt(eps). */
 typedef struct {
   int64_t npoints;     /* P >= 0                                                      */
-  double eps;          /* >= 0, finite; with 0 a point of equal channels gives NaN    */
+  double eps;          /* >= 0, finite; with 0 a point of equal channels has no value: NaN, or what rounding leaves */
   int32_t batch;       /* B, 1 .. 65535                                               */
   int32_t channels;    /* C, 1 .. 1024 channels first, 1 .. 16384 channels last       */
   int32_t layout;      /* FNO_LAYOUT_*                                                */

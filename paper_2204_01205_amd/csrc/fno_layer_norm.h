@@ -103,9 +103,10 @@ __device__ __forceinline__ void store_some(T* p, int count, const float (&v)[V])
 
 // Statistics of a point in two sweeps over registers.  about = sum x / C is the mean up to its rounding; with d = x - about, which is
 // exact near it, the mean is about + off with off = sum d / C, and the variance sum d^2 / C - off^2, from which next to nothing is
-// subtracted.  xh = (d - off) rstd.
+// subtracted.  Where all channels are the same, far from zero, that difference is rounding of either sign: with eps it counts as eps at
+// least (a comparison, so that a NaN stays one).  xh = (d - off) rstd.
 __device__ __forceinline__ float rstd_of(const LayerArgs& a, float off, float squares) {
-  const float var = fmaf(squares, a.inv_c, fmaf(-off, off, a.eps));
+  const float sum = fmaf(squares, a.inv_c, fmaf(-off, off, a.eps)), var = sum < a.eps ? a.eps : sum;
   const float r = __builtin_amdgcn_rsqf(var);
   // one Newton step: the instruction is off by an ulp.  An infinite r (a variance of zero) stays one, and so does a NaN.
   const float e = fmaf(-var * r, r, 1.0f);
