@@ -528,6 +528,8 @@ def alloc_muon_workspace(tensors: MuonTensors, device="cuda") -> torch.Tensor:
 
 def fno_muon_step(tensors: MuonTensors, lr, momentum, ws, iterations=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7,
                   nesterov=True, grad_norm=None, max_norm=1.0) -> None:
+    if len(coefficients) != 3:
+        raise ValueError(f"the polynomial has three coefficients, not {len(coefficients)}")
     stream = _list_stream(tensors)
     if tensors.device is not None:
         _one_device(tensors.device, ws, grad_norm)
