@@ -280,7 +280,7 @@ int fno_group_norm_bwd(const fno_norm_desc* desc, const void* x, const float* ga
  * point.  One channel gives xh = 0; so do equal channels of any value v, within 1e-11 |v| / sqrt(eps). */
 typedef struct {
   int64_t npoints;     /* P >= 0                                                      */
-  double eps;          /* >= 0, finite; with 0 a point of equal channels has no value: NaN, or what rounding leaves */
+  double eps;          /* >= 0, finite; with 0 equal channels have no value: NaN, or rounding */
   int32_t batch;       /* B, 1 .. 65535                                               */
   int32_t channels;    /* C, 1 .. 1024 channels first, 1 .. 16384 channels last       */
   int32_t layout;      /* FNO_LAYOUT_*                                                */
@@ -350,7 +350,8 @@ int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* c
                          void* stream);
 
 /* One Muon step over many tensors of matrices, in place: the momentum of every matrix, made orthogonal by Newton-Schulz
- * products (Higham, Functions of Matrices, ch. 8), is what moves it.  For every matrix on its own
+ * products (Higham, Functions of Matrices, ch. 8), is what moves it (Jordan et al., 2024: Muon, an optimizer for the hidden layers of neural
+ * networks, whose coefficients a, b, c = 3.4445, -4.7750, 2.0315 are the binding's).  For every matrix on its own
  *   g' = s g;  m = momentum m + g';  u = g' + momentum m where nesterov is set, else m;  X = u / (||u||_F + eps);
  *   `iterations` times:  X = a X + (b A + c A A) X,  A = X X^H;
  *   param = param (1 - lr weight_decay) - lr scale X,
@@ -362,9 +363,10 @@ int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* c
  * for every kept mode, the map that the mode mix applies there.  rows, cols <= 32 (FNO_EUNSUPPORTED beyond).
  *
  * Products: single precision for spectral weights and for real matrices with up to 32 on their shorter side and 16384 values;
- * for the others sums of products of 16-bit parts that carry 22 bits of a value, as long as X stays within 64, A within 256 and
- * b A + c A A within 1024 (singular values of X up to 1.2, which the usual coefficients keep, are far from that; what leaves these
- * ranges becomes infinite or NaN).  Sums in float in a fixed order: the same bits on every run of the same list.
+ * for the others sums of products of 16-bit parts that carry 22 bits of a value, none of them below 2^-35 in X, 2^-33 in A and
+ * 2^-31 in b A + c A A, as long as X stays within 64, A within 256 and b A + c A A within 1024 (singular values of X up to 1.2,
+ * which the usual coefficients keep, are far from that; what leaves these ranges becomes infinite or NaN).  Sums in float in a
+ * fixed order: the same bits on every run of the same list.
  *
  * tensors, options: host memory, read during the call only; pointers in tensors are device pointers, param, grad and momentum
  * 4-byte aligned (8-byte: complex ones).  Tensors must not overlap.  Empty tensors (batch, rows or cols 0) and count = 0 are

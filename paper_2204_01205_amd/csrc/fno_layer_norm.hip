@@ -2,8 +2,8 @@
 // first, fno_layer_norm_first.hip) or [B][P][C] (channels last, fno_layer_norm_last.hip) in float or bf16.
 //
 // What the operator moves bounds it: x in and y out (adjoint: x and gy in, gx out), 20 to 40 operations a value.  A point's channels
-// fit the registers of a lane, a group of lanes or a block, so every value is read once; the adjoint works the statistics out again
-// from them.  Measured where an elementwise sum of large arrays reaches 5.9 to 6.2 TB/s: forward, 20 channels, 60 x 60 x 64 x 30
+// fit the registers of a lane, a group of lanes or a block, so every value is read once (but gy of more than 512 channels first); the adjoint works
+// the statistics out again from them.  Measured where an elementwise sum of large arrays reaches 5.9 to 6.2 TB/s: forward, 20 channels, 60 x 60 x 64 x 30
 // points, 207 us = 5.3 TB/s; adjoint, 20 channels, 128 x 128 x 64 x 32 points, 1545 us = 5.2 TB/s; adjoint of 32768 rows of 1024 in
 // bf16, 54 us = 3.7 TB/s.  The gradients of gamma and beta are sums over all points: lanes add up what they see in float over their
 // tiles, blocks write their sums, and one more launch adds the blocks' in double, in a fixed order.

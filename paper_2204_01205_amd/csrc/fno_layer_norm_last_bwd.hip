@@ -73,6 +73,8 @@ __global__ __launch_bounds__(kThreads) void tile_bwd_kernel(LayerArgs a, Rows r,
     a.part[(long long)blockIdx.x * 2 * a.C + k] = (sums[k] + sums[2 * a.C + k]) + (sums[4 * a.C + k] + sums[6 * a.C + k]);
 }
 
+// With sixteen waves a row (f32 from 8193 channels, bf16 from 4097 on) 128 registers do not hold all: 2 are spilled, and with an activation 24 to
+// 34, 100 to 140 bytes a lane (4096 rows of 16384, GELU against none: f32 259 and 211 us, bf16 170 and 136).
 template <class T, int W, int N, int ACT, bool STREAM>
 __global__ __launch_bounds__(kRowThreads<W>) void wide_bwd_kernel(LayerArgs a, long long rows, const T* x, const T* gy, T* gx) {
   constexpr int V = kVec<T>, STEP = 64 * W * V, PER = W == 1 ? 4 : 1;
@@ -164,7 +166,8 @@ __global__ __launch_bounds__(kRowThreads<W>) void wide_bwd_kernel(LayerArgs a, l
 
 // ------------------------------------------------------------------------------------------ launches
 
-// `most` blocks, more where a lane's chain of additions would be longer than 256 rows or tiles; 2^20 is past any memory.
+// `most` blocks, more where a lane's chain of additions would be longer than 256 rows or tiles (2048 terms of eight rows a tile); 2^20 is past
+// any memory.
 int blocks_for(long long items, int each, int most) {
   const long long b = (items + each - 1) / each;
   return (int)std::min(b, std::clamp(b / 256, (long long)most, 1ll << 20));

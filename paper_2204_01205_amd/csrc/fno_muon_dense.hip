@@ -3,8 +3,9 @@
 // Of the three products of an iteration the first two, A = X X^T and B = b A + c A A, are symmetric and half of their tiles are
 // worked out; the third is X = a X + B X.  They run on 16-bit matrix instructions: a value is the sum of two fp16 ones (the
 // second holds what the first rounds off, together 22 bits), and of the four products of two such pairs three count.  That is a third of
-// the 16-bit rate, five times the rate of single-precision products.  X, A and B are scaled by powers of two (kX, kA, kB) so that what the
-// pairs cannot hold lies below 2^-35 of their values of order one, and that values up to 64, 256 and 1024 fit.
+// the 16-bit rate, five times the rate of single-precision products.  X, A and B are scaled by powers of two (kX, kA, kB) so that values
+// up to 64, 256 and 1024 fit; what the pairs cannot hold, half of fp16's smallest step, is then 2^-35, 2^-33 and 2^-31.  For values from 2^-13,
+// 2^-11 and 2^-9 on the 22 bits are the limit.
 //
 // All operands are read along their inner dimension: X by rows and by columns (both are written), A and B are symmetric.  A row
 // is stored in pieces of 32 values, 64 bytes of first parts and 64 of second parts, a cache line that goes to LDS as it is; the
@@ -12,7 +13,8 @@
 //
 // Five iterations of 4 x 1024 x 1024, 1024 x 4096, 4096 x 1024 and 1000 x 1536 (254 GFLOP) take 1.23 ms: 620 TFLOP/s of 16-bit
 // products, where a product of 8192^3 by the library reaches 1070; X = a X + B X alone runs at 770, the symmetric products, with fewer
-// tiles than fit the chip twice, at 590.  Smaller matrices are bound by their launches, three or four of 7 to 9 us an iteration (256 x
+// tiles than fit the chip twice, at 590.  A step of 32 of a tile of 128 reads 64 KB of LDS and writes 32 for some 768 cycles of matrix
+// instructions, 125 bytes a cycle, which is about what LDS gives.  Smaller matrices are bound by their launches, three or four of 7 to 9 us an iteration (256 x
 // 256).
 //
 // All matrices of a list go through a launch together, tile by tile.  Where these are too few for the chip, the sums are split over

@@ -9,7 +9,9 @@
 //   the mirrors, operands from LDS (X by rows, A by columns);
 //   X = B X: its own columns, B from LDS.
 // Matrix instructions bound it: 110592 modes of 16 x 16 take 86 us an iteration, of which these are 52; the rest are the waits of a block's
-// waves for each other and for LDS.  Loads and stores alone take 275 us (4.1 TB/s).
+// waves for each other and for LDS.  Loads and stores alone take 275 us (4.1 TB/s).  Beyond 20 channels a compute unit has room for two
+// blocks or, from 25 on, for one (101 to 131 KB), which all wait at a barrier: 24 channels take 329 us an iteration, 32 channels 593.  (With 25 to 32
+// on the shorter side two of 256 registers are spilled, 12 bytes a lane.)
 // X, A and B take turns in one LDS buffer, [row][tile][mode][column] with one entry of padding a row: a tile read by columns
 // is contiguous, one read by rows has its four rows in neighbouring banks.
 #include "fno_muon_modes.h"

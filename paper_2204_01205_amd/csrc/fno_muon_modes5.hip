@@ -10,8 +10,9 @@
 //   0 to 2:
 //   all 15 pairs.  X = a X + B X: five row tiles in four slots, and the fifth column in two turns: 28 instructions a step for 25
 //   tiles' worth.
-// 110592 modes take 1005 us, 154 an iteration (108 of matrix instructions, the rest vector instructions and LDS that the two waves of
-// a vector unit do not hide); loads and stores alone 529 us, nearly all behind the other waves' iterations.
+// 110592 modes take 1005 to 1046 us, 154 an iteration (108 of matrix instructions, the rest vector instructions and LDS that the two waves of
+// a vector unit do not hide); loads and stores alone take 529 us, 3.3 TB/s, as a wave touches 32 bytes of a cache line, and some 240 of them are
+// not behind other waves' iterations.
 // X, A and B take turns in a wave's 13 KB of LDS, [row][column][mode] with four places of padding a row: rows and columns of a tile are
 // read without bank conflicts.  The fifth column of X has a place of its own beside them.
 #include "fno_muon_modes.h"
