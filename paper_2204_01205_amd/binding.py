@@ -488,7 +488,7 @@ def make_muon_tensors(params, grads, momentum, scale=1.0, weight_decay=0.0) -> M
     scale, decay = each(scale), each(weight_decay)
     if not (len(grads) == len(momentum) == len(scale) == len(decay) == count):
         raise ValueError("params, grads, momentum, scale and weight_decay must have one entry a tensor")
-    array, devices, written = (FnoMuonTensor * max(count, 1))(), set(), set()
+    array, devices, written, spans = (FnoMuonTensor * max(count, 1))(), set(), set(), []
     for k in range(count):
         p, is_complex = params[k], params[k].is_complex()
         if p.dim() < 2 or (not is_complex and p.dim() > 3):
@@ -507,12 +507,19 @@ def make_muon_tensors(params, grads, momentum, scale=1.0, weight_decay=0.0) -> M
                 if t.data_ptr() in written:
                     raise ValueError(f"{name}[{k}] is in the list already")
                 written.add(t.data_ptr())
+            if t.numel():
+                spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grads", f"{name}[{k}]"))
         array[k] = FnoMuonTensor(_ptr(p, name=f"params[{k}]"), _ptr(grads[k], name=f"grads[{k}]"),
                                  _ptr(momentum[k], name=f"momentum[{k}]"), batch, rows, cols,
                                  FNO_MUON_MODES if is_complex else FNO_MUON_MATRICES, scale[k], decay[k])
         devices |= {t.device for t in (p, grads[k], momentum[k])}
     if len(devices) > 1:
         raise ValueError("all tensors of a list must live on one GPU")
+    ends = [0, 0]                                          # of what is read and what is written so far, by address
+    for start, end, is_written, name in sorted(spans):
+        if start < ends[1] or (is_written and start < ends[0]):
+            raise ValueError(f"{name} overlaps a tensor of the list, and the step writes one of them")
+        ends[is_written] = max(ends[is_written], end)
     return MuonTensors(array, count, devices.pop() if devices else None, (list(params), list(grads), list(momentum)))
 
 
