@@ -366,7 +366,8 @@ int fno_adamw_state_read(int32_t count, const fno_adamw_tensor* tensors, void* c
  * for the others sums of products of 16-bit parts that carry 22 bits of a value, none of them below 2^-35 in X, 2^-33 in A and
  * 2^-31 in b A + c A A, as long as X stays within 64, A within 256 and b A + c A A within 1024 (singular values of X up to 1.2,
  * which the usual coefficients keep, are far from that; what leaves these ranges becomes infinite or NaN).  Sums in float in a
- * fixed order: the same bits on every run of the same list.
+ * fixed order: the same bits on every run of the same list.  Norms: squares in double, those of spectral matrices in float where it
+ * holds them (sums between 1e-28 and 1e30).
  *
  * tensors, options: host memory, read during the call only; pointers in tensors are device pointers, param, grad and momentum
  * 4-byte aligned (8-byte: complex ones).  Tensors must not overlap.  Empty tensors (batch, rows or cols 0) and count = 0 are
